@@ -221,6 +221,66 @@ int dflash_kv_commit(dflash_ctx *ctx, const dflash_batch *batch, const int32_t *
 int dflash_prefill(dflash_ctx *ctx, const dflash_batch *batch, const int32_t *tokens, const int32_t *prompt_lens,
                    int32_t *first_tokens, void *stream);
 
+/* ---- sequences that share pages ---------------------------------------------------------------
+ * Several samples of one prompt, beams, requests under one system prompt: block-table rows that name the same pages.  The ledger
+ * calls below keep a block table and a count of who holds which page on the device; the step's calls take their batch from the
+ * ledger's arrays (its first n_seqs rows).  Every call is enqueued on `stream`, reads nothing back and allocates nothing.  Page ids are
+ * taken in ascending order for rows in ascending order: what a call does depends on the ledger alone.  Entries outside the pool count
+ * as "no page". */
+typedef struct {
+  int32_t n_rows;       /* rows of the arrays below: sequences that run, that wait, and room for more */
+  int32_t *block_table; /* (device) [n_rows, max_pages_per_seq] page ids, -1 = none */
+  int32_t *seq_lens;    /* (device) [n_rows] committed length */
+  int32_t *anchor;      /* (device) [n_rows] clean token behind the committed ones */
+  int32_t *page_refs;   /* (device) [n_pages] block-table entries that hold the page, 0 = free.  A caller that fills block_table by
+                           itself keeps these counts; to begin with, all entries are -1 and all counts 0 */
+} dflash_ledger;
+
+/* Children become what their parents are: children[i] gives its pages back and shares the pages of parents[i]'s committed tokens, whose
+ * length and anchor it takes (no page is copied: see dflash_pages_reserve).  parents, children (host) [n], read before the call
+ * returns.  A parent may have many children; a row may be a child once and then not a parent in the same call. */
+int dflash_pages_fork(dflash_ctx *ctx, const dflash_ledger *ledger, int32_t n, const int32_t *parents, const int32_t *children, void *stream);
+
+/* Rows 0..n-1 (n <= max_seqs) get pages of their own for tokens[s] more tokens (device, [n]; 0 or less = the row is left alone): to be
+ * called before whatever writes K/V rows (dflash_draft_block and dflash_verify write a block of B behind seq_lens[s], dflash_prefill the prompt
+ * rounded up to whole blocks).  In the range of positions seq_lens[s] .. seq_lens[s] + tokens[s] - 1 a missing page is taken from the free ones, a page
+ * that other rows hold too is replaced by a free one.  If committed tokens stand in it, their rows (the first seq_lens[s] % 16 rounded up to
+ * four) are copied in every layer of both pools; the last of the call's rows to ask for such a page keeps it when all other holders have
+ * got copies.  A row gets all it asks for or nothing, and behind the first row for which too few pages are free no row gets any.
+ * granted (device, nullable) [n]: 1 if the row now holds every page of its range alone (or asked for none), 0 if not: it must not be written
+ * to then.  Rows that got 0 (too few free pages, or the block-table row is too short) raise the sticky device status. */
+int dflash_pages_reserve(dflash_ctx *ctx, const dflash_ledger *ledger, int32_t n, const int32_t *tokens, int32_t *granted, void *stream);
+
+/* rows[i] gives back the pages behind its first keep[i] tokens (keep null: all pages) and is cut to that length.  rows, keep (host) [n], read
+ * before the call returns; no row twice. */
+int dflash_pages_release(dflash_ctx *ctx, const dflash_ledger *ledger, int32_t n, const int32_t *rows, const int32_t *keep, void *stream);
+
+/* Moves the pages in use to the lowest ids: with L of them, the k-th one at or behind id L goes to the k-th free id below L, in every
+ * layer of both pools; all n_rows block-table rows and the counts follow.  n_live (device, nullable) [1] = L. */
+int dflash_pages_compact(dflash_ctx *ctx, const dflash_ledger *ledger, int32_t *n_live, void *stream);
+
+/* How a batch is cut into groups of consecutive sequences whose block-table rows are expected to begin with the same pages.  What they do
+ * have in common, committed and whole pages, is found on the device: any grouping gives the same attention, up to the order of its sums. */
+typedef struct {
+  int32_t n_groups;            /* in [1, n_seqs] */
+  int32_t prefix_len;          /* (host) about how many tokens the sequences of a group have in common; balances launches, nothing else */
+  const int32_t *group_starts; /* (device) [n_groups] first sequence of each group, ascending from 0; the last group ends with the batch.  May be
+                                  null for one group.  Starts that are not raise the device status and are taken as their running maximum */
+} dflash_groups;
+
+/* While set, dflash_draft_block and dflash_verify attend to the pages that a group has in common once for all rows of the group, instead of
+ * once per sequence.  The struct is copied, group_starts must stay valid; null switches it off.  A batch must have at least n_groups sequences.
+ * dflash_prefill does not look at it. */
+int dflash_set_groups(dflash_ctx *ctx, const dflash_groups *groups);
+
+/* That attention by itself: rows 0..rows-1 of every sequence of the batch, at positions seq_lens[s] .. seq_lens[s] + rows - 1, over the
+ * K/V rows of one layer of a pool, their own (already there) included: causal != 0: row j sees positions up to seq_lens[s] + j, else all
+ * seq_lens[s] + rows.  rows in [1, block_size] (1: plain decoding); batch->block_size is not looked at, batch->max_seq_len balances launches only.
+ * q (device) [S, rows, n_q_heads, head_dim] after norm and rotation, out (device) the same shape; both in the model's dtype, contiguous, 16-byte
+ * aligned.  Uses the workspace as the step's calls do. */
+int dflash_group_attention(dflash_ctx *ctx, const dflash_batch *batch, const dflash_groups *groups, int32_t pool, int32_t layer, int32_t rows,
+                           int32_t causal, const void *q, void *out, void *stream);
+
 /* ---- per-launch timing (benchmarks) -------------------------------------------------------------
  * While enabled, every GEMM and attention launch is bracketed by a pair of HIP events on the caller's
  * stream (this slows the step down: time whole steps with profiling off).  dflash_profile_read

@@ -27,6 +27,7 @@ EXPORTS = [
     "dflash_draft_block", "dflash_verify", "dflash_accept", "dflash_kv_commit",
     "dflash_prefill", "dflash_accept_sampled_noalloc", "dflash_kv_read", "dflash_kv_write", "dflash_profile_enable", "dflash_profile_read", "dflash_moe_stats", "dflash_moe_trace", "dflash_gemm_counts",
     "dflash_probe_hbm_read", "dflash_probe_mfma",
+    "dflash_pages_fork", "dflash_pages_reserve", "dflash_pages_release", "dflash_pages_compact", "dflash_set_groups", "dflash_group_attention",
 ]
 
 
@@ -50,6 +51,14 @@ class Runtime(C.Structure):
 class Batch(C.Structure):
     _fields_ = [("n_seqs", C.c_int32), ("max_seq_len", C.c_int32), ("seq_lens", C.c_void_p), ("block_table", C.c_void_p),
                 ("anchor", C.c_void_p), ("block_size", C.c_int32)]
+
+
+class Ledger(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("block_table", C.c_void_p), ("seq_lens", C.c_void_p), ("anchor", C.c_void_p), ("page_refs", C.c_void_p)]
+
+
+class Groups(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("prefix_len", C.c_int32), ("group_starts", C.c_void_p)]
 
 
 class DFlashError(RuntimeError):
@@ -99,6 +108,12 @@ def lib() -> C.CDLL:
         l.dflash_moe_stats.argtypes = [P, P, C.POINTER(C.c_int64)]
         l.dflash_moe_trace.argtypes = [P, P]
         l.dflash_gemm_counts.argtypes = [P, P]
+        l.dflash_pages_fork.argtypes = [P, C.POINTER(Ledger), I, C.POINTER(I), C.POINTER(I), P]
+        l.dflash_pages_reserve.argtypes = [P, C.POINTER(Ledger), I, P, P, P]
+        l.dflash_pages_release.argtypes = [P, C.POINTER(Ledger), I, C.POINTER(I), C.POINTER(I), P]
+        l.dflash_pages_compact.argtypes = [P, C.POINTER(Ledger), P, P]
+        l.dflash_set_groups.argtypes = [P, C.POINTER(Groups)]
+        l.dflash_group_attention.argtypes = [P, C.POINTER(Batch), C.POINTER(Groups), I, I, I, I, P, P, P]
         for name in EXPORTS:
             if name not in ("dflash_target_blob_bytes", "dflash_draft_blob_bytes", "dflash_kv_pool_bytes",
                             "dflash_workspace_bytes", "dflash_last_error"):
@@ -215,6 +230,19 @@ class Engine:
         assert block_table.shape == (seq_lens.shape[0], self.max_pages_per_seq)
         return Batch(int(seq_lens.shape[0]), int(max_seq_len), _ptr(seq_lens), _ptr(block_table), _ptr(anchor), int(block_size))
 
+    def ledger(self, block_table: torch.Tensor, seq_lens: torch.Tensor, anchor: torch.Tensor, page_refs: torch.Tensor) -> Ledger:
+        """Block table, lengths, anchors and page counts as the dflash_pages_* calls take them (int32, on the engine's device; the tensors
+        must outlive the struct)."""
+        n = int(block_table.shape[0])
+        for t, shape in ((block_table, (n, self.max_pages_per_seq)), (seq_lens, (n,)), (anchor, (n,)), (page_refs, (self.n_pages,))):
+            assert t.dtype == torch.int32 and tuple(t.shape) == shape and t.device == self.device, (t.dtype, tuple(t.shape), shape)
+        return Ledger(n, _ptr(block_table), _ptr(seq_lens), _ptr(anchor), _ptr(page_refs))
+
+    def groups(self, group_starts: Optional[torch.Tensor], prefix_len: int) -> Groups:
+        """Groups of consecutive sequences that begin with the same pages; group_starts None: the whole batch is one."""
+        assert group_starts is None or (group_starts.dtype == torch.int32 and group_starts.dim() == 1 and group_starts.device == self.device)
+        return Groups(1 if group_starts is None else int(group_starts.shape[0]), int(prefix_len), _ptr(group_starts))
+
     def profile_enable(self, on: bool):
         _check(self.l.dflash_profile_enable(self.ctx, int(on)), self.ctx)
 
@@ -304,6 +332,57 @@ def dflash_kv_read(e: Engine, batch: Batch, pool: int, layer: int, seq: int, sta
 def dflash_kv_write(e: Engine, batch: Batch, pool: int, layer: int, seq: int, start: int, k: torch.Tensor, v: torch.Tensor):
     assert k.dtype == torch.float32 and v.dtype == torch.float32 and k.shape == v.shape
     _check(e.l.dflash_kv_write(e.ctx, C.byref(batch), pool, layer, seq, start, int(k.shape[0]), _ptr(k), _ptr(v), _stream()), e.ctx)
+
+
+# ---- sequences that share pages (same names as the C ABI) -----------------------------------------------
+def _host_rows(rows):
+    rows = [int(r) for r in rows]
+    return len(rows), (C.c_int32 * max(1, len(rows)))(*rows)
+
+
+def dflash_pages_fork(e: Engine, ledger: Ledger, parents: Sequence[int], children: Sequence[int]):
+    """children[i] becomes a sequence with the pages, length and anchor of parents[i]."""
+    n, a = _host_rows(parents)
+    k, b = _host_rows(children)
+    assert n == k, (n, k)
+    _check(e.l.dflash_pages_fork(e.ctx, C.byref(ledger), n, a, b, _stream()), e.ctx)
+
+
+def dflash_pages_reserve(e: Engine, ledger: Ledger, tokens: torch.Tensor, granted: Optional[torch.Tensor] = None):
+    """Pages of their own for the next tokens[s] tokens of rows 0 .. len(tokens) - 1; granted[s] = 1 where the row holds them."""
+    n = int(tokens.shape[0])
+    assert tokens.dtype == torch.int32 and tokens.dim() == 1
+    assert granted is None or (granted.dtype == torch.int32 and tuple(granted.shape) == (n,))
+    _check(e.l.dflash_pages_reserve(e.ctx, C.byref(ledger), n, _ptr(tokens), _ptr(granted), _stream()), e.ctx)
+
+
+def dflash_pages_release(e: Engine, ledger: Ledger, rows: Sequence[int], keep: Optional[Sequence[int]] = None):
+    """Gives back the pages behind the first keep[i] tokens of rows[i] (None: all)."""
+    n, a = _host_rows(rows)
+    k, b = _host_rows(keep) if keep is not None else (n, None)
+    assert n == k, (n, k)
+    _check(e.l.dflash_pages_release(e.ctx, C.byref(ledger), n, a, b, _stream()), e.ctx)
+
+
+def dflash_pages_compact(e: Engine, ledger: Ledger, n_live: Optional[torch.Tensor] = None):
+    assert n_live is None or (n_live.dtype == torch.int32 and n_live.numel() == 1)
+    _check(e.l.dflash_pages_compact(e.ctx, C.byref(ledger), _ptr(n_live), _stream()), e.ctx)
+
+
+def dflash_set_groups(e: Engine, groups: Optional[Groups]):
+    """From now on the step's attention reads what the sequences of a group share once (None: per sequence again).  The tensor behind
+    groups.group_starts must outlive its use."""
+    _check(e.l.dflash_set_groups(e.ctx, C.byref(groups) if groups is not None else None), e.ctx)
+
+
+def dflash_group_attention(e: Engine, batch: Batch, groups: Groups, pool: int, layer: int, q: torch.Tensor, out: torch.Tensor, causal: bool = True):
+    """Attention of q [S, rows, n_q_heads, head_dim] at positions seq_lens[s] .. + rows - 1 over one layer of a pool, into out (same shape)."""
+    m = e.target if pool == DFLASH_POOL_TARGET else e.draft
+    dt = torch.bfloat16 if e.dtype == "bf16" else torch.float32
+    assert q.dim() == 4 and tuple(q.shape) == (batch.n_seqs, q.shape[1], m.n_q_heads, m.head_dim), tuple(q.shape)
+    assert out.shape == q.shape and q.dtype == dt and out.dtype == dt
+    _check(e.l.dflash_group_attention(e.ctx, C.byref(batch), C.byref(groups), pool, layer, int(q.shape[1]), int(causal), _ptr(q), _ptr(out), _stream()),
+           e.ctx)
 
 
 # ---- machine probes (same names as the C ABI) -----------------------------------------------------------

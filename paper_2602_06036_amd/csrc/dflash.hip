@@ -16,11 +16,13 @@
 #include <vector>
 
 #include "attn.h"
+#include "attn_group.h"
 #include "attn_mfma.h"
 #include "common.h"
 #include "gemm.h"
 #include "gemm_resid.h"
 #include "gemm_tiled.h"
+#include "ledger.h"
 #include "misc.h"
 #include "moe.h"
 #include "plan.h"
@@ -159,6 +161,20 @@ inline int attn_q_shift(const dflash_dims& m, int block_size) {
   return (m.dtype == DFLASH_BF16 && (m.head_dim == 128 || m.head_dim == 64) && group % (1 << sh) == 0) ? sh : -1;
 }
 
+// launch shape of the attention of S sequences that share pages
+struct GroupShape {
+  int rows, tiles, own_tiles;
+  GroupSplits splits;
+};
+inline GroupShape group_shape(const dflash_dims& m, int S, int block_size, int n_groups, int prefix_tokens, int own_tokens) {
+  GroupShape g;
+  g.rows = block_size * (m.n_q_heads / m.n_kv_heads);
+  g.tiles = group_tile_slots(S, g.rows, n_groups);
+  g.own_tiles = (g.rows + kGroupTile - 1) / kGroupTile;
+  g.splits = group_plan(g.tiles, S, g.own_tiles, m.n_kv_heads, prefix_tokens, own_tokens);
+  return g;
+}
+
 // ---- workspace ------------------------------------------------------------------------------------
 constexpr int ARGMAX_CHUNKS = 32;   // workgroups that share one vocabulary row in the argmax
 
@@ -188,6 +204,7 @@ inline size_t arrive_counters(size_t D) { return std::max<size_t>(1, D / 64); }
 
 struct Workspace {
   size_t status, arena, h, a, q, o, act, taps, fuse, ht, logits_d, logits_t, part_o, part_ml, stats_p, stats_q, amax, lsep, rope_t, rope_d, ssq, arrive, pf_lens, pf_plens, pf_table, pf_tokens, pf_end_row, pf_end_seq, pf_first, pf_anchor, pf_tiles, total;
+  size_t grp_tiles, grp_first, pg_copies, pg_wants, pg_ids, pg_head;   // sequences that share pages: the groups' tables, the ledger's scratch
   size_t moe_sel_e, moe_sel_w, moe_sel_pos, moe_row_of, moe_items, moe_a, moe_act, moe_y;   // routed-expert target only
 };
 Workspace workspace_layout(const dflash_dims& t, const dflash_dims& d, const dflash_runtime& rt, const Knobs& kn) {
@@ -227,6 +244,10 @@ Workspace workspace_layout(const dflash_dims& t, const dflash_dims& d, const dfl
         const SplitPlan p = plan_splits(S, m->n_kv_heads << sh, max_tokens, kn.attn_target_wgs);
         part_rows = std::max(part_rows, (size_t)S * blk * m->n_q_heads * p.bound);
       }
+      for (int blk = 1; blk <= rt.block_size; ++blk) {   // sequences that share pages (one group: the fewest tiles, so the most key ranges)
+        const GroupSplits p = group_shape(*m, S, blk, 1, max_tokens, max_tokens).splits;
+        part_rows = std::max(part_rows, (size_t)S * blk * m->n_q_heads * (p.prefix + p.own));
+      }
     }
   }
   const size_t hd = std::max(t.head_dim, d.head_dim);
@@ -251,6 +272,13 @@ Workspace workspace_layout(const dflash_dims& t, const dflash_dims& d, const dfl
   w.pf_first = take((size_t)rt.max_seqs * 4);
   w.pf_anchor = take((size_t)rt.max_seqs * 4);
   w.pf_tiles = take((size_t)rt.max_seqs * 16);
+  w.grp_tiles = take(((size_t)group_tile_slots(rt.max_seqs, rt.block_size * std::max(t.n_q_heads / t.n_kv_heads, d.n_q_heads / d.n_kv_heads), rt.max_seqs) + 1) * 16);
+  w.grp_first = take((size_t)rt.max_seqs * 4);
+  const size_t half = (size_t)rt.n_pages / 2 + 1;   // pages that a compaction moves, at most
+  w.pg_copies = take(std::max<size_t>(kReserveRows * 16, half * 8));
+  w.pg_wants = take(((size_t)std::min(rt.max_seqs, kReserveRows) * rt.max_pages_per_seq / 64 + 16) * 8);
+  w.pg_ids = take(((size_t)rt.n_pages + 2 * half) * 4);
+  w.pg_head = take(256);
   w.moe_sel_e = w.moe_sel_w = w.moe_sel_pos = w.moe_row_of = w.moe_items = w.moe_a = w.moe_act = w.moe_y = 0;
   if (t.n_experts) {
     const size_t mk = (size_t)M * t.top_k, np = moe_positions(t, M);
@@ -306,6 +334,7 @@ struct dflash_ctx {
   int32_t* moe_trace = nullptr;                        // dflash_moe_trace: where the routed layers also leave their expert choices
   bool have_logits_d = false, have_logits_t = false;   // the workspace holds this step's draft / target logits
   float draft_temperature = 0.f;                       // of the last dflash_draft_block call
+  dflash_groups groups{};                              // dflash_set_groups; n_groups = 0: none
   float stats_q_T = 0.f, stats_p_T = 0.f;              // > 0: ws.stats_q / ws.stats_p hold this step's (max, log-sum-exp) rows at that temperature
   // k.fuse, few-row path (one band of rows, dense bf16 model): 1 = the O projection runs unsplit with the residual update in
   // its epilogue (gemm_resid.h), the down projection split with the update done by the last workgroup of a column block
@@ -386,6 +415,7 @@ struct Engine {
   int lse_parts = 0;     // > 0: ... and that many per-row softmax-statistics partials in ws.lsep
   bool lm_skip_store = false;   // the LM-head GEMM may drop its logits when its argmax is fused (nobody will read them)
   PrefillTiles tiles;    // the layer() call in progress is a prefill's, whose attention goes by these
+  const dflash_groups* groups = nullptr;   // the layer() call in progress attends to what its groups share once (group_plan() has run)
   int pending_tap = -1;  // tap index to be taken from the completed residual stream by the next RMSNorm
 
   // Few-row path: ws.a holds x * gain with the division by the row's rms deferred to the GEMM that reads it; the
@@ -520,6 +550,53 @@ struct Engine {
 
   void attention(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, bool causal);
 
+  // ---- sequences that share pages (attn_group.h): the groups' tables, once a pass, and a layer's attention
+  GroupTables group_tables() { return GroupTables{ws<int4>(c->ws.grp_tiles), ws<int32_t>(c->ws.grp_first)}; }
+  void group_tables_of(const dflash_dims& m, const dflash_batch* b, const dflash_groups& g, int block) {
+    SeqGeom geo = geom(b);
+    geo.block_size = block;
+    hipLaunchKernelGGL(group_plan_kernel, dim3(g.n_groups), dim3(1024), 0, st, geo, g.group_starts, g.n_groups, b->n_seqs,
+                       block * (m.n_q_heads / m.n_kv_heads), group_tables());
+    check();
+  }
+  // of the q rows; `out` rows as GEMM operand or plain
+  void group_attention(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, const dflash_groups& g, int block, bool causal, const T* q,
+                       T* out, bool operand) {
+    const int S = b->n_seqs;
+    const int most = c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE, expected = std::min(g.prefix_len, most);
+    const GroupShape sh = group_shape(m, S, block, g.n_groups, expected, std::min(std::max(0, b->max_seq_len - expected) + block, most));
+    GroupArgs ga{m.n_q_heads, m.n_kv_heads, layer, causal, S, sh.rows, sh.tiles, sh.own_tiles, sh.splits.prefix, sh.splits.own, 1.0f / sqrtf((float)m.head_dim)};
+    SeqGeom geo = geom(b);
+    geo.block_size = block;
+    const int n_rows = S * block * m.n_q_heads;
+    {
+      // algorithmic bytes: what is shared once, as the caller expects it, the rest per sequence
+      const double tokens = (double)g.n_groups * expected + (double)S * (std::max(0, b->max_seq_len - expected) + block);
+      ProfScope prof(c, st, DFLASH_PROF_ATTN, tokens * 2 * m.n_kv_heads * m.head_dim * sizeof(T));
+      group_attn_launch<T>(st, q, pool, geo, ga, m.head_dim, group_tables(), ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml));
+      check();
+    }
+    ProfScope prof(c, st, DFLASH_PROF_ATTN_MERGE, 0.0);
+    const dim3 grid((n_rows + 3) / 4), threads(256);
+    if (operand)
+      hipLaunchKernelGGL((group_merge_kernel<T, true>), grid, threads, 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), out, ga, group_tables().first,
+                         m.head_dim, block, n_rows);
+    else
+      hipLaunchKernelGGL((group_merge_kernel<T, false>), grid, threads, 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), out, ga, group_tables().first,
+                         m.head_dim, block, n_rows);
+    check();
+  }
+  int attend(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, const dflash_groups& g, int rows, bool causal, const void* q, void* out) {
+    group_tables_of(m, b, g, rows);
+    group_attention(m, pool, layer, b, g, rows, causal, static_cast<const T*>(q), static_cast<T*>(out), false);
+    return hip_err ? DFLASH_EHIP : DFLASH_OK;
+  }
+  void use_groups(const dflash_dims& m, const dflash_batch* b) {
+    if (!c->groups.n_groups) return;
+    groups = &c->groups;
+    group_tables_of(m, b, c->groups, blk(b));
+  }
+
   // one Transformer layer on the M block rows held in ws.h.  gain_next (nullable): gain of the RMSNorm behind the layer, which may
   // then be deferred; tap: index under which the layer's output is tapped, or -1
   void layer(const dflash_dims& m, const char* lbase, const LayerOff& lo, T* pool, int l, const dflash_batch* b, bool causal,
@@ -632,6 +709,7 @@ struct Engine {
                        RopeTab{ws<float2>(c->ws.rope_d), log((double)d.rope_theta), d.head_dim}, RopeTab{nullptr, 0.0, 0}, ef,
                        EmbedBlock{b->anchor, draft_tokens, c->rt.mask_token_id}, arrivals(d, M));
     check();
+    use_groups(d, b);
     for (int i = 0; i < d.n_layers; ++i) {
       const char* lb = l0 + c->dl.lo.end * i;
       const float* gn = i + 1 < d.n_layers ? reinterpret_cast<const float*>(lb + c->dl.lo.end + c->dl.lo.g1) : nullptr;
@@ -670,6 +748,7 @@ struct Engine {
                        RopeTab{ws<float2>(c->ws.rope_t), log((double)t.rope_theta), t.head_dim},
                        RopeTab{ws<float2>(c->ws.rope_d), log((double)c->d.rope_theta), c->d.head_dim}, ef, EmbedBlock{}, arrivals(t, M));
     check();
+    use_groups(t, b);
     int tap = 0;
     for (int l = 0; l < t.n_layers; ++l) {
       const char* lb = l0 + c->tl.lo.end * l;
@@ -1162,6 +1241,7 @@ void Engine<float>::resid(const float*, const float*, int, int, int, const float
 template <typename T>
 void Engine<T>::attention(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, bool causal) {
   const int S = b->n_seqs, B = blk(b), M = S * B;
+  if (groups) return group_attention(m, pool, layer, b, *groups, B, causal, ws<T>(c->ws.q), ws<T>(c->ws.o), true);
   const int max_tokens = std::min(b->max_seq_len + B, c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE);
   const int q_shift = attn_q_shift(m, B);
   const SplitPlan p = plan_splits(S, m.n_kv_heads << q_shift, max_tokens, c->k.attn_target_wgs);
@@ -1292,6 +1372,62 @@ int check_batch(dflash_ctx* ctx, const dflash_batch* b) {
     return CTX_FAIL(ctx, DFLASH_ECAPACITY, "batch: max_seq_len %d + block %d exceeds the %d tokens a block-table row covers", b->max_seq_len,
                     blk, ctx->rt.max_pages_per_seq * DFLASH_PAGE_SIZE);
   return DFLASH_OK;
+}
+
+// n_groups = 0 (none set) fits every batch
+int check_groups(dflash_ctx* ctx, const dflash_batch* b, const dflash_groups* g) {
+  if (g->n_groups > b->n_seqs) return CTX_FAIL(ctx, DFLASH_EINVAL, "groups: %d groups of %d sequences", g->n_groups, b->n_seqs);
+  return DFLASH_OK;
+}
+int check_group_struct(dflash_ctx* ctx, const dflash_groups* g) {
+  if (g->n_groups < 1 || g->prefix_len < 0) return CTX_FAIL(ctx, DFLASH_EINVAL, "groups: n_groups %d and prefix_len %d must be positive and not negative", g->n_groups, g->prefix_len);
+  if (g->n_groups > 1 && !g->group_starts) return CTX_FAIL(ctx, DFLASH_EINVAL, "groups: null group_starts of %d groups", g->n_groups);
+  return DFLASH_OK;
+}
+
+// ---- page ledger -----------------------------------------------------------------------------------------
+int check_ledger(dflash_ctx* ctx, const dflash_ledger* l) {
+  if (!ctx) return fail(nullptr, DFLASH_EINVAL, "ctx: null");
+  if (!l || !l->block_table || !l->seq_lens || !l->anchor || !l->page_refs) return CTX_FAIL(ctx, DFLASH_EINVAL, "ledger: null pointer");
+  if (l->n_rows < 1) return CTX_FAIL(ctx, DFLASH_EINVAL, "ledger: n_rows %d", l->n_rows);
+  return DFLASH_OK;
+}
+Ledger device_ledger(dflash_ctx* ctx, const dflash_ledger* l) {
+  return Ledger{l->block_table, l->seq_lens, l->anchor, l->page_refs, l->n_rows, ctx->rt.max_pages_per_seq, ctx->rt.n_pages,
+                reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.status)};
+}
+PageBlocks page_blocks(const dflash_ctx* ctx) {
+  PageBlocks b;
+  const int es = (int)esize(ctx->t.dtype);
+  b.target = reinterpret_cast<u32x4*>(ctx->rt.target_kv_pool);
+  b.draft = reinterpret_cast<u32x4*>(ctx->rt.draft_kv_pool);
+  b.target_layers = ctx->t.n_layers;
+  b.layers = ctx->t.n_layers + ctx->d.n_layers;
+  b.target_part = ctx->t.head_dim * es;
+  b.draft_part = ctx->d.head_dim * es;
+  b.target_units = b.target_part * 2 * ctx->t.n_kv_heads;
+  b.draft_units = b.draft_part * 2 * ctx->d.n_kv_heads;
+  b.n_pages = ctx->rt.n_pages;
+  b.key_units = es / 2;
+  return b;
+}
+int launched(dflash_ctx* ctx, const char* what) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? DFLASH_OK : CTX_FAIL(ctx, DFLASH_EHIP, "%s: HIP launch failed: %s", what, hipGetErrorString(e));
+}
+// rows in range, none of them twice; a row's place in `given`
+int check_rows(dflash_ctx* ctx, const dflash_ledger* l, int n, const int32_t* rows, const char* what) {
+  for (int i = 0; i < n; ++i)
+    if (rows[i] < 0 || rows[i] >= l->n_rows) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: row %d outside [0,%d)", what, rows[i], l->n_rows);
+  return DFLASH_OK;
+}
+bool has_twice(int n, const int32_t* a, int m, const int32_t* b) {   // a value twice in a, or in a and b
+  std::vector<int32_t> x(a, a + n);
+  std::sort(x.begin(), x.end());
+  if (std::adjacent_find(x.begin(), x.end()) != x.end()) return true;
+  for (int i = 0; i < m; ++i)
+    if (std::binary_search(x.begin(), x.end(), b[i])) return true;
+  return false;
 }
 
 }  // namespace
@@ -1523,6 +1659,7 @@ int dflash_draft_block(dflash_ctx* ctx, const dflash_batch* batch, float tempera
   if (!draft_tokens) return CTX_FAIL(ctx, DFLASH_EINVAL, "draft_block: draft_tokens is null");
   if (!(temperature >= 0.f)) return CTX_FAIL(ctx, DFLASH_EINVAL, "draft_block: negative temperature");
   if (temperature > 0.f && !rng_key) return CTX_FAIL(ctx, DFLASH_EINVAL, "draft_block: sampling needs rng_key");
+  if ((rc = check_groups(ctx, batch, &ctx->groups))) return rc;
   return DISPATCH(ctx, draft_block(batch, temperature, rng_key, draft_tokens, logits_out));
 }
 
@@ -1531,6 +1668,7 @@ int dflash_verify(dflash_ctx* ctx, const dflash_batch* batch, const int32_t* tok
   if ((rc = check_batch(ctx, batch))) return rc;
   if (batch->n_seqs == 0) return DFLASH_OK;
   if (!tokens) return CTX_FAIL(ctx, DFLASH_EINVAL, "verify: null tokens");
+  if ((rc = check_groups(ctx, batch, &ctx->groups))) return rc;
   return DISPATCH(ctx, verify(batch, tokens, tgt_argmax, logits_out));
 }
 
@@ -1622,6 +1760,111 @@ int dflash_accept_sampled_noalloc(const float* target_logits, const float* draft
                         rng_key, n_seqs, block_size, vocab, inv_T, accept_len, out_tokens, best, DFLASH_NOALLOC_BESTS, arrive);
   if (hipGetLastError() != hipSuccess) return fail(nullptr, DFLASH_EHIP, "accept_sampled_noalloc: launch failed");
   return DFLASH_OK;
+}
+
+int dflash_pages_fork(dflash_ctx* ctx, const dflash_ledger* ledger, int32_t n, const int32_t* parents, const int32_t* children, void* stream) {
+  int rc;
+  if ((rc = check_ledger(ctx, ledger))) return rc;
+  if (n < 0 || (n > 0 && (!parents || !children))) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_fork: bad count or null rows");
+  if ((rc = check_rows(ctx, ledger, n, parents, "pages_fork")) || (rc = check_rows(ctx, ledger, n, children, "pages_fork"))) return rc;
+  try {
+    if (has_twice(n, children, n, parents)) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_fork: a row is a child twice, or child and parent");
+  } catch (const std::bad_alloc&) {
+    return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_fork: out of host memory");
+  }
+  const Ledger l = device_ledger(ctx, ledger);
+  for (int i = 0; i < n; i += kRowsPerLaunch) {
+    const int k = std::min(n - i, kRowsPerLaunch);
+    RowPairs rows;
+    std::copy(parents + i, parents + i + k, rows.a);
+    std::copy(children + i, children + i + k, rows.b);
+    hipLaunchKernelGGL(pages_fork_kernel, dim3((l.mpps + 255) / 256, k), dim3(256), 0, (hipStream_t)stream, l, rows);
+  }
+  return launched(ctx, "pages_fork");
+}
+
+int dflash_pages_release(dflash_ctx* ctx, const dflash_ledger* ledger, int32_t n, const int32_t* rows, const int32_t* keep, void* stream) {
+  int rc;
+  if ((rc = check_ledger(ctx, ledger))) return rc;
+  if (n < 0 || (n > 0 && !rows)) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_release: bad count or null rows");
+  if ((rc = check_rows(ctx, ledger, n, rows, "pages_release"))) return rc;
+  for (int i = 0; keep && i < n; ++i)
+    if (keep[i] < 0) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_release: negative length %d", keep[i]);
+  try {
+    if (has_twice(n, rows, 0, nullptr)) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_release: a row is given twice");
+  } catch (const std::bad_alloc&) {
+    return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_release: out of host memory");
+  }
+  const Ledger l = device_ledger(ctx, ledger);
+  for (int i = 0; i < n; i += kRowsPerLaunch) {
+    const int k = std::min(n - i, kRowsPerLaunch);
+    RowPairs pairs;
+    std::copy(rows + i, rows + i + k, pairs.a);
+    if (keep) std::copy(keep + i, keep + i + k, pairs.b);
+    else std::fill(pairs.b, pairs.b + k, 0);
+    hipLaunchKernelGGL(pages_release_kernel, dim3((l.mpps + 255) / 256, k), dim3(256), 0, (hipStream_t)stream, l, pairs);
+  }
+  return launched(ctx, "pages_release");
+}
+
+int dflash_pages_reserve(dflash_ctx* ctx, const dflash_ledger* ledger, int32_t n, const int32_t* tokens, int32_t* granted, void* stream) {
+  int rc;
+  if ((rc = check_ledger(ctx, ledger))) return rc;
+  if (n < 0 || n > ledger->n_rows || n > ctx->rt.max_seqs)
+    return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_reserve: n %d outside [0,%d]", n, std::min(ledger->n_rows, ctx->rt.max_seqs));
+  if (n == 0) return DFLASH_OK;
+  if (!tokens) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_reserve: null tokens");
+  const Ledger l = device_ledger(ctx, ledger);
+  const PageBlocks blocks = page_blocks(ctx);
+  const ReserveScratch sc{reinterpret_cast<int4*>(ctx->wsp + ctx->ws.pg_copies), reinterpret_cast<unsigned long long*>(ctx->wsp + ctx->ws.pg_wants),
+                          reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.pg_ids), reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.pg_head)};
+  for (int i = 0; i < n; i += kReserveRows) {
+    const int k = std::min(n - i, kReserveRows);
+    hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(1024), 0, (hipStream_t)stream, l, i, k, tokens, granted, sc);
+    hipLaunchKernelGGL(pages_copy_kernel, dim3(blocks.layers, k), dim3(256), 0, (hipStream_t)stream, blocks, sc.copies);
+  }
+  return launched(ctx, "pages_reserve");
+}
+
+int dflash_pages_compact(dflash_ctx* ctx, const dflash_ledger* ledger, int32_t* n_live, void* stream) {
+  int rc;
+  if ((rc = check_ledger(ctx, ledger))) return rc;
+  const Ledger l = device_ledger(ctx, ledger);
+  const PageBlocks blocks = page_blocks(ctx);
+  const int half = l.n_pages / 2 + 1;
+  int32_t* ids = reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.pg_ids);
+  const CompactScratch sc{reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.pg_head), reinterpret_cast<int2*>(ctx->wsp + ctx->ws.pg_copies), ids, ids + l.n_pages,
+                          ids + l.n_pages + half};
+  hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(1024), 0, (hipStream_t)stream, l, sc, n_live);
+  const long long most = (long long)half * blocks.layers;
+  hipLaunchKernelGGL(pages_move_kernel, dim3((unsigned)std::min<long long>(most, 2048)), dim3(256), 0, (hipStream_t)stream, l, blocks, sc);
+  return launched(ctx, "pages_compact");
+}
+
+int dflash_set_groups(dflash_ctx* ctx, const dflash_groups* groups) {
+  int rc;
+  if (!ctx) return fail(nullptr, DFLASH_EINVAL, "ctx: null");
+  if (groups && (rc = check_group_struct(ctx, groups))) return rc;
+  ctx->groups = groups ? *groups : dflash_groups{};
+  return DFLASH_OK;
+}
+
+int dflash_group_attention(dflash_ctx* ctx, const dflash_batch* batch, const dflash_groups* groups, int32_t pool, int32_t layer, int32_t rows,
+                           int32_t causal, const void* q, void* out, void* stream) {
+  int rc;
+  if ((rc = check_batch(ctx, batch))) return rc;
+  if (batch->n_seqs == 0) return DFLASH_OK;
+  if (!groups) return CTX_FAIL(ctx, DFLASH_EINVAL, "group_attention: null groups");
+  if ((rc = check_group_struct(ctx, groups)) || (rc = check_groups(ctx, batch, groups))) return rc;
+  if (pool != DFLASH_POOL_TARGET && pool != DFLASH_POOL_DRAFT) return CTX_FAIL(ctx, DFLASH_EINVAL, "group_attention: bad pool");
+  const dflash_dims& m = pool == DFLASH_POOL_TARGET ? ctx->t : ctx->d;
+  if (layer < 0 || layer >= m.n_layers) return CTX_FAIL(ctx, DFLASH_EINVAL, "group_attention: layer %d outside [0,%d)", layer, m.n_layers);
+  if (rows < 1 || rows > ctx->rt.block_size) return CTX_FAIL(ctx, DFLASH_EINVAL, "group_attention: rows %d outside [1,%d]", rows, ctx->rt.block_size);
+  if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 15)) return CTX_FAIL(ctx, DFLASH_EINVAL, "group_attention: q and out must be 16-byte aligned device buffers");
+  const void* kv = pool == DFLASH_POOL_TARGET ? ctx->rt.target_kv_pool : ctx->rt.draft_kv_pool;
+  if (ctx->t.dtype == DFLASH_BF16)
+    return Engine<bf16_t>{ctx, (hipStream_t)stream}.attend(m, static_cast<const bf16_t*>(kv), layer, batch, *groups, rows, causal != 0, q, out);
+  return Engine<float>{ctx, (hipStream_t)stream}.attend(m, static_cast<const float*>(kv), layer, batch, *groups, rows, causal != 0, q, out);
 }
 
 static int kv_copy_checked(dflash_ctx* ctx, const dflash_batch* batch, int32_t pool, int32_t layer, int32_t seq, int32_t start, int32_t count,

@@ -111,6 +111,16 @@ inline bool attention_by_tiles(int tiles, int blocks, int head_groups, int cache
   return cached <= 768 || blocks * head_groups * 10 >= rounds * 512 * 9;   // nine tenths of the rounds' places for blocks taken
 }
 
+// ---- attention of sequences that share pages: key ranges of the prefix part and of the own parts ----------------------
+struct GroupSplits {
+  int prefix, own;
+};
+inline int group_splits(int wgs, int tokens) { return std::max(1, std::min({256 / std::max(1, wgs), (tokens + 127) / 128, 32})); }
+// tiles, own_tiles: workgroups of a kv head in all and of a sequence; prefix and own tokens as the caller expects them
+inline GroupSplits group_plan(int tiles, int n_seqs, int own_tiles, int n_kv_heads, int prefix_tokens, int own_tokens) {
+  return {group_splits(tiles * n_kv_heads, prefix_tokens), group_splits(n_seqs * own_tiles * n_kv_heads, own_tokens)};
+}
+
 // ---- GEMMs ----------------------------------------------------------------------------------------------
 // rows of partial results the split-K arena holds for a context of at most max_rows activation rows
 inline int arena_rows(int max_rows) { return std::max(1024, 4 * max_rows); }
