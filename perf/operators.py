@@ -267,7 +267,7 @@ def prepare(case, seed):
         if own:
             # the causal cases read the target's pool, the others the draft's
             st.e = _engine(c, st.block, c["seqs"], st.width, st.n_pages, 2, 2, st.pool if c["causal"] else None, None if c["causal"] else st.pool)
-            st.starts_dev = torch.tensor(st.starts, dtype=torch.int32, device=DEV)
+            st.starts_dev = torch.tensor(st.starts[:-1], dtype=torch.int32, device=DEV)
             st.anchor = torch.zeros(c["seqs"], dtype=torch.int32, device=DEV)
             st.out = torch.empty_like(st.q)
             st.batch = st.e.batch(st.seq_lens, st.table, st.anchor, max(st.lens))
