@@ -319,6 +319,297 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
     *reinterpret_cast<float4*>(part_o + pr * HD + dt * 16 + 4 * g) = make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]);
 }
 
+// ---- bf16, head dim 64 or 128: wavefronts split the keys ------------------------------------------------------------------
+// Eight wavefronts take every eighth pair of pages each for all RB blocks of 16 query rows, from a ring of their own in LDS: the pages go there
+// directly (global_load_lds), K refilled as soon as a pair's scores are done and V as soon as its products are, so nothing in flight costs a
+// register and no wavefront waits for another before the end, where their partial results are added in LDS.  The loads are counted by hand (NI per half page,
+// in order): the compiler would wait for all of them ahead of every LDS read.
+template <int HD>
+struct KeySplit {
+  static constexpr int KT = HD / 32, DT = HD / 16, NW = 8, LD = HD + 4;
+  static constexpr int PART = DF_PAGE * HD * 2, NI = PART / 1024;   // bytes of the K or V part of a page, load instructions for it
+  static constexpr int RING = NW * 4 * PART;                        // per wavefront: K of page A, of page B, V of page A, of page B
+  static constexpr int bytes(int rb) { return (RING + rb * KT * 1024 > 4 * rb * 16 * LD * 4 ? RING + rb * KT * 1024 : 4 * rb * 16 * LD * 4); }
+};
+
+template <int HD, int RB>
+__device__ __forceinline__ void group_sweep_keys(char* s_raw, float2 (*s_ml)[64], const GroupWork& w, int kvh, const bf16_t* __restrict__ q,
+                                                 const bf16_t* __restrict__ pool, const SeqGeom& geo, const GroupArgs& ga, float* __restrict__ part_o,
+                                                 float2* __restrict__ part_ml) {
+  typedef KeySplit<HD> C;
+  constexpr int KT = C::KT, DT = C::DT, NW = C::NW, LD = C::LD, PART = C::PART, NI = C::NI;
+  float (*s_o)[RB * 16][LD] = reinterpret_cast<float (*)[RB * 16][LD]>(s_raw);   // overlays ring and queries in the end
+  u32x4* q_lds = reinterpret_cast<u32x4*>(s_raw + C::RING);                      // [rb][kt][lane]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int group = ga.n_q_heads / ga.n_kv_heads, page0 = w.c0 / DF_PAGE;
+  // page ids of this wavefront's pairs, 32 pairs at a time: lane l holds page l % 2 of its pair k0 + l / 2; the next set is requested as a set comes into use
+  auto load_ids = [&](int k0) { return w.table[min(page0 + 2 * (wave + NW * (k0 + (lane >> 1))) + (lane & 1), geo.max_pages_per_seq - 1)]; };
+  int ids = load_ids(0);
+  const int n_pairs = w.c1 > w.c0 ? (w.c1 - w.c0 + 31) >> 5 : 0, my_pairs = n_pairs > wave ? (n_pairs - wave + NW - 1) / NW : 0;
+  int ids_next = my_pairs > 32 ? load_ids(32) : 0;
+  u32x4 qr[KT];
+  {
+    const int r = (wave < RB ? wave : 0) * 16 + n, row = w.row0 + min(r, w.n_rows - 1);
+    const int s = row / ga.rows, slot = row % ga.rows / group;
+    const u32x4* qp = reinterpret_cast<const u32x4*>(q + ((size_t)(s * geo.block_size + slot) * ga.n_q_heads + kvh * group + row % group) * HD);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) qr[kt] = qp[kt * 4 + g];   // a row that is not there reads along and is not stored
+  }
+  int last[RB];   // last key that a lane's row sees (of a sequence's own part under the causal mask)
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+    last[rb] = w.own_len >= 0 ? w.own_len + (w.row0 + min(rb * 16 + n, w.n_rows - 1)) % ga.rows / group : 0x7FFFFFFF;
+  const int n_all = w.own_len >= 0 ? min(w.c1, w.own_len) : w.c1;   // keys below this are visible to every row
+
+  const unsigned ring = (unsigned)(size_t)s_raw + (unsigned)wave * (4 * PART), voff = lane * 16;
+  auto fetch = [&](const bf16_t* src, unsigned at) {   // one part of a page into the ring at byte `at`
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const unsigned dst = __builtin_amdgcn_readfirstlane(ring + at + i * 1024);
+      const bf16_t* from = src + i * 512;
+      unsigned keep_m0;   // whatever the compiler keeps in m0 is put back
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_nop 0\n\ts_mov_b32 m0, %0"
+                   : "=&s"(keep_m0) : "s"(dst), "v"(voff), "s"(from) : "memory");
+    }
+  };
+  struct Pair {
+    const bf16_t *a, *b;   // the pages' K parts (V follows)
+    bool ok_a, ok_b;
+  };
+  auto pair_of = [&](int k) {   // this wavefront's k-th pair; foreign or missing pages alias a readable one and weigh nothing
+    Pair p;
+    const int pa = __builtin_amdgcn_readlane(ids, (k & 31) * 2), pb = __builtin_amdgcn_readlane(ids, (k & 31) * 2 + 1);
+    p.ok_a = pa >= 0 && pa < geo.n_pages;
+    p.ok_b = w.c0 + (wave + NW * k) * 32 + 16 < w.c1 && pb >= 0 && pb < geo.n_pages;
+    const int a = p.ok_a ? pa : 0, b = p.ok_b ? pb : a;
+    p.a = pool + kv_head_base(ga.layer, geo.n_pages, a, ga.n_kv_heads, kvh, HD);
+    p.b = pool + kv_head_base(ga.layer, geo.n_pages, b, ga.n_kv_heads, kvh, HD);
+    return p;
+  };
+  Pair cur{pool, pool, false, false};
+  if (my_pairs > 0) {
+    cur = pair_of(0);
+    fetch(cur.a, 0);
+    fetch(cur.b, PART);
+    fetch(cur.a + DF_PAGE * HD, 2 * PART);
+    fetch(cur.b + DF_PAGE * HD, 3 * PART);
+  }
+  if (wave < RB) {
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) q_lds[(wave * KT + kt) * 64 + lane] = qr[kt];
+  }
+  __syncthreads();
+
+  float m_run[RB], l_run[RB];
+  f32x4 acc[RB][DT];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    m_run[rb] = -INFINITY;
+    l_run[rb] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[rb][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+  const float scale2 = ga.scale * 1.44269504088896341f;
+  const char* my_ring = s_raw + wave * (4 * PART);
+
+  for (int k = 0; k < my_pairs; ++k) {
+    const int base = w.c0 + (wave + NW * k) * 32;
+    const bool more = k + 1 < my_pairs;
+    if (more && ((k + 1) & 31) == 0) {
+      ids = ids_next;
+      if (k + 33 < my_pairs) ids_next = load_ids(k + 33);
+    }
+    Pair nxt = cur;
+    if (more) nxt = pair_of(k + 1);
+
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");   // this pair's K is there (its V still on the way)
+    f32x4 sc[RB][2];
+    {
+      const u32x4* kp = reinterpret_cast<const u32x4*>(my_ring) + lane;
+      u32x4 ka[KT], kb[KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        ka[kt] = kp[kt * 64];
+        kb[kt] = kp[PART / 16 + kt * 64];
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        asm volatile("" ::: "memory");   // the query fragments of one row block at a time: together they would cost 64 registers
+        sc[rb][0] = sc[rb][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+          const u32x4 qf = q_lds[(rb * KT + kt) * 64 + lane];
+          sc[rb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[kt]), __builtin_bit_cast(bf16x8, qf), sc[rb][0], 0, 0, 0);
+          sc[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kb[kt]), __builtin_bit_cast(bf16x8, qf), sc[rb][1], 0, 0, 0);
+        }
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the K half has been read
+    if (more) {
+      fetch(nxt.a, 0);
+      fetch(nxt.b, PART);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    const bool tail = !cur.ok_a || !cur.ok_b || base + 32 > n_all;   // (n_all <= c1: keys behind the range as well)
+    if (tail) {
+      const int p0 = base + 4 * g;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int upto = min(w.c1 - 1, last[rb]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (!(cur.ok_a && p0 + i <= upto)) sc[rb][0][i] = -INFINITY;
+          if (!(cur.ok_b && p0 + 16 + i <= upto)) sc[rb][1][i] = -INFINITY;
+        }
+      }
+    }
+    // Lazy reference maximum: it moves only when a row's has grown by more than 8 (in powers of two), decided from each lane's own scores, so the
+    // accumulators are rescaled once or twice a sweep; until then the exponentials stay below 256.
+    float lmx[RB];
+    bool grew = false;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const f32x4 x = sc[rb][0], y = sc[rb][1];
+      lmx[rb] = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))) * scale2;
+      grew = grew || lmx[rb] > m_run[rb] + 8.f;
+    }
+    if (__builtin_amdgcn_ballot_w64(grew) != 0ull) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float mx = quarter_max(lmx[rb]);
+        const bool grow = mx > m_run[rb] + 8.f;
+        const float corr = grow ? (m_run[rb] == -INFINITY ? 0.f : exp2f(m_run[rb] - mx)) : 1.f;
+        l_run[rb] *= corr;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          acc[rb][dt][0] *= corr; acc[rb][dt][1] *= corr; acc[rb][dt][2] *= corr; acc[rb][dt][3] *= corr;
+        }
+        if (grow) m_run[rb] = mx;
+      }
+    }
+    u32x4 ph[RB], pl[RB];   // probabilities as hi + lo pairs
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const float mb = (m_run[rb] == -INFINITY) ? 0.f : m_run[rb];
+      float pe[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pe[i] = __builtin_amdgcn_exp2f(fmaf(sc[rb][0][i], scale2, -mb));
+        pe[4 + i] = __builtin_amdgcn_exp2f(fmaf(sc[rb][1][i], scale2, -mb));
+      }
+      l_run[rb] += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t h = pack_bf16_pair(pe[2 * i], pe[2 * i + 1]);
+        ph[rb][i] = h;
+        pl[rb][i] = pack_bf16_pair(pe[2 * i] - __uint_as_float(h << 16), pe[2 * i + 1] - __uint_as_float(h & 0xFFFF0000u));
+      }
+    }
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");   // V is there (the next pair's K may still be on its way)
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    u32x4 keep = {~0u, ~0u, ~0u, ~0u};   // V of rows that were never written and of foreign pages: 0 * whatever is there must stay 0
+    if (base + 32 > w.c1 || !cur.ok_a || !cur.ok_b) {
+      const int pos_a = base + 4 * g, pos_b = base + 16 + 4 * g;
+      auto half = [&](bool ok, int p0) { return (ok && p0 < w.c1 ? 0x0000FFFFu : 0u) | (ok && p0 + 1 < w.c1 ? 0xFFFF0000u : 0u); };
+      keep = (u32x4){half(cur.ok_a, pos_a), half(cur.ok_a, pos_a + 2), half(cur.ok_b, pos_b), half(cur.ok_b, pos_b + 2)};
+    }
+    {
+      const uint2* va = reinterpret_cast<const uint2*>(my_ring + 2 * PART) + lane;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint2 a = va[dt * 64], b = va[PART / 8 + dt * 64];
+        const u32x4 vf = (u32x4){a.x, a.y, b.x, b.y} & keep;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)   // all hi products, then all lo products: two MFMAs on one accumulator are never back to back
+          acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, ph[rb]), acc[rb][dt], 0, 0, 0);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pl[rb]), acc[rb][dt], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the V half has been read
+    if (more) {
+      fetch(nxt.a + DF_PAGE * HD, 2 * PART);
+      fetch(nxt.b + DF_PAGE * HD, 3 * PART);
+    }
+    cur = nxt;
+  }
+
+  // ---- the wavefronts' parts together: the upper four hand theirs to the lower four, then all rows leave
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const float l = quarter_sum(l_run[rb]);
+    if (g == 0) s_ml[wave][rb * 16 + n] = make_float2(m_run[rb], l);
+  }
+  __syncthreads();   // also: every wavefront is done with the ring and the queries that s_o overlays
+  float mine[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    float m_all = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) m_all = fmaxf(m_all, s_ml[v][rb * 16 + n].x);
+    mine[rb] = m_run[rb] == m_all ? 1.f : __builtin_amdgcn_exp2f(m_run[rb] - m_all);   // (no key: both are -inf)
+  }
+  auto slot = [&](int v, int rb, int dt) { return reinterpret_cast<float4*>(&s_o[v][rb * 16 + n][dt * 16 + 4 * g]); };
+  if (wave >= 4) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        *slot(wave - 4, rb, dt) = make_float4(acc[rb][dt][0] * mine[rb], acc[rb][dt][1] * mine[rb], acc[rb][dt][2] * mine[rb], acc[rb][dt][3] * mine[rb]);
+  }
+  __syncthreads();
+  if (wave < 4) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        float4* p = slot(wave, rb, dt);
+        const float4 u = *p;
+        *p = make_float4(acc[rb][dt][0] * mine[rb] + u.x, acc[rb][dt][1] * mine[rb] + u.y, acc[rb][dt][2] * mine[rb] + u.z, acc[rb][dt][3] * mine[rb] + u.w);
+      }
+  }
+  __syncthreads();
+  const int parts = ga.prefix_splits + ga.own_splits;
+  for (int i = threadIdx.x; i < w.n_rows * (HD / 4); i += 64 * NW) {
+    const int r = i / (HD / 4), d4 = i % (HD / 4), row = w.row0 + r;
+    const int s = row / ga.rows, at = row % ga.rows;
+    const size_t pr = ((size_t)(s * geo.block_size + at / group) * ga.n_q_heads + kvh * group + at % group) * parts + w.part;
+    float4 o = *reinterpret_cast<const float4*>(&s_o[0][r][d4 * 4]);
+#pragma unroll
+    for (int v = 1; v < 4; ++v) {
+      const float4 a = *reinterpret_cast<const float4*>(&s_o[v][r][d4 * 4]);
+      o.x += a.x; o.y += a.y; o.z += a.z; o.w += a.w;
+    }
+    *reinterpret_cast<float4*>(part_o + pr * HD + d4 * 4) = o;
+    if (d4 == 0) {
+      float m_all = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) m_all = fmaxf(m_all, s_ml[v][r].x);
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        const float2 ml = s_ml[v][r];
+        l += ml.y == 0.f ? 0.f : ml.y * (ml.x == m_all ? 1.f : __builtin_amdgcn_exp2f(ml.x - m_all));
+      }
+      part_ml[pr] = make_float2(m_all, l);
+    }
+  }
+}
+
+template <int HD, int RBP, int RBO>
+__global__ __launch_bounds__(512, 2) void group_attn_keys_kernel(const bf16_t* __restrict__ q, const bf16_t* __restrict__ pool, SeqGeom geo, GroupArgs ga,
+                                                                 GroupTables gt, float* __restrict__ part_o, float2* __restrict__ part_ml) {
+  constexpr int RB = RBP > RBO ? RBP : RBO;
+  __shared__ __attribute__((aligned(1024))) char s_raw[KeySplit<HD>::bytes(RB)];
+  __shared__ float2 s_ml[8][64];
+  GroupWork w;
+  int kvh;
+  if (!group_work(w, kvh, geo, ga, gt)) return;
+  if (w.part < ga.prefix_splits) group_sweep_keys<HD, RBP>(s_raw, s_ml, w, kvh, q, pool, geo, ga, part_o, part_ml);
+  else group_sweep_keys<HD, RBO>(s_raw, s_ml, w, kvh, q, pool, geo, ga, part_o, part_ml);
+}
+
 // Parts -> rows, a wavefront a row, two dims a lane.  A part without keys (its sum is exactly 0) is left out.  OPERAND: GEMM activation operand (Act<T>), else
 // plain rows of the model's type.
 template <typename T, bool OPERAND>
@@ -363,6 +654,17 @@ template <typename T>
 inline void group_attn_launch(hipStream_t st, const T* q, const T* pool, const SeqGeom& geo, const GroupArgs& ga, int hd, const GroupTables& gt, float* part_o,
                               float2* part_ml) {
   const dim3 grid((ga.max_tiles * ga.prefix_splits + ga.n_seqs * ga.own_tiles * ga.own_splits) * ga.n_kv_heads), block(256);
+  if constexpr (sizeof(T) == 2) {
+    const bool few = ga.rows <= 16, few_all = (long long)ga.n_seqs * ga.rows <= 16;
+    auto keys = [&](auto c) {
+      constexpr int HD = decltype(c)::value;
+      if (few_all) hipLaunchKernelGGL((group_attn_keys_kernel<HD, 1, 1>), grid, dim3(512), 0, st, q, pool, geo, ga, gt, part_o, part_ml);
+      else if (few) hipLaunchKernelGGL((group_attn_keys_kernel<HD, 4, 1>), grid, dim3(512), 0, st, q, pool, geo, ga, gt, part_o, part_ml);
+      else hipLaunchKernelGGL((group_attn_keys_kernel<HD, 4, 4>), grid, dim3(512), 0, st, q, pool, geo, ga, gt, part_o, part_ml);
+    };
+    if (hd == 128) return keys(std::integral_constant<int, 128>{});
+    if (hd == 64) return keys(std::integral_constant<int, 64>{});
+  }
   auto go = [&](auto c) { hipLaunchKernelGGL((group_attn_kernel<T, decltype(c)::value>), grid, block, 0, st, q, pool, geo, ga, gt, part_o, part_ml); };
   switch (hd) {
     case 16: return go(std::integral_constant<int, 16>{});
