@@ -2,10 +2,10 @@
 //
 // The batch is cut into groups of consecutive sequences.  The leading pages that the block-table rows of a group have in common are attended
 // to once for all rows of the group (the prefix part), what lies behind them by each sequence for itself (its own part):
-//     row r:  o = softmax(q K^T * scale) V over both parts = (sum of parts of e^(m_i - m) o_i) / (sum of e^(m_i - m) l_i),
-// m_i, l_i, o_i a part's running maximum, sum of exponentials and unnormalised output, m the largest of the maxima.  Both parts are split along their
-// keys into ranges of equal length, ranges in a fixed order in the sum, so a call repeats itself bit for bit.  A row that sees no key is zeros; a NaN among
-// its scores makes it NaN.
+//     row r:  o = softmax(q K^T * scale) V over both parts = (sum of parts of 2^(m_i - m) o_i) / (sum of 2^(m_i - m) l_i),
+// m_i, l_i, o_i a part's reference maximum, sum of exponentials (base 2, scores times log2 e) and unnormalised output, m the largest of the maxima.  Both
+// parts are split along their keys into ranges of equal length, ranges in a fixed order in the sum, so a call repeats itself bit for bit.  A row that sees
+// no key is zeros; a NaN among its scores makes it NaN.
 //
 // What sequences share is found on the device, so a wrong grouping costs time and nothing else.
 //
@@ -13,70 +13,135 @@
 #pragma once
 #include "attn_mfma.h"
 
-constexpr int kGroupTile = 64;   // query rows of a workgroup
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct GroupArgs {
   int n_q_heads, n_kv_heads, layer, causal;
   int n_seqs, rows;         // query rows of a sequence and kv head = block size * (n_q_heads / n_kv_heads)
+  int tile;                 // rows of a tile of the prefix part: 64 or 128
   int max_tiles;            // tiles of the prefix part, at most
-  int own_tiles;            // tiles of a sequence's own part
+  int own_tiles;            // tiles (of 64 rows) of a sequence's own part
   int prefix_splits, own_splits;
   float scale;
 };
 
+constexpr int kOwnTile = 64;   // query rows of a workgroup of an own part
+
 // Written by group_plan_kernel, read by the launches behind it.
 struct GroupTables {
-  int4* tiles;      // first row, rows (0: no tile), block-table row to read, tokens of the prefix
-  int32_t* first;   // [n_seqs] tokens in front of a sequence's own part
+  int4* tiles;       // first row, rows (0: no tile), first sequence of the group, first one behind it
+  int2* group;       // [n_seqs] first sequence of the sequence's group, first one behind it
+  int32_t* common;   // [n_seqs] tokens that the sequence has in common with the first one of its group: whole pages, committed in both
 };
-// Tiles of the prefix part: group g, which starts at sequence a, has those from a * rows / kGroupTile + g on (rounded down: whatever the groups in
+// Tiles of the prefix part: a group that starts at sequence a and is the g-th has those from a * rows / tile + g on (rounded down: whatever the groups in
 // front of it need lies below), so no group has to wait for another's count.
-__host__ __device__ __forceinline__ int group_tile_slots(int n_seqs, int rows, int n_groups) { return (int)((long long)n_seqs * rows / kGroupTile) + n_groups; }
+__host__ __device__ __forceinline__ int group_tile_slots(int n_seqs, int rows, int tile, int n_groups) { return (int)((long long)n_seqs * rows / tile) + n_groups; }
 
-// Groups -> tiles, a workgroup each: where the group starts and ends (the caller's starts as their running maximum, inside the batch, the first 0 and the
-// last end n_seqs), and how many leading pages its rows have in common and committed.  n_groups = 1 needs no starts.
-__global__ __launch_bounds__(1024) void group_plan_kernel(SeqGeom geo, const int32_t* __restrict__ starts, int n_groups, int n_seqs, int rows, GroupTables gt) {
-  __shared__ int s_start, s_end, s_pages;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, g = blockIdx.x;
+// Groups -> tiles, a workgroup a sequence: which group it belongs to (the caller's starts as their running maximum, inside the batch; the first is 0), what it has in
+// common with the group's first sequence, and, of that one, the group's tiles.  n_groups = 1 needs no starts.
+__global__ __launch_bounds__(256) void group_plan_kernel(SeqGeom geo, const int32_t* __restrict__ starts, int n_groups, int n_seqs, int rows, int tile, GroupTables gt) {
+  __shared__ int s_next, s_start, s_end, s_after, s_pages;
+  const int t = threadIdx.x, s = blockIdx.x, mpps = geo.max_pages_per_seq;
   if (t == 0) {
+    s_next = s_after = n_groups;   // the first groups whose starts lie behind this sequence and behind the group's end
     s_start = 0;
-    s_end = g + 1 < n_groups ? 0 : n_seqs;
-    s_pages = geo.max_pages_per_seq;
+    s_end = n_seqs;
+    s_pages = mpps;
   }
   __syncthreads();
   if (n_groups > 1) {
-    for (int i = t; i <= g + 1 && i < n_groups; i += 1024) {
-      const int given = starts[i], at = i == 0 ? 0 : min(max(given, 0), n_seqs);
-      if (given != at || (i + 1 < n_groups && starts[i + 1] < given)) atomicOr(geo.status, DF_STATUS_CAPACITY);
-      if (i <= g) atomicMax(&s_start, at);
-      atomicMax(&s_end, at);
-    }
-    __syncthreads();
-  }
-  const int start = s_start, end = s_end, size = end - start, mpps = geo.max_pages_per_seq;
-  if (size > 0) {
-    for (int s = start + t; s < end; s += 1024) atomicMin(&s_pages, size > 1 ? max(geo.seq_lens[s], 0) / DF_PAGE : 0);
-    __syncthreads();
-    const int32_t* lead = geo.block_table + (size_t)start * mpps;
-    int most = s_pages;
-    __syncthreads();
-    for (int k = wave; k < size; k += 16) {   // the first one against the range of page ids, the others against it
-      const int32_t* row = lead + (size_t)k * mpps;
-      for (int p = lane; p < most; p += 64) {
-        const int id = lead[p];
-        if (k ? row[p] != id : (id < 0 || id >= geo.n_pages)) most = p;
+    for (int i = 1 + t; i < n_groups; i += 256)
+      if (starts[i] > s) {
+        atomicMin(&s_next, i);
+        break;
       }
-    }
-    atomicMin(&s_pages, most);
     __syncthreads();
-    for (int s = start + t; s < end; s += 1024) gt.first[s] = s_pages * DF_PAGE;
+    const int next = s_next;
+    for (int i = t; i < n_groups; i += 256) {
+      const int at = starts[i];
+      if (i > 0 && i < next) atomicMax(&s_start, min(max(at, 0), n_seqs));
+      if (i == next) s_end = min(at, n_seqs);
+      if (s == 0 && (i == 0 ? at != 0 : at < starts[i - 1] || at > n_seqs)) atomicOr(geo.status, DF_STATUS_CAPACITY);
+    }
+    __syncthreads();
+    for (int i = 1 + t; i < n_groups; i += 256)
+      if (starts[i] > s_end) {
+        atomicMin(&s_after, i);
+        break;
+      }
   }
-  // this group's tiles, and the slots behind them up to the next group's
-  const int row0 = start * rows, row1 = end * rows, slot0 = row0 / kGroupTile + g, slot1 = row1 / kGroupTile + g + 1;
-  for (int i = slot0 + t; i < slot1; i += 1024) {
-    const int r = row0 + (i - slot0) * kGroupTile;
-    gt.tiles[i] = make_int4(r, size > 0 ? max(0, min(kGroupTile, row1 - r)) : 0, start, s_pages * DF_PAGE);
+  const int g = s_next - 1, start = s_start, end = s_end;
+  const int32_t *lead = geo.block_table + (size_t)start * mpps, *row = geo.block_table + (size_t)s * mpps;
+  const int most = end - start > 1 ? min(mpps, min(max(geo.seq_lens[s], 0), max(geo.seq_lens[start], 0)) / DF_PAGE) : 0;
+  int pages = most;
+  for (int p = t; p < pages; p += 256) {
+    const int id = lead[p];
+    if (id < 0 || id >= geo.n_pages || row[p] != id) pages = p;
   }
+  if (pages < most) atomicMin(&s_pages, pages);
+  __syncthreads();
+  if (t == 0) {
+    gt.group[s] = make_int2(start, end);
+    gt.common[s] = min(most, s_pages) * DF_PAGE;
+  }
+  if (s != start) return;
+  // this group's tiles, then empty ones up to those of the group that sequence `end` belongs to (groups without sequences lie between)
+  const int row0 = start * rows, row1 = end * rows, slot0 = row0 / tile + g;
+  const int slot1 = end < n_seqs ? row1 / tile + s_after - 1 : group_tile_slots(n_seqs, rows, tile, n_groups);
+  for (int i = (s == 0 ? 0 : slot0) + t; i < slot1; i += 256) {
+    const int r = row0 + (i - slot0) * tile;
+    gt.tiles[i] = make_int4(r, i < slot0 ? 0 : max(0, min(tile, row1 - r)), start, end);
+  }
+}
+
+// What a workgroup does: query rows, their keys' pages, and where the partial results go.
+struct GroupWork {
+  int row0, n_rows;         // rows of the kv head
+  const int32_t* table;     // block-table row
+  int c0, c1;               // keys from c0 to below c1
+  int own_len;              // causal mask of a sequence's own part: tokens in front of its block; < 0: every row sees every key
+  int part;                 // index of the partial result
+};
+
+// tokens that a group has in common (the same in all lanes)
+__device__ __forceinline__ int group_prefix(const GroupTables& gt, int start, int end) {
+  int c = 0x7FFFFFFF;
+  for (int s = start + (threadIdx.x & 63); s < end; s += 64) c = min(c, gt.common[s]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) c = min(c, __shfl_xor(c, d, 64));
+  return __builtin_amdgcn_readfirstlane(c);
+}
+
+// grid: (tiles of the prefix part x its key ranges, then tiles of the own parts x theirs) x kv heads, kv heads fastest: workgroups that read the same keys lie a
+// multiple of 8 apart where heads x ranges divide by 8, so on one XCD.  False: there is nothing to do (a tile without rows), or a prefix range has no keys, which
+// this writes down.
+template <int THREADS>
+__device__ __forceinline__ bool group_work(GroupWork& w, int& kvh, const SeqGeom& geo, const GroupArgs& ga, const GroupTables& gt, float2* part_ml) {
+  int i = blockIdx.x / ga.n_kv_heads;
+  kvh = blockIdx.x % ga.n_kv_heads;
+  const int n_prefix = ga.max_tiles * ga.prefix_splits;
+  if (i < n_prefix) {
+    const int4 t = gt.tiles[i / ga.prefix_splits];
+    if (t.y == 0) return false;
+    const int split = i % ga.prefix_splits, prefix = group_prefix(gt, t.z, t.w);
+    const int chunk = ((prefix + 31) / 32 + ga.prefix_splits - 1) / ga.prefix_splits * 32;
+    w = {t.x, t.y, geo.block_table + (size_t)t.z * geo.max_pages_per_seq, min(split * chunk, prefix), min((split + 1) * chunk, prefix), -1, split};
+    if (w.c0 < w.c1) return true;
+    const int parts = ga.prefix_splits + ga.own_splits, group = ga.n_q_heads / ga.n_kv_heads;
+    for (int r = threadIdx.x; r < t.y; r += THREADS) {
+      const int row = t.x + r, s = row / ga.rows, at = row % ga.rows;
+      part_ml[((size_t)(s * geo.block_size + at / group) * ga.n_q_heads + kvh * group + at % group) * parts + split] = make_float2(-INFINITY, 0.f);
+    }
+    return false;
+  }
+  i -= n_prefix;
+  const int split = i % ga.own_splits, tile = i / ga.own_splits % ga.own_tiles, s = i / (ga.own_splits * ga.own_tiles);
+  const int2 g = gt.group[s];
+  const int len = max(geo.seq_lens[s], 0), n_tok = min(len + geo.block_size, geo.max_pages_per_seq * DF_PAGE), first = group_prefix(gt, g.x, g.y);
+  const int chunk = ((n_tok - first + 31) / 32 + ga.own_splits - 1) / ga.own_splits * 32;
+  w = {s * ga.rows + tile * kOwnTile, min(kOwnTile, ga.rows - tile * kOwnTile), geo.block_table + (size_t)s * geo.max_pages_per_seq,
+       min(first + split * chunk, n_tok), min(first + (split + 1) * chunk, n_tok), ga.causal ? len : -1, ga.prefix_splits + split};
+  return true;
 }
 
 // ---- storage types: fragments of a page pair and their products ------------------------------------------------------------
@@ -126,14 +191,14 @@ struct PairFrags<bf16_t, HD> {
       sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k.b[kt]), __builtin_bit_cast(bf16x8, q.q[kt]), sb, 0, 0, 0);
     }
   }
-  // V elements of keys that are not there (never written, another sequence's): 0 * whatever they hold must stay 0
-  static __device__ __forceinline__ void clear(Values& f, const bool (&there)[8]) {
-    auto half = [&](int i) { return (there[i] ? 0x0000FFFFu : 0u) | (there[i + 1] ? 0xFFFF0000u : 0u); };
-    const unsigned m[4] = {half(0), half(2), half(4), half(6)};
+  // V elements of keys that are not there (never written, another sequence's; there: a bit a key): 0 * whatever they hold must stay 0
+  static __device__ __forceinline__ void clear(Values& f, unsigned there) {
+    auto half = [&](int i) { return (there >> i & 1 ? 0x0000FFFFu : 0u) | (there >> i & 2 ? 0xFFFF0000u : 0u); };
+    const unsigned m0 = half(0), m1 = half(2), m2 = half(4), m3 = half(6);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      f.a[dt].x &= m[0]; f.a[dt].y &= m[1];
-      f.b[dt].x &= m[2]; f.b[dt].y &= m[3];
+      f.a[dt].x &= m0; f.a[dt].y &= m1;
+      f.b[dt].x &= m2; f.b[dt].y &= m3;
     }
   }
   static __device__ __forceinline__ void add(f32x4 (&acc)[DT], const Values& v, const float (&p)[8]) {
@@ -192,11 +257,12 @@ struct PairFrags<float, HD> {
       sb = __builtin_amdgcn_mfma_f32_16x16x4f32(k.b[kt].y, q.q[kt].y, sb, 0, 0, 0);
     }
   }
-  static __device__ __forceinline__ void clear(Values& f, const bool (&there)[8]) {
+  static __device__ __forceinline__ void clear(Values& f, unsigned there) {
+    auto keep = [&](int i, float v) { return there >> i & 1 ? v : 0.f; };
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      f.a[dt] = make_float4(there[0] ? f.a[dt].x : 0.f, there[1] ? f.a[dt].y : 0.f, there[2] ? f.a[dt].z : 0.f, there[3] ? f.a[dt].w : 0.f);
-      f.b[dt] = make_float4(there[4] ? f.b[dt].x : 0.f, there[5] ? f.b[dt].y : 0.f, there[6] ? f.b[dt].z : 0.f, there[7] ? f.b[dt].w : 0.f);
+      f.a[dt] = make_float4(keep(0, f.a[dt].x), keep(1, f.a[dt].y), keep(2, f.a[dt].z), keep(3, f.a[dt].w));
+      f.b[dt] = make_float4(keep(4, f.b[dt].x), keep(5, f.b[dt].y), keep(6, f.b[dt].z), keep(7, f.b[dt].w));
     }
   }
   static __device__ __forceinline__ void add(f32x4 (&acc)[DT], const Values& v, const float (&p)[8]) {
@@ -214,57 +280,29 @@ struct PairFrags<float, HD> {
   }
 };
 
-// What a workgroup does: query rows, their keys' pages, and where the partial results go.
-struct GroupWork {
-  int row0, n_rows;         // rows of the kv head
-  const int32_t* table;     // block-table row
-  int c0, c1, n_tok;        // keys from c0 to below c1; keys from n_tok on were never written
-  int own_len;              // causal mask of a sequence's own part: tokens in front of its block; < 0: every row sees every key
-  int part;                 // index of the partial result
-};
-
-// grid: (tiles of the prefix part x its key ranges, then tiles of the own parts x theirs) x kv heads, kv heads fastest: the tiles that share keys lie
-// max_tiles apart in steps of a multiple of the heads and ranges
-__device__ __forceinline__ bool group_work(GroupWork& w, int& kvh, const SeqGeom& geo, const GroupArgs& ga, const GroupTables& gt) {
-  int i = blockIdx.x / ga.n_kv_heads;
-  kvh = blockIdx.x % ga.n_kv_heads;
-  const int n_prefix = ga.max_tiles * ga.prefix_splits;
-  if (i < n_prefix) {
-    const int4 t = gt.tiles[i / ga.prefix_splits];
-    const int split = i % ga.prefix_splits;
-    if (t.y == 0 || t.w == 0) return false;   // the merge looks at `first` and leaves the prefix out
-    const int chunk = ((t.w + 31) / 32 + ga.prefix_splits - 1) / ga.prefix_splits * 32;
-    w = {t.x, t.y, geo.block_table + (size_t)t.z * geo.max_pages_per_seq, min(split * chunk, t.w), min((split + 1) * chunk, t.w), t.w, -1, split};
-    return true;
-  }
-  i -= n_prefix;
-  const int split = i % ga.own_splits, tile = i / ga.own_splits % ga.own_tiles, s = i / (ga.own_splits * ga.own_tiles);
-  const int len = max(geo.seq_lens[s], 0), n_tok = min(len + geo.block_size, geo.max_pages_per_seq * DF_PAGE), first = gt.first[s];
-  const int chunk = ((n_tok - first + 31) / 32 + ga.own_splits - 1) / ga.own_splits * 32;
-  w = {s * ga.rows + tile * kGroupTile, min(kGroupTile, ga.rows - tile * kGroupTile), geo.block_table + (size_t)s * geo.max_pages_per_seq,
-       min(first + split * chunk, n_tok), min(first + (split + 1) * chunk, n_tok), n_tok, ga.causal ? len : -1, ga.prefix_splits + split};
-  return true;
-}
-
-// Any storage type and head dim.  Four wavefronts of 16 rows each sweep the workgroup's keys, a pair of pages at a time straight from memory.
+// Any storage type and head dim.  A wavefront sweeps 16 rows, pairs of pages straight from memory; the workgroup's four share its rows (up to 64) or, where there
+// are fewer, the keys too, and add their parts in LDS.
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict__ q, const T* __restrict__ pool, SeqGeom geo, GroupArgs ga, GroupTables gt,
                                                             float* __restrict__ part_o, float2* __restrict__ part_ml) {
   typedef PairFrags<T, HD> F;
-  constexpr int DT = HD / 16;
+  constexpr int DT = HD / 16, LD = HD + 4;
+  __shared__ float s_o[3][16][LD];
+  __shared__ float2 s_ml[3][16];
   GroupWork w;
   int kvh;
-  if (!group_work(w, kvh, geo, ga, gt)) return;
+  if (!group_work<256>(w, kvh, geo, ga, gt, part_ml)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  if (wave * 16 >= w.n_rows) return;
+  const int blocks = w.n_rows > 32 ? 4 : w.n_rows > 16 ? 2 : 1, shares = 4 / blocks;   // wavefronts that share rows, and that share keys
+  const int block = wave % blocks, share = wave / blocks;
   const int group = ga.n_q_heads / ga.n_kv_heads;
-  const bool valid = wave * 16 + n < w.n_rows;
-  const int row = w.row0 + (valid ? wave * 16 + n : 0);
+  const bool valid = block * 16 + n < w.n_rows;
+  const int row = w.row0 + (valid ? block * 16 + n : 0);
   const int s = row / ga.rows, slot = row % ga.rows / group, hq = kvh * group + row % group;   // rows is a multiple of the group
   const size_t m_hq = (size_t)(s * geo.block_size + slot) * ga.n_q_heads + hq;
   typename F::Query qf;
   F::query(qf, valid ? q + m_hq * HD : nullptr, lane);
-  const int last = !valid ? -1 : (w.own_len >= 0 ? w.own_len + slot : w.n_tok - 1);
+  const int last = !valid ? -1 : (w.own_len >= 0 ? w.own_len + slot : 0x7FFFFFFF);
 
   float m_run = -INFINITY, l_run = 0.f;
   f32x4 acc[DT];
@@ -272,30 +310,39 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
   for (int dt = 0; dt < DT; ++dt) acc[dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
   const float scale2 = ga.scale * 1.44269504088896341f;   // base-2 exponents
 
-  for (int base = w.c0; base < w.c1; base += 32) {
+  struct Ids { int a, b; };
+  auto ids_of = [&](int base) {   // foreign and missing pages as -1
     const int at = base / DF_PAGE;
-    int pa = w.table[at], pb = base + DF_PAGE < w.c1 ? w.table[at + 1] : -1;
-    const bool ok_a = pa >= 0 && pa < geo.n_pages, ok_b = pb >= 0 && pb < geo.n_pages;
-    pa = ok_a ? pa : 0;   // a page that may be read; its keys weigh nothing
-    pb = ok_b ? pb : pa;
-    const T* ka = pool + kv_head_base(ga.layer, geo.n_pages, pa, ga.n_kv_heads, kvh, HD);
-    const T* kb = pool + kv_head_base(ga.layer, geo.n_pages, pb, ga.n_kv_heads, kvh, HD);
-    typename F::Keys kf;
-    typename F::Values vf;
-    F::keys(kf, ka, kb, lane);
-    F::values(vf, ka, kb, lane);
+    Ids p{-1, -1};
+    if (base < w.c1) p.a = w.table[at];
+    if (base + DF_PAGE < w.c1) p.b = w.table[at + 1];
+    if (p.a < 0 || p.a >= geo.n_pages) p.a = -1;
+    if (p.b < 0 || p.b >= geo.n_pages) p.b = -1;
+    return p;
+  };
+  auto page = [&](int id) { return pool + kv_head_base(ga.layer, geo.n_pages, id, ga.n_kv_heads, kvh, HD); };
+  const int step = 32 * shares;
+  int base = w.c0 + 32 * share;
+  Ids id = ids_of(base);
+  typename F::Keys kf;
+  typename F::Values vf;
+  if (base < w.c1) F::keys(kf, page(max(id.a, 0)), page(id.b >= 0 ? id.b : max(id.a, 0)), lane);   // a page that may be read; its keys weigh nothing
+  for (; base < w.c1; base += step) {
+    const bool ok_a = id.a >= 0, ok_b = id.b >= 0;
+    F::values(vf, page(max(id.a, 0)), page(ok_b ? id.b : max(id.a, 0)), lane);
+    id = ids_of(base + step);
     f32x4 sa, sb;
     F::scores(sa, sb, kf, qf);
+    if (base + step < w.c1) F::keys(kf, page(max(id.a, 0)), page(id.b >= 0 ? id.b : max(id.a, 0)), lane);   // the next pair's, behind the softmax and the products
     float v[8], p[8];
-    bool there[8], all = true;
+    unsigned there = 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int pos = base + (i >> 2) * DF_PAGE + 4 * g + (i & 3);
-      there[i] = (i < 4 ? ok_a : ok_b) && pos < w.c1;
-      all = all && there[i];
-      v[i] = there[i] && pos <= last ? (i < 4 ? sa[i & 3] : sb[i & 3]) * scale2 : -INFINITY;
+      const bool in = (i < 4 ? ok_a : ok_b) && pos < w.c1;
+      there |= in ? 1u << i : 0u;
+      v[i] = in && pos <= last ? (i < 4 ? sa[i & 3] : sb[i & 3]) * scale2 : -INFINITY;
     }
-    if (!all) F::clear(vf, there);
     float mx = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
     mx = quarter_max(mx);
     const float m_new = fmaxf(m_run, mx), mb = m_new == -INFINITY ? 0.f : m_new;   // nothing visible yet: exp2(-inf - 0) = 0
@@ -308,9 +355,34 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
     for (int dt = 0; dt < DT; ++dt) {
       acc[dt][0] *= corr; acc[dt][1] *= corr; acc[dt][2] *= corr; acc[dt][3] *= corr;
     }
+    if (there != 0xFFu) F::clear(vf, there);
     F::add(acc, vf, p);
   }
-  const float l = quarter_sum(l_run);
+  float l = quarter_sum(l_run);
+  if (shares > 1) {   // uniform over the workgroup
+    if (share > 0) {
+      const int to = (share - 1) * blocks + block;
+      if (g == 0) s_ml[to][n] = make_float2(m_run, l);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<float4*>(&s_o[to][n][dt * 16 + 4 * g]) = make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]);
+    }
+    __syncthreads();
+    if (share > 0) return;
+    for (int i = 1; i < shares; ++i) {
+      const int from = (i - 1) * blocks + block;
+      const float2 ml = s_ml[from][n];
+      if (ml.y == 0.f) continue;   // no visible key
+      const float m_new = fmaxf(m_run, ml.x);
+      const float f0 = m_run == m_new ? 1.f : exp2f(m_run - m_new), f1 = ml.x == m_new ? 1.f : exp2f(ml.x - m_new);
+      l = l * f0 + ml.y * f1;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const float4 o = *reinterpret_cast<const float4*>(&s_o[from][n][dt * 16 + 4 * g]);
+        acc[dt] = (f32x4){acc[dt][0] * f0 + o.x * f1, acc[dt][1] * f0 + o.y * f1, acc[dt][2] * f0 + o.z * f1, acc[dt][3] * f0 + o.w * f1};
+      }
+    }
+  }
   if (!valid) return;
   const size_t pr = m_hq * (ga.prefix_splits + ga.own_splits) + w.part;
   if (g == 0) part_ml[pr] = make_float2(m_run, l);
@@ -320,25 +392,28 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
 }
 
 // ---- bf16, head dim 64 or 128: wavefronts split the keys ------------------------------------------------------------------
-// Eight wavefronts take every eighth pair of pages each for all RB blocks of 16 query rows, from a ring of their own in LDS: the pages go there
+// Four wavefronts take every fourth pair of pages each for all RB blocks of 16 query rows, from a ring of their own in LDS: the pages go there
 // directly (global_load_lds), K refilled as soon as a pair's scores are done and V as soon as its products are, so nothing in flight costs a
 // register and no wavefront waits for another before the end, where their partial results are added in LDS.  The loads are counted by hand (NI per half page,
-// in order): the compiler would wait for all of them ahead of every LDS read.
+// in order): the compiler would wait for all of them ahead of every LDS read.  Two workgroups a CU.
 template <int HD>
 struct KeySplit {
-  static constexpr int KT = HD / 32, DT = HD / 16, NW = 8, LD = HD + 4;
+  static constexpr int KT = HD / 32, DT = HD / 16, NW = 4, LD = HD + 4;
   static constexpr int PART = DF_PAGE * HD * 2, NI = PART / 1024;   // bytes of the K or V part of a page, load instructions for it
   static constexpr int RING = NW * 4 * PART;                        // per wavefront: K of page A, of page B, V of page A, of page B
-  static constexpr int bytes(int rb) { return (RING + rb * KT * 1024 > 4 * rb * 16 * LD * 4 ? RING + rb * KT * 1024 : 4 * rb * 16 * LD * 4); }
+  // ring and queries; in the end two wavefronts' rows from the start and all wavefronts' maxima and sums behind them
+  static constexpr int OUT(int rb) { return 2 * rb * 16 * LD * 4; }
+  static constexpr int bytes(int rb) { return RING + rb * KT * 1024 > OUT(rb) + NW * rb * 16 * 8 ? RING + rb * KT * 1024 : OUT(rb) + NW * rb * 16 * 8; }
 };
 
 template <int HD, int RB>
-__device__ __forceinline__ void group_sweep_keys(char* s_raw, float2 (*s_ml)[64], const GroupWork& w, int kvh, const bf16_t* __restrict__ q,
+__device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w, int kvh, const bf16_t* __restrict__ q,
                                                  const bf16_t* __restrict__ pool, const SeqGeom& geo, const GroupArgs& ga, float* __restrict__ part_o,
                                                  float2* __restrict__ part_ml) {
   typedef KeySplit<HD> C;
   constexpr int KT = C::KT, DT = C::DT, NW = C::NW, LD = C::LD, PART = C::PART, NI = C::NI;
-  float (*s_o)[RB * 16][LD] = reinterpret_cast<float (*)[RB * 16][LD]>(s_raw);   // overlays ring and queries in the end
+  float (*s_o)[RB * 16][LD] = reinterpret_cast<float (*)[RB * 16][LD]>(s_raw);
+  float2 (*s_ml)[RB * 16] = reinterpret_cast<float2 (*)[RB * 16]>(s_raw + C::OUT(RB));
   u32x4* q_lds = reinterpret_cast<u32x4*>(s_raw + C::RING);                      // [rb][kt][lane]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int group = ga.n_q_heads / ga.n_kv_heads, page0 = w.c0 / DF_PAGE;
@@ -412,55 +487,40 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, float2 (*s_ml)[64]
   const float scale2 = ga.scale * 1.44269504088896341f;
   const char* my_ring = s_raw + wave * (4 * PART);
 
-  for (int k = 0; k < my_pairs; ++k) {
-    const int base = w.c0 + (wave + NW * k) * 32;
-    const bool more = k + 1 < my_pairs;
-    if (more && ((k + 1) & 31) == 0) {
-      ids = ids_next;
-      if (k + 33 < my_pairs) ids_next = load_ids(k + 33);
-    }
-    Pair nxt = cur;
-    if (more) nxt = pair_of(k + 1);
-
+  f32x4 sc[RB][2];
+  u32x4 ph[RB], pl[RB];   // probabilities as hi + lo pairs
+  auto scores = [&](int k) {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");   // this pair's K is there (its V still on the way)
-    f32x4 sc[RB][2];
-    {
-      const u32x4* kp = reinterpret_cast<const u32x4*>(my_ring) + lane;
-      u32x4 ka[KT], kb[KT];
+    const u32x4* kp = reinterpret_cast<const u32x4*>(my_ring) + lane;
+    u32x4 ka[KT], kb[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      ka[kt] = kp[kt * 64];
+      kb[kt] = kp[PART / 16 + kt * 64];
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      asm volatile("" ::: "memory");   // the query fragments of one row block at a time: together they would cost 64 registers
+      sc[rb][0] = sc[rb][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
-        ka[kt] = kp[kt * 64];
-        kb[kt] = kp[PART / 16 + kt * 64];
-      }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        asm volatile("" ::: "memory");   // the query fragments of one row block at a time: together they would cost 64 registers
-        sc[rb][0] = sc[rb][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          const u32x4 qf = q_lds[(rb * KT + kt) * 64 + lane];
-          sc[rb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[kt]), __builtin_bit_cast(bf16x8, qf), sc[rb][0], 0, 0, 0);
-          sc[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kb[kt]), __builtin_bit_cast(bf16x8, qf), sc[rb][1], 0, 0, 0);
-        }
+        const u32x4 qf = q_lds[(rb * KT + kt) * 64 + lane];
+        sc[rb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[kt]), __builtin_bit_cast(bf16x8, qf), sc[rb][0], 0, 0, 0);
+        sc[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kb[kt]), __builtin_bit_cast(bf16x8, qf), sc[rb][1], 0, 0, 0);
       }
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the K half has been read
-    if (more) {
-      fetch(nxt.a, 0);
-      fetch(nxt.b, PART);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-
-    const bool tail = !cur.ok_a || !cur.ok_b || base + 32 > n_all;   // (n_all <= c1: keys behind the range as well)
-    if (tail) {
+  };
+  auto softmax = [&](const Pair& pr, int base) {
+    if (!pr.ok_a || !pr.ok_b || base + 32 > n_all) {   // (n_all <= c1: keys behind the range as well)
       const int p0 = base + 4 * g;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const int upto = min(w.c1 - 1, last[rb]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (!(cur.ok_a && p0 + i <= upto)) sc[rb][0][i] = -INFINITY;
-          if (!(cur.ok_b && p0 + 16 + i <= upto)) sc[rb][1][i] = -INFINITY;
+          if (!(pr.ok_a && p0 + i <= upto)) sc[rb][0][i] = -INFINITY;
+          if (!(pr.ok_b && p0 + 16 + i <= upto)) sc[rb][1][i] = -INFINITY;
         }
       }
     }
@@ -488,7 +548,6 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, float2 (*s_ml)[64]
         if (grow) m_run[rb] = mx;
       }
     }
-    u32x4 ph[RB], pl[RB];   // probabilities as hi + lo pairs
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const float mb = (m_run[rb] == -INFINITY) ? 0.f : m_run[rb];
@@ -506,43 +565,74 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, float2 (*s_ml)[64]
         pl[rb][i] = pack_bf16_pair(pe[2 * i] - __uint_as_float(h << 16), pe[2 * i + 1] - __uint_as_float(h & 0xFFFF0000u));
       }
     }
-    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");   // V is there (the next pair's K may still be on its way)
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    u32x4 keep = {~0u, ~0u, ~0u, ~0u};   // V of rows that were never written and of foreign pages: 0 * whatever is there must stay 0
-    if (base + 32 > w.c1 || !cur.ok_a || !cur.ok_b) {
+  };
+  auto products = [&](const Pair& pr, int base) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");   // V is there (the next pair's K may still be on its way)
+    uint2* va = reinterpret_cast<uint2*>(s_raw + wave * (4 * PART) + 2 * PART) + lane;
+    if (base + 32 > w.c1 || !pr.ok_a || !pr.ok_b) {   // V of rows that were never written and of foreign pages: 0 * whatever is there must stay 0
       const int pos_a = base + 4 * g, pos_b = base + 16 + 4 * g;
       auto half = [&](bool ok, int p0) { return (ok && p0 < w.c1 ? 0x0000FFFFu : 0u) | (ok && p0 + 1 < w.c1 ? 0xFFFF0000u : 0u); };
-      keep = (u32x4){half(cur.ok_a, pos_a), half(cur.ok_a, pos_a + 2), half(cur.ok_b, pos_b), half(cur.ok_b, pos_b + 2)};
-    }
-    {
-      const uint2* va = reinterpret_cast<const uint2*>(my_ring + 2 * PART) + lane;
-#pragma unroll
+      const unsigned a0 = half(pr.ok_a, pos_a), a1 = half(pr.ok_a, pos_a + 2), b0 = half(pr.ok_b, pos_b), b1 = half(pr.ok_b, pos_b + 2);
+#pragma unroll 1
       for (int dt = 0; dt < DT; ++dt) {
-        const uint2 a = va[dt * 64], b = va[PART / 8 + dt * 64];
-        const u32x4 vf = (u32x4){a.x, a.y, b.x, b.y} & keep;
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)   // all hi products, then all lo products: two MFMAs on one accumulator are never back to back
-          acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, ph[rb]), acc[rb][dt], 0, 0, 0);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-          acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pl[rb]), acc[rb][dt], 0, 0, 0);
+        uint2 a = va[dt * 64], b = va[PART / 8 + dt * 64];
+        va[dt * 64] = make_uint2(a.x & a0, a.y & a1);
+        va[PART / 8 + dt * 64] = make_uint2(b.x & b0, b.y & b1);
       }
+      asm volatile("" ::: "memory");
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const uint2 a = va[dt * 64], b = va[PART / 8 + dt * 64];
+      const u32x4 vf = {a.x, a.y, b.x, b.y};
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)   // all hi products, then all lo products: two MFMAs on one accumulator are never back to back
+        acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, ph[rb]), acc[rb][dt], 0, 0, 0);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+        acc[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pl[rb]), acc[rb][dt], 0, 0, 0);
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the V half has been read
-    if (more) {
-      fetch(nxt.a + DF_PAGE * HD, 2 * PART);
-      fetch(nxt.b + DF_PAGE * HD, 3 * PART);
+  };
+  if (my_pairs > 0) {
+    Pair prev = cur;
+    auto next = [&](int k) {   // the K of pair k on its way, after the last pair that one's again: the number of loads in flight stays the same
+      if (k < my_pairs) {
+        if ((k & 31) == 0) {
+          ids = ids_next;
+          if (k + 32 < my_pairs) ids_next = load_ids(k + 32);
+          asm volatile("" : "+v"(ids_next));   // waited for here: left to the compiler it would be a wait for every copy at the end of every pair
+        }
+        cur = pair_of(k);
+      }
+      fetch(cur.a, 0);
+      fetch(cur.b, PART);
+    };
+    scores(0);
+    next(1);
+    softmax(prev, w.c0 + wave * 32);
+    for (int k = 1; k < my_pairs; ++k) {
+      const int base = w.c0 + (wave + NW * k) * 32;
+      products(prev, base - NW * 32);
+      prev = cur;
+      fetch(cur.a + DF_PAGE * HD, 2 * PART);
+      fetch(cur.b + DF_PAGE * HD, 3 * PART);
+      scores(k);
+      next(k + 1);
+      softmax(prev, base);
     }
-    cur = nxt;
+    products(prev, w.c0 + (wave + NW * (my_pairs - 1)) * 32);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may still be on its way into the ring when it is overlaid
   }
 
-  // ---- the wavefronts' parts together: the upper four hand theirs to the lower four, then all rows leave
+  // ---- the wavefronts' parts together: the upper two hand theirs to the lower two, then all rows leave
+  __syncthreads();   // every wavefront is done with the ring and the queries
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const float l = quarter_sum(l_run[rb]);
     if (g == 0) s_ml[wave][rb * 16 + n] = make_float2(m_run[rb], l);
   }
-  __syncthreads();   // also: every wavefront is done with the ring and the queries that s_o overlays
+  __syncthreads();
   float mine[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -552,15 +642,15 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, float2 (*s_ml)[64]
     mine[rb] = m_run[rb] == m_all ? 1.f : __builtin_amdgcn_exp2f(m_run[rb] - m_all);   // (no key: both are -inf)
   }
   auto slot = [&](int v, int rb, int dt) { return reinterpret_cast<float4*>(&s_o[v][rb * 16 + n][dt * 16 + 4 * g]); };
-  if (wave >= 4) {
+  if (wave >= 2) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
-        *slot(wave - 4, rb, dt) = make_float4(acc[rb][dt][0] * mine[rb], acc[rb][dt][1] * mine[rb], acc[rb][dt][2] * mine[rb], acc[rb][dt][3] * mine[rb]);
+        *slot(wave - 2, rb, dt) = make_float4(acc[rb][dt][0] * mine[rb], acc[rb][dt][1] * mine[rb], acc[rb][dt][2] * mine[rb], acc[rb][dt][3] * mine[rb]);
   }
   __syncthreads();
-  if (wave < 4) {
+  if (wave < 2) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -576,13 +666,8 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, float2 (*s_ml)[64]
     const int r = i / (HD / 4), d4 = i % (HD / 4), row = w.row0 + r;
     const int s = row / ga.rows, at = row % ga.rows;
     const size_t pr = ((size_t)(s * geo.block_size + at / group) * ga.n_q_heads + kvh * group + at % group) * parts + w.part;
-    float4 o = *reinterpret_cast<const float4*>(&s_o[0][r][d4 * 4]);
-#pragma unroll
-    for (int v = 1; v < 4; ++v) {
-      const float4 a = *reinterpret_cast<const float4*>(&s_o[v][r][d4 * 4]);
-      o.x += a.x; o.y += a.y; o.z += a.z; o.w += a.w;
-    }
-    *reinterpret_cast<float4*>(part_o + pr * HD + d4 * 4) = o;
+    const float4 o = *reinterpret_cast<const float4*>(&s_o[0][r][d4 * 4]), o1 = *reinterpret_cast<const float4*>(&s_o[1][r][d4 * 4]);
+    *reinterpret_cast<float4*>(part_o + pr * HD + d4 * 4) = make_float4(o.x + o1.x, o.y + o1.y, o.z + o1.z, o.w + o1.w);
     if (d4 == 0) {
       float m_all = -INFINITY, l = 0.f;
 #pragma unroll
@@ -597,45 +682,302 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, float2 (*s_ml)[64]
   }
 }
 
-template <int HD, int RBP, int RBO>
-__global__ __launch_bounds__(512, 2) void group_attn_keys_kernel(const bf16_t* __restrict__ q, const bf16_t* __restrict__ pool, SeqGeom geo, GroupArgs ga,
+// ---- bf16, head dim 64 or 128: tiles of 128 query rows of the prefix part -----------------------------------------------------
+// Four wavefronts of 32 rows, the pages staged in an LDS ring that all four read (a stage is a pair of pages: K of page A, of page B, V of A, of B; every
+// wavefront copies a quarter), one barrier a stage, two workgroups a CU.  32x32x16 MFMAs: S^T = K . Q^T leaves a lane 16 of the pair's keys (quartets h and h + 2
+// of either page, h = lane / 32) of query column lane % 32, and O^T += V^T . P^T takes them as they are.
+// Three stages of the sweep are in work at once, independent of each other: scores of pair i + 2, softmax of pair i + 1, products of pair i.  Matrix and vector
+// instructions of one wavefront then run side by side, and the other workgroup's fill what is left.
+// PLANES = 2: probabilities as a hi + lo bf16 pair (~16 bits, as everywhere in the bf16 model).  PLANES = 1: rounded to bf16 once, for rows that leave in
+// bf16 themselves: the weights' error of 2^-9 each, averaged over the keys, lies below the output's own rounding, and a third of the matrix work is gone.
+template <int HD>
+struct TileSweep {
+  static constexpr int KT = HD / 16, MT = HD / 32, NS = 5;
+  static constexpr int PART = DF_PAGE * HD * 2, NI = PART / 1024, STAGE = 4 * PART, BYTES = NS * STAGE;   // PART: K or V of a page, NI copies of 1 KB
+};
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+
+template <int HD, int PLANES>
+__device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w, int kvh, const bf16_t* __restrict__ q, const bf16_t* __restrict__ pool,
+                                                 const SeqGeom& geo, const GroupArgs& ga, float* __restrict__ part_o, float2* __restrict__ part_ml) {
+  typedef TileSweep<HD> C;
+  constexpr int KT = C::KT, MT = C::MT, NS = C::NS, PART = C::PART, NI = C::NI, STAGE = C::STAGE;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  const int group = ga.n_q_heads / ga.n_kv_heads, n_pairs = (w.c1 - w.c0 + 31) >> 5, page0 = w.c0 / DF_PAGE;
+  const int row = w.row0 + min(wave * 32 + n, w.n_rows - 1), rs = row / ga.rows, rat = row % ga.rows;   // a row that is not there reads along and is not stored
+  const size_t out_row = (size_t)(rs * geo.block_size + rat / group) * ga.n_q_heads + kvh * group + rat % group;
+  auto load_ids = [&](int p0) { return w.table[min(page0 + 2 * p0 + lane, geo.max_pages_per_seq - 1)]; };   // 32 pairs' page ids
+  int ids = load_ids(0), ids_next = n_pairs > 32 ? load_ids(32) : 0;
+  u32x4 qf[KT];   // dims 16 kt + 8 h .. + 7 of the lane's row
+  {
+    const u32x4* qp = reinterpret_cast<const u32x4*>(q + out_row * HD);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) qf[kt] = qp[kt * 2 + h];
+  }
+  const bool live = wave * 32 < w.n_rows;   // a wavefront without rows copies its quarters
+  const bool half_pair = (w.c1 - w.c0) & DF_PAGE;   // the last pair has no page B: page A in its place, and its keys weigh nothing
+  const unsigned lds = (unsigned)(size_t)s_raw + (unsigned)((wave & 1) * 2 + (wave >> 1)) * PART, voff = lane * 16;
+  const size_t page_elems = (size_t)ga.n_kv_heads * 2 * DF_PAGE * HD;
+  const bf16_t* mine = pool + kv_head_base(ga.layer, geo.n_pages, 0, ga.n_kv_heads, kvh, HD) + (size_t)(wave & 1) * DF_PAGE * HD;
+  int fetch_slot = 0;
+  // this wavefront's quarter of a stage: the K or V half (wave & 1) of page A or B (wave >> 1); past the end the last stage again, into a slot that nobody reads.
+  // The pages of a prefix are all there (group_plan_kernel)
+  auto fetch = [&](int st) {
+    const int real = min(st, n_pairs - 1), at = (real & 31) * 2 + (half_pair && real == n_pairs - 1 ? 0 : wave >> 1);
+    const bf16_t* src = mine + (size_t)__builtin_amdgcn_readlane(ids, at) * page_elems;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const unsigned dst = __builtin_amdgcn_readfirstlane(lds + (unsigned)(fetch_slot * STAGE + i * 1024));
+      const bf16_t* from = src + i * 512;
+      unsigned keep_m0;   // whatever the compiler keeps in m0 is put back
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_nop 0\n\ts_mov_b32 m0, %0"
+                   : "=&s"(keep_m0) : "s"(dst), "v"(voff), "s"(from) : "memory");
+    }
+    fetch_slot = fetch_slot + 1 == NS ? 0 : fetch_slot + 1;
+  };
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) asm volatile("" : "+v"(qf[kt]));   // waited for here: inside the loop that would be a wait for every copy
+  asm volatile("" : "+v"(ids_next));
+  for (int st = 0; st < NS - 1; ++st) fetch(st);
+
+  float m_run = -INFINITY, neg_m = 0.f, l_run = 0.f;
+  f32x16 acc[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) acc[mt] = (f32x16){};
+  const float scale2 = ga.scale * 1.44269504088896341f;   // base-2 exponents
+  struct P { u32x4 v[PLANES][2]; };   // probabilities of page A's and page B's keys
+  P p0, p1;
+  f32x16 s0, s1;
+
+  auto ready = [&]() {   // all stages but the youngest have landed, and everybody is done with the oldest
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NI) : "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto read_k = [&](u32x4 (&kf)[KT], int slot) {
+    const u32x4* kp = reinterpret_cast<const u32x4*>(s_raw + slot * STAGE + (n >> 4) * PART) + h * 16 + (n & 15);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) kf[kt] = kp[kt * 32];
+  };
+  auto read_v = [&](u32x4 (&vf)[2][MT], int slot) {
+    const uint2* vp = reinterpret_cast<const uint2*>(s_raw + slot * STAGE + 2 * PART) + (n >> 4) * 64 + h * 16 + (n & 15);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint2 x = vp[mt * 128 + b * (PART / 8)], y = vp[mt * 128 + b * (PART / 8) + 32];   // quartets h and h + 2
+        vf[b][mt] = (u32x4){x.x, x.y, y.x, y.y};
+      }
+  };
+  auto qk = [&](f32x16& s, const u32x4& k, int kt) {
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[kt]), s, 0, 0, 0);
+  };
+  auto pv = [&](const u32x4& v, const u32x4& p, int mt) {
+    acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), acc[mt], 0, 0, 0);
+  };
+  // Lazy reference maximum: it moves only when a row's has grown by more than 8 (in powers of two), decided from each lane's own scores, so the accumulators
+  // are rescaled once or twice a sweep.  Maxima are rounded up to whole numbers: the factor for what is there already is a power of two, which the probabilities
+  // on their way to the products take exactly.  (maximum, not fmax: NaN passes through, which the latter would buy with an instruction a score.)
+  auto raise = [&](const f32x16& s, P& p) {
+    const float a = max3(max3(s[0], s[1], s[2]), s[3], s[4]), b = max3(max3(s[5], s[6], s[7]), s[8], s[9]), c = max3(max3(s[10], s[11], s[12]), s[13], s[14]);
+    const float lmx = max3(max3(a, b, c), s[15], s[15]) * scale2;
+    if (__builtin_amdgcn_ballot_w64(lmx > m_run + 8.f) != 0ull) {
+      const LanePair x = lane_swap32(lmx, lmx);
+      const float mx = ceilf(fmaxf(x.lo, x.hi));
+      const bool grow = mx > m_run + 8.f;
+      const float corr = grow ? (m_run == -INFINITY ? 0.f : exp2f(m_run - mx)) : 1.f;
+      l_run *= corr;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) acc[mt] *= corr;
+#pragma unroll
+      for (int pl = 0; pl < PLANES; ++pl)
+#pragma unroll
+        for (int b2 = 0; b2 < 2; ++b2)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t v = p.v[pl][b2][i];
+            p.v[pl][b2][i] = pack_bf16_pair(__uint_as_float(v << 16) * corr, __uint_as_float(v & 0xFFFF0000u) * corr);
+          }
+      if (grow) { m_run = mx; neg_m = -mx; }
+    }
+  };
+  auto soft = [&](const f32x16& s, P& p) {
+    float e[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, neg_m));
+    l_run += (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]))) + (((e[8] + e[9]) + (e[10] + e[11])) + ((e[12] + e[13]) + (e[14] + e[15])));
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = e[8 * b + 2 * i], y = e[8 * b + 2 * i + 1];
+        const uint32_t v = pack_bf16_pair(x, y);
+        p.v[0][b][i] = v;
+        if constexpr (PLANES == 2) p.v[1][b][i] = pack_bf16_pair(x - __uint_as_float(v << 16), y - __uint_as_float(v & 0xFFFF0000u));
+      }
+  };
+  auto scores = [&](f32x16& s, int slot) {
+    u32x4 kf[KT];
+    read_k(kf, slot);
+    s = (f32x16){};
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) qk(s, kf[kt], kt);
+  };
+  auto without_b = [&](f32x16& s) {
+#pragma unroll
+    for (int i = 8; i < 16; ++i) s[i] = -INFINITY;
+  };
+
+  ready();   // stages 0, 1 and 2
+  if (live) {
+    scores(s0, 0);
+    if (half_pair && n_pairs == 1) without_b(s0);
+    P none{};
+    raise(s0, none);
+    soft(s0, p0);
+    if (n_pairs > 1) scores(s1, 1);
+  }
+  int slot = 0;   // of stage i
+  auto step = [&](P& p, const f32x16& s, P& pn, f32x16& sn) {   // products with p, softmax of s into pn, scores into sn
+    if (live) {
+      raise(s, p);
+      u32x4 kf[KT], vf[2][MT];
+      __builtin_amdgcn_sched_barrier(0);
+      read_v(vf, slot);
+      read_k(kf, slot + 2 >= NS ? slot + 2 - NS : slot + 2);
+      sn = (f32x16){};
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {   // KT = 2 MT: the chain of the scores between products that do not wait for each other
+#pragma unroll
+        for (int j = 0; j < PLANES; ++j) {
+          const int at = kt * PLANES + j;
+          pv(vf[at / MT % 2][at % MT], p.v[at / (2 * MT)][at / MT % 2], at % MT);
+        }
+        qk(sn, kf[kt], kt);
+      }
+      soft(s, pn);
+      if constexpr (PLANES == 1) {   // a matrix instruction and four vector ones in turn (128 pairs a workgroup: 187 us as the compiler orders them, 174 so; two planes 225 and 231)
+#pragma unroll
+        for (int j = 0; j < 2 * KT; ++j) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x402, 4, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    slot = slot + 1 == NS ? 0 : slot + 1;
+  };
+  auto turn = [&](int i) {   // stage i + 2 is there; stage i + 4 goes where stage i - 1 was
+    ready();
+    const int ahead = i + NS - 1;
+    if ((ahead & 31) == 0 && ahead < n_pairs) {   // uniform: the next set of page ids comes into use
+      ids = ids_next;
+      if (ahead + 32 < n_pairs) ids_next = load_ids(ahead + 32);
+      asm volatile("" : "+v"(ids_next));
+    }
+    fetch(ahead);
+  };
+  int i = 0;
+  for (; i + 3 < n_pairs; i += 2) {
+    turn(i);
+    step(p0, s1, p1, s0);
+    turn(i + 1);
+    step(p1, s0, p0, s1);
+  }
+  if (i + 2 < n_pairs) {
+    turn(i);
+    step(p0, s1, p1, s0);
+    ++i;
+    p0 = p1;
+    s1 = s0;
+  }
+  ready();
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may still be on its way into LDS when the workgroup ends
+  if (!live) return;
+  auto last = [&](const P& p, bool cut) {
+    u32x4 vf[2][MT];
+    read_v(vf, slot);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      if (cut) vf[1][mt] = (u32x4){0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int pl = 0; pl < PLANES; ++pl) pv(vf[b][mt], p.v[pl][b], mt);
+    }
+    slot = slot + 1 == NS ? 0 : slot + 1;
+  };
+  if (i + 1 < n_pairs) {
+    if (half_pair) without_b(s1);
+    raise(s1, p0);
+    soft(s1, p1);
+    last(p0, false);
+    p0 = p1;
+  }
+  last(p0, half_pair);
+  const LanePair l = lane_swap32(l_run, l_run);
+  if (wave * 32 + n >= w.n_rows) return;
+  const size_t pr = out_row * (ga.prefix_splits + ga.own_splits) + w.part;
+  if (h == 0) part_ml[pr] = make_float2(m_run, l.lo + l.hi);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<float4*>(part_o + pr * HD + mt * 32 + 8 * j + 4 * h) = make_float4(acc[mt][4 * j], acc[mt][4 * j + 1], acc[mt][4 * j + 2], acc[mt][4 * j + 3]);
+}
+
+// PLANES > 0: the prefix part by tiles of 128 rows; 0: by key-split workgroups of RBP blocks of 16 rows.  RBO: row blocks of an own part's workgroup.
+template <int HD, int PLANES, int RBP, int RBO>
+__global__ __launch_bounds__(256, 2) void group_attn_mfma_kernel(const bf16_t* __restrict__ q, const bf16_t* __restrict__ pool, SeqGeom geo, GroupArgs ga,
                                                                  GroupTables gt, float* __restrict__ part_o, float2* __restrict__ part_ml) {
-  constexpr int RB = RBP > RBO ? RBP : RBO;
-  __shared__ __attribute__((aligned(1024))) char s_raw[KeySplit<HD>::bytes(RB)];
-  __shared__ float2 s_ml[8][64];
+  constexpr int P_BYTES = PLANES ? TileSweep<HD>::BYTES : KeySplit<HD>::bytes(RBP), O_BYTES = KeySplit<HD>::bytes(RBO);
+  __shared__ __attribute__((aligned(1024))) char s_raw[P_BYTES > O_BYTES ? P_BYTES : O_BYTES];
+  static_assert(sizeof(s_raw) <= 80 * 1024, "two workgroups a CU");
   GroupWork w;
   int kvh;
-  if (!group_work(w, kvh, geo, ga, gt)) return;
-  if (w.part < ga.prefix_splits) group_sweep_keys<HD, RBP>(s_raw, s_ml, w, kvh, q, pool, geo, ga, part_o, part_ml);
-  else group_sweep_keys<HD, RBO>(s_raw, s_ml, w, kvh, q, pool, geo, ga, part_o, part_ml);
+  if (!group_work<256>(w, kvh, geo, ga, gt, part_ml)) return;
+  if (w.part >= ga.prefix_splits) return group_sweep_keys<HD, RBO>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
+  if constexpr (PLANES > 0) group_sweep_tile<HD, PLANES>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
+  else group_sweep_keys<HD, RBP>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
 }
 
 // Parts -> rows, a wavefront a row, two dims a lane.  A part without keys (its sum is exactly 0) is left out.  OPERAND: GEMM activation operand (Act<T>), else
 // plain rows of the model's type.
 template <typename T, bool OPERAND>
 __global__ __launch_bounds__(256) void group_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, T* __restrict__ out, GroupArgs ga,
-                                                          const int32_t* __restrict__ first, int hd, int block, int n_rows) {
+                                                          int hd, int n_rows) {
   const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // m * n_q_heads + hq
   if (row >= n_rows) return;
   const int parts = ga.prefix_splits + ga.own_splits, m = row / ga.n_q_heads, hq = row % ga.n_q_heads;
-  const int from = first[m / block] > 0 ? 0 : ga.prefix_splits;   // nothing in common: the prefix part was not computed
-  const float2 ml = lane >= from && lane < parts ? part_ml[(size_t)row * parts + lane] : make_float2(-INFINITY, 0.f);
+  const float2 ml = lane < parts ? part_ml[(size_t)row * parts + lane] : make_float2(-INFINITY, 0.f);
   const bool some = ml.y != 0.f;
   const float mx = wave_reduce_max(some ? ml.x : -INFINITY);
   const float wgt = some ? __builtin_amdgcn_exp2f(ml.x - (mx == -INFINITY ? 0.f : mx)) : 0.f;
-  const unsigned long long live = __ballot(some);
   const float* po = part_o + (size_t)row * parts * hd + 2 * lane;
   float L = 0.f;
   float2 o = make_float2(0.f, 0.f);
   const bool mine = 2 * lane < hd;
-  for (int i = from; i < parts; ++i)
-    if (live >> i & 1) {
-      const float w = lane_value(wgt, i);
-      L += w * lane_value(ml.y, i);
-      const float2 x = mine ? *reinterpret_cast<const float2*>(po + (size_t)i * hd) : make_float2(0.f, 0.f);
-      o.x += w * x.x;
-      o.y += w * x.y;
+  unsigned long long live = __ballot(some);
+  while (live) {   // four parts' rows on their way together, in ascending order in the sums
+    int at[4];
+    float2 x[4];
+    const int n = min(4, (int)__popcll(live));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      at[u] = u < n ? __ffsll(live) - 1 : at[0];
+      if (u < n) live &= live - 1;
+      x[u] = mine ? *reinterpret_cast<const float2*>(po + (size_t)at[u] * hd) : make_float2(0.f, 0.f);
     }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (u < n) {
+        const float w = lane_value(wgt, at[u]);
+        L += w * lane_value(ml.y, at[u]);
+        o.x += w * x[u].x;
+        o.y += w * x[u].y;
+      }
+  }
   if (!mine) return;
   const float by = L != 0.f ? L : INFINITY;   // no visible key: zeros
   o.x /= by;
@@ -650,30 +992,41 @@ __global__ __launch_bounds__(256) void group_merge_kernel(const float* __restric
   }
 }
 
+// whether the prefix part goes by tiles of 128 rows: the groups have more rows, on average, than a key-split workgroup
+inline bool group_by_tiles(bool bf16, int hd, int n_seqs, int rows, int n_groups) {
+  return bf16 && (hd == 128 || hd == 64) && (long long)n_seqs * rows > (long long)n_groups * kOwnTile;
+}
+
+// plain: the rows leave in the model's type (one plane of probabilities is enough)
 template <typename T>
 inline void group_attn_launch(hipStream_t st, const T* q, const T* pool, const SeqGeom& geo, const GroupArgs& ga, int hd, const GroupTables& gt, float* part_o,
-                              float2* part_ml) {
+                              float2* part_ml, bool plain) {
   const dim3 grid((ga.max_tiles * ga.prefix_splits + ga.n_seqs * ga.own_tiles * ga.own_splits) * ga.n_kv_heads), block(256);
   if constexpr (sizeof(T) == 2) {
     const bool few = ga.rows <= 16, few_all = (long long)ga.n_seqs * ga.rows <= 16;
-    auto keys = [&](auto c) {
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, q, pool, geo, ga, gt, part_o, part_ml); };
+    auto mfma = [&](auto c) {
       constexpr int HD = decltype(c)::value;
-      if (few_all) hipLaunchKernelGGL((group_attn_keys_kernel<HD, 1, 1>), grid, dim3(512), 0, st, q, pool, geo, ga, gt, part_o, part_ml);
-      else if (few) hipLaunchKernelGGL((group_attn_keys_kernel<HD, 4, 1>), grid, dim3(512), 0, st, q, pool, geo, ga, gt, part_o, part_ml);
-      else hipLaunchKernelGGL((group_attn_keys_kernel<HD, 4, 4>), grid, dim3(512), 0, st, q, pool, geo, ga, gt, part_o, part_ml);
+      if (ga.tile > kOwnTile && plain) few ? launch(group_attn_mfma_kernel<HD, 1, 0, 1>) : launch(group_attn_mfma_kernel<HD, 1, 0, 4>);
+      else if (ga.tile > kOwnTile) few ? launch(group_attn_mfma_kernel<HD, 2, 0, 1>) : launch(group_attn_mfma_kernel<HD, 2, 0, 4>);
+      else if (few_all) launch(group_attn_mfma_kernel<HD, 0, 1, 1>);
+      else few ? launch(group_attn_mfma_kernel<HD, 0, 4, 1>) : launch(group_attn_mfma_kernel<HD, 0, 4, 4>);
     };
-    if (hd == 128) return keys(std::integral_constant<int, 128>{});
-    if (hd == 64) return keys(std::integral_constant<int, 64>{});
+    if (hd == 128) return mfma(std::integral_constant<int, 128>{});
+    if (hd == 64) return mfma(std::integral_constant<int, 64>{});
   }
   auto go = [&](auto c) { hipLaunchKernelGGL((group_attn_kernel<T, decltype(c)::value>), grid, block, 0, st, q, pool, geo, ga, gt, part_o, part_ml); };
   switch (hd) {
     case 16: return go(std::integral_constant<int, 16>{});
     case 32: return go(std::integral_constant<int, 32>{});
     case 48: return go(std::integral_constant<int, 48>{});
-    case 64: return go(std::integral_constant<int, 64>{});
     case 80: return go(std::integral_constant<int, 80>{});
     case 96: return go(std::integral_constant<int, 96>{});
     case 112: return go(std::integral_constant<int, 112>{});
-    default: return go(std::integral_constant<int, 128>{});
+    default: break;
+  }
+  if constexpr (sizeof(T) == 4) {
+    if (hd == 64) return go(std::integral_constant<int, 64>{});
+    go(std::integral_constant<int, 128>{});
   }
 }

@@ -163,15 +163,16 @@ inline int attn_q_shift(const dflash_dims& m, int block_size) {
 
 // launch shape of the attention of S sequences that share pages
 struct GroupShape {
-  int rows, tiles, own_tiles;
+  int rows, tile, tiles, own_tiles;
   GroupSplits splits;
 };
 inline GroupShape group_shape(const dflash_dims& m, int S, int block_size, int n_groups, int prefix_tokens, int own_tokens) {
   GroupShape g;
   g.rows = block_size * (m.n_q_heads / m.n_kv_heads);
-  g.tiles = group_tile_slots(S, g.rows, n_groups);
-  g.own_tiles = (g.rows + kGroupTile - 1) / kGroupTile;
-  g.splits = group_plan(g.tiles, S, g.own_tiles, m.n_kv_heads, prefix_tokens, own_tokens);
+  g.tile = group_by_tiles(m.dtype == DFLASH_BF16, m.head_dim, S, g.rows, n_groups) ? 128 : kOwnTile;
+  g.tiles = group_tile_slots(S, g.rows, g.tile, n_groups);
+  g.own_tiles = (g.rows + kOwnTile - 1) / kOwnTile;
+  g.splits = group_plan((int)((long long)S * g.rows + g.tile - 1) / g.tile, S, g.own_tiles, m.n_kv_heads, prefix_tokens, own_tokens);
   return g;
 }
 
@@ -204,7 +205,7 @@ inline size_t arrive_counters(size_t D) { return std::max<size_t>(1, D / 64); }
 
 struct Workspace {
   size_t status, arena, h, a, q, o, act, taps, fuse, ht, logits_d, logits_t, part_o, part_ml, stats_p, stats_q, amax, lsep, rope_t, rope_d, ssq, arrive, pf_lens, pf_plens, pf_table, pf_tokens, pf_end_row, pf_end_seq, pf_first, pf_anchor, pf_tiles, total;
-  size_t grp_tiles, grp_first, pg_copies, pg_wants, pg_ids, pg_head;   // sequences that share pages: the groups' tables, the ledger's scratch
+  size_t grp_tiles, grp_seqs, grp_common, pg_copies, pg_wants, pg_ids, pg_head;   // sequences that share pages: the groups' tables, the ledger's scratch
   size_t moe_sel_e, moe_sel_w, moe_sel_pos, moe_row_of, moe_items, moe_a, moe_act, moe_y;   // routed-expert target only
 };
 Workspace workspace_layout(const dflash_dims& t, const dflash_dims& d, const dflash_runtime& rt, const Knobs& kn) {
@@ -272,8 +273,9 @@ Workspace workspace_layout(const dflash_dims& t, const dflash_dims& d, const dfl
   w.pf_first = take((size_t)rt.max_seqs * 4);
   w.pf_anchor = take((size_t)rt.max_seqs * 4);
   w.pf_tiles = take((size_t)rt.max_seqs * 16);
-  w.grp_tiles = take(((size_t)group_tile_slots(rt.max_seqs, rt.block_size * std::max(t.n_q_heads / t.n_kv_heads, d.n_q_heads / d.n_kv_heads), rt.max_seqs) + 1) * 16);
-  w.grp_first = take((size_t)rt.max_seqs * 4);
+  w.grp_tiles = take(((size_t)group_tile_slots(rt.max_seqs, rt.block_size * std::max(t.n_q_heads / t.n_kv_heads, d.n_q_heads / d.n_kv_heads), kOwnTile, rt.max_seqs) + 1) * 16);
+  w.grp_seqs = take((size_t)rt.max_seqs * 8);
+  w.grp_common = take((size_t)rt.max_seqs * 4);
   const size_t half = (size_t)rt.n_pages / 2 + 1;   // pages that a compaction moves, at most
   w.pg_copies = take(std::max<size_t>(kReserveRows * 16, half * 8));
   w.pg_wants = take(((size_t)std::min(rt.max_seqs, kReserveRows) * rt.max_pages_per_seq / 64 + 16) * 8);
@@ -551,12 +553,12 @@ struct Engine {
   void attention(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, bool causal);
 
   // ---- sequences that share pages (attn_group.h): the groups' tables, once a pass, and a layer's attention
-  GroupTables group_tables() { return GroupTables{ws<int4>(c->ws.grp_tiles), ws<int32_t>(c->ws.grp_first)}; }
+  GroupTables group_tables() { return GroupTables{ws<int4>(c->ws.grp_tiles), ws<int2>(c->ws.grp_seqs), ws<int32_t>(c->ws.grp_common)}; }
   void group_tables_of(const dflash_dims& m, const dflash_batch* b, const dflash_groups& g, int block) {
     SeqGeom geo = geom(b);
     geo.block_size = block;
-    hipLaunchKernelGGL(group_plan_kernel, dim3(g.n_groups), dim3(1024), 0, st, geo, g.group_starts, g.n_groups, b->n_seqs,
-                       block * (m.n_q_heads / m.n_kv_heads), group_tables());
+    const GroupShape sh = group_shape(m, b->n_seqs, block, g.n_groups, 0, 0);
+    hipLaunchKernelGGL(group_plan_kernel, dim3(b->n_seqs), dim3(256), 0, st, geo, g.group_starts, g.n_groups, b->n_seqs, sh.rows, sh.tile, group_tables());
     check();
   }
   // of the q rows; `out` rows as GEMM operand or plain
@@ -565,7 +567,7 @@ struct Engine {
     const int S = b->n_seqs;
     const int most = c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE, expected = std::min(g.prefix_len, most);
     const GroupShape sh = group_shape(m, S, block, g.n_groups, expected, std::min(std::max(0, b->max_seq_len - expected) + block, most));
-    GroupArgs ga{m.n_q_heads, m.n_kv_heads, layer, causal, S, sh.rows, sh.tiles, sh.own_tiles, sh.splits.prefix, sh.splits.own, 1.0f / sqrtf((float)m.head_dim)};
+    GroupArgs ga{m.n_q_heads, m.n_kv_heads, layer, causal, S, sh.rows, sh.tile, sh.tiles, sh.own_tiles, sh.splits.prefix, sh.splits.own, 1.0f / sqrtf((float)m.head_dim)};
     SeqGeom geo = geom(b);
     geo.block_size = block;
     const int n_rows = S * block * m.n_q_heads;
@@ -573,17 +575,15 @@ struct Engine {
       // algorithmic bytes: what is shared once, as the caller expects it, the rest per sequence
       const double tokens = (double)g.n_groups * expected + (double)S * (std::max(0, b->max_seq_len - expected) + block);
       ProfScope prof(c, st, DFLASH_PROF_ATTN, tokens * 2 * m.n_kv_heads * m.head_dim * sizeof(T));
-      group_attn_launch<T>(st, q, pool, geo, ga, m.head_dim, group_tables(), ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml));
+      group_attn_launch<T>(st, q, pool, geo, ga, m.head_dim, group_tables(), ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), !operand);
       check();
     }
     ProfScope prof(c, st, DFLASH_PROF_ATTN_MERGE, 0.0);
     const dim3 grid((n_rows + 3) / 4), threads(256);
     if (operand)
-      hipLaunchKernelGGL((group_merge_kernel<T, true>), grid, threads, 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), out, ga, group_tables().first,
-                         m.head_dim, block, n_rows);
+      hipLaunchKernelGGL((group_merge_kernel<T, true>), grid, threads, 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), out, ga, m.head_dim, n_rows);
     else
-      hipLaunchKernelGGL((group_merge_kernel<T, false>), grid, threads, 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), out, ga, group_tables().first,
-                         m.head_dim, block, n_rows);
+      hipLaunchKernelGGL((group_merge_kernel<T, false>), grid, threads, 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), out, ga, m.head_dim, n_rows);
     check();
   }
   int attend(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, const dflash_groups& g, int rows, bool causal, const void* q, void* out) {

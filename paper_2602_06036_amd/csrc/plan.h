@@ -115,7 +115,7 @@ inline bool attention_by_tiles(int tiles, int blocks, int head_groups, int cache
 struct GroupSplits {
   int prefix, own;
 };
-inline int group_splits(int wgs, int tokens) { return std::max(1, std::min({256 / std::max(1, wgs), (tokens + 127) / 128, 32})); }
+inline int group_splits(int wgs, int tokens) { return std::max(1, std::min({512 / std::max(1, wgs), (tokens + 255) / 256, 32})); }
 // tiles, own_tiles: workgroups of a kv head in all and of a sequence; prefix and own tokens as the caller expects them
 inline GroupSplits group_plan(int tiles, int n_seqs, int own_tiles, int n_kv_heads, int prefix_tokens, int own_tokens) {
   return {group_splits(tiles * n_kv_heads, prefix_tokens), group_splits(n_seqs * own_tiles * n_kv_heads, own_tokens)};

@@ -23,10 +23,10 @@ def unpack(pool, layer, heads, hd):
 
 def attention64(q, k, v, table, lens, causal, n_pages):
     """q [S, R, Hq, hd]; k, v [page, key, Hkv, hd], all float64 on the CPU.  (outputs, error that the kernels' fp32 sums may add per row of bf16 or fp32
-    inputs).  Keys on entries outside the pool are not there; a row without keys is zeros."""
+    inputs, averages of |v| with the rows' weights).  Keys on entries outside the pool are not there; a row without keys is zeros."""
     S, R, Hq, hd = q.shape
     Hkv = k.shape[2]
-    out, slack = torch.zeros_like(q), torch.zeros(S, R, Hq, 1, dtype=torch.float64)
+    out, slack, wabs = torch.zeros_like(q), torch.zeros(S, R, Hq, 1, dtype=torch.float64), torch.zeros_like(q)
     for s in range(S):
         n = min(int(lens[s]) + R, table.shape[1] * PAGE)
         pos = np.arange(n)
@@ -41,18 +41,26 @@ def attention64(q, k, v, table, lens, causal, n_pages):
                 K, V = k[ids[see], at % PAGE, h * Hkv // Hq], v[ids[see], at % PAGE, h * Hkv // Hq]
                 x = K @ q[s, j, h] / hd ** 0.5
                 out[s, j, h] = torch.softmax(x, 0) @ V
+                wabs[s, j, h] = torch.softmax(x, 0) @ V.abs()
                 # hd products and a sum in fp32 for a score, the scale's rounding and that of the exponent's argument; a score off by d moves the row by at
                 # most 2 d max|v|; as many additions as keys and parts in the two sums
                 score = (hd + 8) * 2.0 ** -24 * float((K.abs() @ q[s, j, h].abs()).max() / hd ** 0.5 + x.abs().max())
                 slack[s, j, h] = float(V.abs().max()) * (2 * score + 2 * (len(at) + 64) * 2.0 ** -24)
-    return out, slack
+    return out, slack, wabs
 
 
-def allowed(ref, slack, vmax, dtype):
-    """bf16: the probabilities' pair of bf16 numbers (2^-16 of the weights, in numerator alone) and the output's rounding."""
+def by_tiles(hd, rows, n_seqs, n_groups):
+    """Whether the prefix part of a bf16 model goes by tiles of 128 rows (rows: query rows of a sequence and kv head)."""
+    return hd in (64, 128) and n_seqs * rows > 64 * n_groups
+
+
+def allowed(ref, slack, wabs, dtype, one_plane):
+    """bf16: the output's rounding, and that of the probabilities.  As a hi + lo pair of bf16 numbers: hi is off by at most 2^-8 of the value, lo by 2^-8 of that,
+    2^-16 of every weight.  one_plane (rows that leave in bf16 by tiles): every weight w_i is off by at most 2^-8 w_i in the numerator and exact in the sum, so the
+    row by at most 2^-8 sum w_i |v_i| = 2^-8 wabs."""
     if dtype == "f32":
         return slack + 2.0 ** -23 * ref.abs()
-    return slack + 2.0 ** -16 * vmax + 2.0 ** -8 * ref.abs()
+    return slack + (2.0 ** -8 if one_plane else 2.0 ** -16) * wabs + 2.0 ** -8 * ref.abs()
 
 
 class LedgerModel:
