@@ -401,9 +401,10 @@ struct KeySplit {
   static constexpr int KT = HD / 32, DT = HD / 16, NW = 4, LD = HD + 4;
   static constexpr int PART = DF_PAGE * HD * 2, NI = PART / 1024;   // bytes of the K or V part of a page, load instructions for it
   static constexpr int RING = NW * 4 * PART;                        // per wavefront: K of page A, of page B, V of page A, of page B
-  // ring and queries; in the end two wavefronts' rows from the start and all wavefronts' maxima and sums behind them
+  // ring and queries; in the end two wavefronts' rows from the start and all wavefronts' maxima and sums behind them, then the rows' places
   static constexpr int OUT(int rb) { return 2 * rb * 16 * LD * 4; }
-  static constexpr int bytes(int rb) { return RING + rb * KT * 1024 > OUT(rb) + NW * rb * 16 * 8 ? RING + rb * KT * 1024 : OUT(rb) + NW * rb * 16 * 8; }
+  static constexpr int ROWS_AT(int rb) { return OUT(rb) + NW * rb * 16 * 8; }
+  static constexpr int bytes(int rb) { return RING + rb * KT * 1024 > ROWS_AT(rb) + rb * 16 * 4 ? RING + rb * KT * 1024 : ROWS_AT(rb) + rb * 16 * 4; }
 };
 
 template <int HD, int RB>
@@ -627,6 +628,11 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
 
   // ---- the wavefronts' parts together: the upper two hand theirs to the lower two, then all rows leave
   __syncthreads();   // every wavefront is done with the ring and the queries
+  int* s_row = reinterpret_cast<int*>(s_raw + C::ROWS_AT(RB));   // the rows' places among the query rows of all heads: divisions once a row
+  if ((int)threadIdx.x < w.n_rows) {
+    const int row = w.row0 + threadIdx.x, at = row % ga.rows;
+    s_row[threadIdx.x] = (row / ga.rows * geo.block_size + at / group) * ga.n_q_heads + kvh * group + at % group;
+  }
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const float l = quarter_sum(l_run[rb]);
@@ -663,9 +669,8 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
   __syncthreads();
   const int parts = ga.prefix_splits + ga.own_splits;
   for (int i = threadIdx.x; i < w.n_rows * (HD / 4); i += 64 * NW) {
-    const int r = i / (HD / 4), d4 = i % (HD / 4), row = w.row0 + r;
-    const int s = row / ga.rows, at = row % ga.rows;
-    const size_t pr = ((size_t)(s * geo.block_size + at / group) * ga.n_q_heads + kvh * group + at % group) * parts + w.part;
+    const int r = i / (HD / 4), d4 = i % (HD / 4);
+    const size_t pr = (size_t)s_row[r] * parts + w.part;
     const float4 o = *reinterpret_cast<const float4*>(&s_o[0][r][d4 * 4]), o1 = *reinterpret_cast<const float4*>(&s_o[1][r][d4 * 4]);
     *reinterpret_cast<float4*>(part_o + pr * HD + d4 * 4) = make_float4(o.x + o1.x, o.y + o1.y, o.z + o1.z, o.w + o1.w);
     if (d4 == 0) {
@@ -942,53 +947,52 @@ __global__ __launch_bounds__(256, 2) void group_attn_mfma_kernel(const bf16_t* _
   else group_sweep_keys<HD, RBP>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
 }
 
-// Parts -> rows, a wavefront a row, two dims a lane.  A part without keys (its sum is exactly 0) is left out.  OPERAND: GEMM activation operand (Act<T>), else
-// plain rows of the model's type.
+// Parts -> rows, a wavefront a row, four dims a lane, as many parts side by side as that leaves room for (two of 128 dims) and four times that on their way.  A part
+// without keys (its sum is exactly 0) is left out.  OPERAND: GEMM activation operand (Act<T>), else plain rows of the model's type.
 template <typename T, bool OPERAND>
 __global__ __launch_bounds__(256) void group_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, T* __restrict__ out, GroupArgs ga,
                                                           int hd, int n_rows) {
   const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // m * n_q_heads + hq
   if (row >= n_rows) return;
   const int parts = ga.prefix_splits + ga.own_splits, m = row / ga.n_q_heads, hq = row % ga.n_q_heads;
+  const int width = hd > 64 ? 32 : hd > 32 ? 16 : 8, beside = 64 / width, sub = lane / width, d = lane % width * 4;   // lanes of a part, parts side by side
   const float2 ml = lane < parts ? part_ml[(size_t)row * parts + lane] : make_float2(-INFINITY, 0.f);
-  const bool some = ml.y != 0.f;
+  const bool some = ml.y != 0.f, mine = d < hd;
   const float mx = wave_reduce_max(some ? ml.x : -INFINITY);
   const float wgt = some ? __builtin_amdgcn_exp2f(ml.x - (mx == -INFINITY ? 0.f : mx)) : 0.f;
-  const float* po = part_o + (size_t)row * parts * hd + 2 * lane;
-  float L = 0.f;
-  float2 o = make_float2(0.f, 0.f);
-  const bool mine = 2 * lane < hd;
-  unsigned long long live = __ballot(some);
-  while (live) {   // four parts' rows on their way together, in ascending order in the sums
-    int at[4];
-    float2 x[4];
-    const int n = min(4, (int)__popcll(live));
+  const float L = wave_reduce_sum(some ? wgt * ml.y : 0.f);
+  const unsigned long long live = __ballot(some);
+  const float* po = part_o + (size_t)row * parts * hd + d;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p0 = 0; p0 < parts; p0 += 4 * beside) {
+    float4 x[4];
+    bool on[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      at[u] = u < n ? __ffsll(live) - 1 : at[0];
-      if (u < n) live &= live - 1;
-      x[u] = mine ? *reinterpret_cast<const float2*>(po + (size_t)at[u] * hd) : make_float2(0.f, 0.f);
+      const int p = p0 + u * beside + sub;
+      on[u] = mine && p < parts && (live >> p & 1);
+      x[u] = on[u] ? *reinterpret_cast<const float4*>(po + (size_t)p * hd) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (u < n) {
-        const float w = lane_value(wgt, at[u]);
-        L += w * lane_value(ml.y, at[u]);
-        o.x += w * x[u].x;
-        o.y += w * x[u].y;
+    for (int u = 0; u < 4; ++u) {
+      const float w = __shfl(wgt, min(p0 + u * beside + sub, 63), 64);
+      if (on[u]) {
+        o.x += w * x[u].x; o.y += w * x[u].y; o.z += w * x[u].z; o.w += w * x[u].w;
       }
+    }
   }
-  if (!mine) return;
+  for (int k = width; k < 64; k <<= 1) {
+    o.x += __shfl_xor(o.x, k, 64); o.y += __shfl_xor(o.y, k, 64); o.z += __shfl_xor(o.z, k, 64); o.w += __shfl_xor(o.w, k, 64);
+  }
+  if (!mine || sub > 0) return;
   const float by = L != 0.f ? L : INFINITY;   // no visible key: zeros
-  o.x /= by;
-  o.y /= by;
+  o = make_float4(o.x / by, o.y / by, o.z / by, o.w / by);
   if constexpr (OPERAND) {
-    Act<T>::store(out, m, hq * hd + 2 * lane, ga.n_q_heads * hd, o.x);
-    Act<T>::store(out, m, hq * hd + 2 * lane + 1, ga.n_q_heads * hd, o.y);
+    Act<T>::store4(out, m, hq * hd + d, ga.n_q_heads * hd, o);
+  } else if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint2*>(out + (size_t)row * hd + d) = make_uint2(pack_bf16_pair(o.x, o.y), pack_bf16_pair(o.z, o.w));
   } else {
-    T* to = out + (size_t)row * hd + 2 * lane;
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(to) = pack_bf16_pair(o.x, o.y);
-    else *reinterpret_cast<float2*>(to) = o;
+    *reinterpret_cast<float4*>(out + (size_t)row * hd + d) = o;
   }
 }
 

@@ -172,7 +172,8 @@ inline GroupShape group_shape(const dflash_dims& m, int S, int block_size, int n
   g.tile = group_by_tiles(m.dtype == DFLASH_BF16, m.head_dim, S, g.rows, n_groups) ? 128 : kOwnTile;
   g.tiles = group_tile_slots(S, g.rows, g.tile, n_groups);
   g.own_tiles = (g.rows + kOwnTile - 1) / kOwnTile;
-  g.splits = group_plan((int)((long long)S * g.rows + g.tile - 1) / g.tile, S, g.own_tiles, m.n_kv_heads, prefix_tokens, own_tokens);
+  g.splits = group_plan((int)((long long)S * g.rows + g.tile - 1) / g.tile, S, g.rows, m.n_kv_heads, prefix_tokens, own_tokens,
+                        S * block_size * m.n_q_heads);
   return g;
 }
 
@@ -205,7 +206,8 @@ inline size_t arrive_counters(size_t D) { return std::max<size_t>(1, D / 64); }
 
 struct Workspace {
   size_t status, arena, h, a, q, o, act, taps, fuse, ht, logits_d, logits_t, part_o, part_ml, stats_p, stats_q, amax, lsep, rope_t, rope_d, ssq, arrive, pf_lens, pf_plens, pf_table, pf_tokens, pf_end_row, pf_end_seq, pf_first, pf_anchor, pf_tiles, total;
-  size_t grp_tiles, grp_seqs, grp_common, pg_copies, pg_wants, pg_ids, pg_head;   // sequences that share pages: the groups' tables, the ledger's scratch
+  size_t grp_tiles, grp_seqs, grp_common, pg_copies, pg_wants, pg_ids, pg_head;
+  size_t part_rows;   // rows of part_o and part_ml   // sequences that share pages: the groups' tables, the ledger's scratch
   size_t moe_sel_e, moe_sel_w, moe_sel_pos, moe_row_of, moe_items, moe_a, moe_act, moe_y;   // routed-expert target only
 };
 Workspace workspace_layout(const dflash_dims& t, const dflash_dims& d, const dflash_runtime& rt, const Knobs& kn) {
@@ -245,13 +247,14 @@ Workspace workspace_layout(const dflash_dims& t, const dflash_dims& d, const dfl
         const SplitPlan p = plan_splits(S, m->n_kv_heads << sh, max_tokens, kn.attn_target_wgs);
         part_rows = std::max(part_rows, (size_t)S * blk * m->n_q_heads * p.bound);
       }
-      for (int blk = 1; blk <= rt.block_size; ++blk) {   // sequences that share pages (one group: the fewest tiles, so the most key ranges)
-        const GroupSplits p = group_shape(*m, S, blk, 1, max_tokens, max_tokens).splits;
-        part_rows = std::max(part_rows, (size_t)S * blk * m->n_q_heads * (p.prefix + p.own));
+      for (int blk = 1; blk <= rt.block_size; ++blk) {   // sequences that share pages: whatever their lengths and groups
+        const int rows = S * blk * m->n_q_heads;
+        part_rows = std::max(part_rows, (size_t)rows * group_parts(rows));
       }
     }
   }
   const size_t hd = std::max(t.head_dim, d.head_dim);
+  w.part_rows = part_rows;
   w.part_o = take(part_rows * hd * 4);
   w.part_ml = take(part_rows * 8);
   w.stats_p = take((size_t)M * 8);
@@ -571,6 +574,11 @@ struct Engine {
     SeqGeom geo = geom(b);
     geo.block_size = block;
     const int n_rows = S * block * m.n_q_heads;
+    if ((size_t)n_rows * (sh.splits.prefix + sh.splits.own) > c->ws.part_rows) {   // (group_plan keeps to group_parts)
+      hip_err = 1;
+      fail(c->err, DFLASH_EWORKSPACE, "group attention: %d rows in %d ranges exceed the workspace's %zu partial rows", n_rows, sh.splits.prefix + sh.splits.own, c->ws.part_rows);
+      return;
+    }
     {
       // algorithmic bytes: what is shared once, as the caller expects it, the rest per sequence
       const double tokens = (double)g.n_groups * expected + (double)S * (std::max(0, b->max_seq_len - expected) + block);
