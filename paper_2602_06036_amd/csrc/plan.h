@@ -113,7 +113,7 @@ inline bool attention_by_tiles(int tiles, int blocks, int head_groups, int cache
 
 // ---- attention of sequences that share pages: key ranges of the prefix part and of the own parts ----------------------
 // Estimated time of a launch, microseconds, by the pairs of pages (32 keys) of a workgroup's range.  Prefix tiles: `alone` a pair with a CU to itself, `shared` on a CU
-// that has two workgroups; own parts `own`, of few rows (up to 16: one block, bound by its pages) `own_few`.  Ramps and ends: `ends` for the longest workgroup, `filled`
+// that has two workgroups; own parts `own_alone` and `own`, of few rows (up to 16: one block, bound by its pages) less.  Ramps and ends: `ends` for the longest workgroup, `filled`
 // where others fill them, `round` for each further round of own parts; `join` for a row of a further range, written and read.  Launches of 32 x 1 row behind 8192
 // shared and 326 own tokens, prefix ranges 4, 8, 16, 32: 60, 35, 24, 20; 16 x 16 rows behind 1968 and 600, ranges (prefix, own) (2, 1) 36, (4, 1) 30, (4, 2) 28,
 // (6, 2) 36, (8, 4) 39; 32 x 16 behind 16384 and 800 (2, 1) 244, (3, 1) 209, (4, 1) 198; 4 x 16 behind 4096 and 64, 8, 16, 32: 21, 19, 27.
@@ -126,7 +126,7 @@ inline int group_parts(int all_rows) { return std::max(2, std::min(64, kGroupPar
 inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, int prefix_tokens, int own_tokens, int all_rows) {
   const double alone = 0.9, shared = 0.68, ends = 10.0, filled = 8.0, join = 1.5e-4;
   const bool few = rows <= 16;
-  const double own = few ? 0.3 : 0.4, own_fixed = few ? 0.5 : 2.0, round = few ? 2.0 : 10.0;
+  const double own = few ? 0.3 : 0.4, own_alone = few ? 0.3 : 0.6, own_fixed = few ? 0.5 : 2.0, round = few ? 2.0 : 10.0;
   const int tried[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
   const int a = std::max(1, tiles * n_kv_heads), b = n_seqs * ((rows + 63) / 64) * n_kv_heads, pp = (prefix_tokens + 31) / 32, po = (own_tokens + 31) / 32;
   const int most = group_parts(all_rows);
@@ -138,7 +138,7 @@ inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, i
     for (int ns : tried) {
       if (ns > 1 && (ns * 4 > po || np + ns > most)) break;
       const int o = (po + ns - 1) / ns;
-      const double longest = std::max(on_cu > 1 ? shared * on_cu * p : alone * on_cu * p, own * o + own_fixed) + ends;
+      const double longest = std::max(on_cu > 1 ? shared * on_cu * p : alone * on_cu * p, own_alone * o + own_fixed) + ends;
       const double all = (wgs * shared * p + b * ns * (own * 0.5 * o + own_fixed)) / 256 + filled;   // own parts: half of the longest one's keys on average
       const double t = std::max(longest, all) + round * ((wgs + b * ns + 511) / 512 - 1) + join * all_rows * (np + ns);
       if (t < best_t) { best_t = t; best = {np, ns}; }
