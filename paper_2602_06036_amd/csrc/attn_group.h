@@ -39,7 +39,8 @@ __host__ __device__ __forceinline__ int group_tile_slots(int n_seqs, int rows, i
 
 // Groups -> tiles, a workgroup a sequence: which group it belongs to (the caller's starts as their running maximum, inside the batch; the first is 0), what it has in
 // common with the group's first sequence, and, of that one, the group's tiles.  n_groups = 1 needs no starts.
-__global__ __launch_bounds__(256) void group_plan_kernel(SeqGeom geo, const int32_t* __restrict__ starts, int n_groups, int n_seqs, int rows, int tile, GroupTables gt) {
+__global__ __launch_bounds__(256) void group_plan_kernel(SeqGeom geo, const int32_t* __restrict__ starts, int n_groups, int n_seqs, int rows, int tile, int expected,
+                                                      GroupTables gt) {
   __shared__ int s_next, s_start, s_end, s_after, s_pages;
   const int t = threadIdx.x, s = blockIdx.x, mpps = geo.max_pages_per_seq;
   if (t == 0) {
@@ -72,7 +73,8 @@ __global__ __launch_bounds__(256) void group_plan_kernel(SeqGeom geo, const int3
   }
   const int g = s_next - 1, start = s_start, end = s_end;
   const int32_t *lead = geo.block_table + (size_t)start * mpps, *row = geo.block_table + (size_t)s * mpps;
-  const int most = end - start > 1 ? min(mpps, min(max(geo.seq_lens[s], 0), max(geo.seq_lens[start], 0)) / DF_PAGE) : 0;
+  int most = min(mpps, min(max(geo.seq_lens[s], 0), max(geo.seq_lens[start], 0)) / DF_PAGE);
+  if (end - start == 1) most = min(most, expected / DF_PAGE);   // a sequence by itself is cut where its launch's ranges expect it
   int pages = most;
   for (int p = t; p < pages; p += 256) {
     const int id = lead[p];
@@ -280,7 +282,7 @@ struct PairFrags<float, HD> {
   }
 };
 
-// Any storage type and head dim.  A wavefront sweeps 16 rows, pairs of pages straight from memory; the workgroup's four share its rows (up to 64) or, where there
+// fp32, and bf16 with other head dims.  A wavefront sweeps 16 rows, pairs of pages straight from memory; the workgroup's four share its rows (up to 64) or, where there
 // are fewer, the keys too, and add their parts in LDS.
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict__ q, const T* __restrict__ pool, SeqGeom geo, GroupArgs ga, GroupTables gt,
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
     *reinterpret_cast<float4*>(part_o + pr * HD + dt * 16 + 4 * g) = make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]);
 }
 
-// ---- bf16, head dim 64 or 128: wavefronts split the keys ------------------------------------------------------------------
+// ---- bf16, head dims 32, 64, 96 and 128: wavefronts split the keys ------------------------------------------------------------------
 // Four wavefronts take every fourth pair of pages each for all RB blocks of 16 query rows, from a ring of their own in LDS: the pages go there
 // directly (global_load_lds), K refilled as soon as a pair's scores are done and V as soon as its products are, so nothing in flight costs a
 // register and no wavefront waits for another before the end, where their partial results are added in LDS.  The loads are counted by hand (NI per half page,
@@ -687,7 +689,7 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
   }
 }
 
-// ---- bf16, head dim 64 or 128: tiles of 128 query rows of the prefix part -----------------------------------------------------
+// ---- bf16, head dims 32, 64, 96 and 128: tiles of 128 query rows of the prefix part -----------------------------------------------------
 // Four wavefronts of 32 rows, the pages staged in an LDS ring that all four read (a stage is a pair of pages: K of page A, of page B, V of A, of B; every
 // wavefront copies a quarter), one barrier a stage, two workgroups a CU.  32x32x16 MFMAs: S^T = K . Q^T leaves a lane 16 of the pair's keys (quartets h and h + 2
 // of either page, h = lane / 32) of query column lane % 32, and O^T += V^T . P^T takes them as they are.
@@ -998,7 +1000,7 @@ __global__ __launch_bounds__(256) void group_merge_kernel(const float* __restric
 
 // whether the prefix part goes by tiles of 128 rows: the groups have more rows, on average, than a key-split workgroup
 inline bool group_by_tiles(bool bf16, int hd, int n_seqs, int rows, int n_groups) {
-  return bf16 && (hd == 128 || hd == 64) && (long long)n_seqs * rows > (long long)n_groups * kOwnTile;
+  return bf16 && hd % 32 == 0 && (long long)n_seqs * rows > (long long)n_groups * kOwnTile;
 }
 
 // plain: the rows leave in the model's type (one plane of probabilities is enough)
@@ -1017,20 +1019,22 @@ inline void group_attn_launch(hipStream_t st, const T* q, const T* pool, const S
       else few ? launch(group_attn_mfma_kernel<HD, 0, 4, 1>) : launch(group_attn_mfma_kernel<HD, 0, 4, 4>);
     };
     if (hd == 128) return mfma(std::integral_constant<int, 128>{});
+    if (hd == 96) return mfma(std::integral_constant<int, 96>{});
     if (hd == 64) return mfma(std::integral_constant<int, 64>{});
+    if (hd == 32) return mfma(std::integral_constant<int, 32>{});
   }
   auto go = [&](auto c) { hipLaunchKernelGGL((group_attn_kernel<T, decltype(c)::value>), grid, block, 0, st, q, pool, geo, ga, gt, part_o, part_ml); };
   switch (hd) {
     case 16: return go(std::integral_constant<int, 16>{});
-    case 32: return go(std::integral_constant<int, 32>{});
     case 48: return go(std::integral_constant<int, 48>{});
     case 80: return go(std::integral_constant<int, 80>{});
-    case 96: return go(std::integral_constant<int, 96>{});
     case 112: return go(std::integral_constant<int, 112>{});
     default: break;
   }
   if constexpr (sizeof(T) == 4) {
+    if (hd == 32) return go(std::integral_constant<int, 32>{});
     if (hd == 64) return go(std::integral_constant<int, 64>{});
+    if (hd == 96) return go(std::integral_constant<int, 96>{});
     go(std::integral_constant<int, 128>{});
   }
 }

@@ -561,7 +561,8 @@ struct Engine {
     SeqGeom geo = geom(b);
     geo.block_size = block;
     const GroupShape sh = group_shape(m, b->n_seqs, block, g.n_groups, 0, 0);
-    hipLaunchKernelGGL(group_plan_kernel, dim3(b->n_seqs), dim3(256), 0, st, geo, g.group_starts, g.n_groups, b->n_seqs, sh.rows, sh.tile, group_tables());
+    hipLaunchKernelGGL(group_plan_kernel, dim3(b->n_seqs), dim3(256), 0, st, geo, g.group_starts, g.n_groups, b->n_seqs, sh.rows, sh.tile, g.prefix_len,
+                       group_tables());
     check();
   }
   // of the q rows; `out` rows as GEMM operand or plain

@@ -51,7 +51,7 @@ def attention64(q, k, v, table, lens, causal, n_pages):
 
 def by_tiles(hd, rows, n_seqs, n_groups):
     """Whether the prefix part of a bf16 model goes by tiles of 128 rows (rows: query rows of a sequence and kv head)."""
-    return hd in (64, 128) and n_seqs * rows > 64 * n_groups
+    return hd % 32 == 0 and n_seqs * rows > 64 * n_groups
 
 
 def allowed(ref, slack, wabs, dtype, one_plane):
