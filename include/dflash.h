@@ -265,7 +265,8 @@ typedef struct {
   int32_t n_groups;            /* in [1, n_seqs] */
   int32_t prefix_len;          /* (host) about how many tokens the sequences of a group have in common; balances launches, nothing else */
   const int32_t *group_starts; /* (device) [n_groups] first sequence of each group, ascending from 0; the last group ends with the batch.  May be
-                                  null for one group.  Starts that are not raise the device status and are taken as their running maximum */
+                                  null for one group.  Other starts are taken as their running maximum and raise the device status, where they are
+                                  looked at: small calls attend sequence by sequence and do without */
 } dflash_groups;
 
 /* While set, dflash_draft_block and dflash_verify attend to the pages that a group has in common once for all rows of the group, instead of

@@ -21,8 +21,10 @@ struct GroupArgs {
   int tile;                 // rows of a tile of the prefix part: 64 or 128
   int max_tiles;            // tiles of the prefix part, at most
   int own_tiles;            // tiles (of 64 rows) of a sequence's own part
-  int prefix_splits, own_splits;
+  int prefix_splits, own_splits;   // prefix_splits 0: every sequence by itself from its first key, without a plan
   float scale;
+  void* out;                // one range in all: the finished rows go here and no merge follows
+  int operand;              // ... as GEMM operand (Act<T>), else plain rows of the model's type
 };
 
 constexpr int kOwnTile = 64;   // query rows of a workgroup of an own part
@@ -138,8 +140,12 @@ __device__ __forceinline__ bool group_work(GroupWork& w, int& kvh, const SeqGeom
   }
   i -= n_prefix;
   const int split = i % ga.own_splits, tile = i / ga.own_splits % ga.own_tiles, s = i / (ga.own_splits * ga.own_tiles);
-  const int2 g = gt.group[s];
-  const int len = max(geo.seq_lens[s], 0), n_tok = min(len + geo.block_size, geo.max_pages_per_seq * DF_PAGE), first = group_prefix(gt, g.x, g.y);
+  const int len = max(geo.seq_lens[s], 0), n_tok = min(len + geo.block_size, geo.max_pages_per_seq * DF_PAGE);
+  int first = 0;
+  if (ga.prefix_splits) {
+    const int2 g = gt.group[s];
+    first = group_prefix(gt, g.x, g.y);
+  }
   const int chunk = ((n_tok - first + 31) / 32 + ga.own_splits - 1) / ga.own_splits * 32;
   w = {s * ga.rows + tile * kOwnTile, min(kOwnTile, ga.rows - tile * kOwnTile), geo.block_table + (size_t)s * geo.max_pages_per_seq,
        min(first + split * chunk, n_tok), min(first + (split + 1) * chunk, n_tok), ga.causal ? len : -1, ga.prefix_splits + split};
@@ -282,6 +288,17 @@ struct PairFrags<float, HD> {
   }
 };
 
+// four dims of a finished row (m_hq: its place among the query rows of all heads)
+template <typename T>
+__device__ __forceinline__ void group_store(const GroupArgs& ga, size_t m_hq, int hd, int d, float4 o, float l) {
+  const float by = l != 0.f ? l : INFINITY;   // no visible key: zeros
+  o = make_float4(o.x / by, o.y / by, o.z / by, o.w / by);
+  T* out = static_cast<T*>(ga.out);
+  if (ga.operand) Act<T>::store4(out, (int)(m_hq / ga.n_q_heads), (int)(m_hq % ga.n_q_heads) * hd + d, ga.n_q_heads * hd, o);
+  else if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out + m_hq * hd + d) = make_uint2(pack_bf16_pair(o.x, o.y), pack_bf16_pair(o.z, o.w));
+  else *reinterpret_cast<float4*>(out + m_hq * hd + d) = o;
+}
+
 // fp32, and bf16 with other head dims.  A wavefront sweeps 16 rows, pairs of pages straight from memory; the workgroup's four share its rows (up to 64) or, where there
 // are fewer, the keys too, and add their parts in LDS.
 template <typename T, int HD>
@@ -386,6 +403,11 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
     }
   }
   if (!valid) return;
+  if (ga.out) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) group_store<T>(ga, m_hq, HD, dt * 16 + 4 * g, make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]), l);
+    return;
+  }
   const size_t pr = m_hq * (ga.prefix_splits + ga.own_splits) + w.part;
   if (g == 0) part_ml[pr] = make_float2(m_run, l);
 #pragma unroll
@@ -673,9 +695,7 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
   for (int i = threadIdx.x; i < w.n_rows * (HD / 4); i += 64 * NW) {
     const int r = i / (HD / 4), d4 = i % (HD / 4);
     const size_t pr = (size_t)s_row[r] * parts + w.part;
-    const float4 o = *reinterpret_cast<const float4*>(&s_o[0][r][d4 * 4]), o1 = *reinterpret_cast<const float4*>(&s_o[1][r][d4 * 4]);
-    *reinterpret_cast<float4*>(part_o + pr * HD + d4 * 4) = make_float4(o.x + o1.x, o.y + o1.y, o.z + o1.z, o.w + o1.w);
-    if (d4 == 0) {
+    auto sum = [&]() {   // (maximum, sum) of the row
       float m_all = -INFINITY, l = 0.f;
 #pragma unroll
       for (int v = 0; v < NW; ++v) m_all = fmaxf(m_all, s_ml[v][r].x);
@@ -684,8 +704,16 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
         const float2 ml = s_ml[v][r];
         l += ml.y == 0.f ? 0.f : ml.y * (ml.x == m_all ? 1.f : __builtin_amdgcn_exp2f(ml.x - m_all));
       }
-      part_ml[pr] = make_float2(m_all, l);
+      return make_float2(m_all, l);
+    };
+    const float4 o = *reinterpret_cast<const float4*>(&s_o[0][r][d4 * 4]), o1 = *reinterpret_cast<const float4*>(&s_o[1][r][d4 * 4]);
+    const float4 x = make_float4(o.x + o1.x, o.y + o1.y, o.z + o1.z, o.w + o1.w);
+    if (ga.out) {
+      group_store<bf16_t>(ga, s_row[r], HD, d4 * 4, x, sum().y);
+      continue;
     }
+    *reinterpret_cast<float4*>(part_o + pr * HD + d4 * 4) = x;
+    if (d4 == 0) part_ml[pr] = sum();
   }
 }
 
@@ -950,13 +978,13 @@ __global__ __launch_bounds__(256, 2) void group_attn_mfma_kernel(const bf16_t* _
 }
 
 // Parts -> rows, a wavefront a row, four dims a lane, as many parts side by side as that leaves room for (two of 128 dims) and four times that on their way.  A part
-// without keys (its sum is exactly 0) is left out.  OPERAND: GEMM activation operand (Act<T>), else plain rows of the model's type.
-template <typename T, bool OPERAND>
-__global__ __launch_bounds__(256) void group_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, T* __restrict__ out, GroupArgs ga,
-                                                          int hd, int n_rows) {
+// without keys (its sum is exactly 0) is left out.
+template <typename T>
+__global__ __launch_bounds__(256) void group_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, GroupArgs ga, int hd,
+                                                          int n_rows) {
   const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // m * n_q_heads + hq
   if (row >= n_rows) return;
-  const int parts = ga.prefix_splits + ga.own_splits, m = row / ga.n_q_heads, hq = row % ga.n_q_heads;
+  const int parts = ga.prefix_splits + ga.own_splits;
   const int width = hd > 64 ? 32 : hd > 32 ? 16 : 8, beside = 64 / width, sub = lane / width, d = lane % width * 4;   // lanes of a part, parts side by side
   const float2 ml = lane < parts ? part_ml[(size_t)row * parts + lane] : make_float2(-INFINITY, 0.f);
   const bool some = ml.y != 0.f, mine = d < hd;
@@ -987,15 +1015,7 @@ __global__ __launch_bounds__(256) void group_merge_kernel(const float* __restric
     o.x += __shfl_xor(o.x, k, 64); o.y += __shfl_xor(o.y, k, 64); o.z += __shfl_xor(o.z, k, 64); o.w += __shfl_xor(o.w, k, 64);
   }
   if (!mine || sub > 0) return;
-  const float by = L != 0.f ? L : INFINITY;   // no visible key: zeros
-  o = make_float4(o.x / by, o.y / by, o.z / by, o.w / by);
-  if constexpr (OPERAND) {
-    Act<T>::store4(out, m, hq * hd + d, ga.n_q_heads * hd, o);
-  } else if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<uint2*>(out + (size_t)row * hd + d) = make_uint2(pack_bf16_pair(o.x, o.y), pack_bf16_pair(o.z, o.w));
-  } else {
-    *reinterpret_cast<float4*>(out + (size_t)row * hd + d) = o;
-  }
+  group_store<T>(ga, row, hd, d, o, L);
 }
 
 // whether the prefix part goes by tiles of 128 rows: the groups have more rows, on average, than a key-split workgroup
@@ -1013,7 +1033,8 @@ inline void group_attn_launch(hipStream_t st, const T* q, const T* pool, const S
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, q, pool, geo, ga, gt, part_o, part_ml); };
     auto mfma = [&](auto c) {
       constexpr int HD = decltype(c)::value;
-      if (ga.tile > kOwnTile && plain) few ? launch(group_attn_mfma_kernel<HD, 1, 0, 1>) : launch(group_attn_mfma_kernel<HD, 1, 0, 4>);
+      if (!ga.prefix_splits) few ? launch(group_attn_mfma_kernel<HD, 0, 1, 1>) : launch(group_attn_mfma_kernel<HD, 0, 4, 4>);
+      else if (ga.tile > kOwnTile && plain) few ? launch(group_attn_mfma_kernel<HD, 1, 0, 1>) : launch(group_attn_mfma_kernel<HD, 1, 0, 4>);
       else if (ga.tile > kOwnTile) few ? launch(group_attn_mfma_kernel<HD, 2, 0, 1>) : launch(group_attn_mfma_kernel<HD, 2, 0, 4>);
       else if (few_all) launch(group_attn_mfma_kernel<HD, 0, 1, 1>);
       else few ? launch(group_attn_mfma_kernel<HD, 0, 4, 1>) : launch(group_attn_mfma_kernel<HD, 0, 4, 4>);

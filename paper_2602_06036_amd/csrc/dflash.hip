@@ -165,6 +165,7 @@ inline int attn_q_shift(const dflash_dims& m, int block_size) {
 struct GroupShape {
   int rows, tile, tiles, own_tiles;
   GroupSplits splits;
+  bool apart;      // every sequence by itself
 };
 inline GroupShape group_shape(const dflash_dims& m, int S, int block_size, int n_groups, int prefix_tokens, int own_tokens) {
   GroupShape g;
@@ -420,7 +421,8 @@ struct Engine {
   int lse_parts = 0;     // > 0: ... and that many per-row softmax-statistics partials in ws.lsep
   bool lm_skip_store = false;   // the LM-head GEMM may drop its logits when its argmax is fused (nobody will read them)
   PrefillTiles tiles;    // the layer() call in progress is a prefill's, whose attention goes by these
-  const dflash_groups* groups = nullptr;   // the layer() call in progress attends to what its groups share once (group_plan() has run)
+  const dflash_groups* groups = nullptr;   // the layer() call in progress attends to what its groups share once (use_groups)
+  GroupShape shape{};
   int pending_tap = -1;  // tap index to be taken from the completed residual stream by the next RMSNorm
 
   // Few-row path: ws.a holds x * gain with the division by the row's rms deferred to the GEMM that reads it; the
@@ -555,55 +557,60 @@ struct Engine {
 
   void attention(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, bool causal);
 
-  // ---- sequences that share pages (attn_group.h): the groups' tables, once a pass, and a layer's attention
+  // ---- sequences that share pages (attn_group.h): launch shape and tables of the groups, once a pass, and a layer's attention
   GroupTables group_tables() { return GroupTables{ws<int4>(c->ws.grp_tiles), ws<int2>(c->ws.grp_seqs), ws<int32_t>(c->ws.grp_common)}; }
-  void group_tables_of(const dflash_dims& m, const dflash_batch* b, const dflash_groups& g, int block) {
+  GroupShape shape_of(const dflash_dims& m, const dflash_batch* b, const dflash_groups& g, int block) {
+    const int most = c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE, expected = std::min(g.prefix_len, most), tokens = std::min(b->max_seq_len + block, most);
+    GroupShape sh = group_shape(m, b->n_seqs, block, g.n_groups, expected, std::max(block, tokens - expected));
+    sh.apart = group_apart(sh.splits.us, b->n_seqs, sh.rows, m.n_kv_heads, tokens, std::is_same<T, bf16_t>::value && m.head_dim % 32 == 0, c->k.group_apart);
+    return sh;
+  }
+  void group_tables_of(const GroupShape& sh, const dflash_batch* b, const dflash_groups& g, int block) {
     SeqGeom geo = geom(b);
     geo.block_size = block;
-    const GroupShape sh = group_shape(m, b->n_seqs, block, g.n_groups, 0, 0);
     hipLaunchKernelGGL(group_plan_kernel, dim3(b->n_seqs), dim3(256), 0, st, geo, g.group_starts, g.n_groups, b->n_seqs, sh.rows, sh.tile, g.prefix_len,
                        group_tables());
     check();
   }
   // of the q rows; `out` rows as GEMM operand or plain
-  void group_attention(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, const dflash_groups& g, int block, bool causal, const T* q,
-                       T* out, bool operand) {
-    const int S = b->n_seqs;
-    const int most = c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE, expected = std::min(g.prefix_len, most);
-    const GroupShape sh = group_shape(m, S, block, g.n_groups, expected, std::min(std::max(0, b->max_seq_len - expected) + block, most));
-    GroupArgs ga{m.n_q_heads, m.n_kv_heads, layer, causal, S, sh.rows, sh.tile, sh.tiles, sh.own_tiles, sh.splits.prefix, sh.splits.own, 1.0f / sqrtf((float)m.head_dim)};
-    SeqGeom geo = geom(b);
-    geo.block_size = block;
-    const int n_rows = S * block * m.n_q_heads;
-    if ((size_t)n_rows * (sh.splits.prefix + sh.splits.own) > c->ws.part_rows) {   // (group_plan keeps to group_parts)
+  void group_attention(const GroupShape& sh, const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, const dflash_groups& g, int block, bool causal,
+                       const T* q, T* out, bool operand) {
+    const int S = b->n_seqs, n_rows = S * block * m.n_q_heads;
+    GroupArgs ga{m.n_q_heads, m.n_kv_heads, layer, causal, S, sh.rows, sh.tile, sh.apart ? 0 : sh.tiles, sh.own_tiles, sh.apart ? 0 : sh.splits.prefix,
+                 sh.apart ? 1 : sh.splits.own, 1.0f / sqrtf((float)m.head_dim), sh.apart ? out : nullptr, operand};
+    if (!sh.apart && (size_t)n_rows * (ga.prefix_splits + ga.own_splits) > c->ws.part_rows) {   // (group_plan keeps to group_parts)
       hip_err = 1;
-      fail(c->err, DFLASH_EWORKSPACE, "group attention: %d rows in %d ranges exceed the workspace's %zu partial rows", n_rows, sh.splits.prefix + sh.splits.own, c->ws.part_rows);
+      fail(c->err, DFLASH_EWORKSPACE, "group attention: %d rows in %d ranges exceed the workspace's %zu partial rows", n_rows, ga.prefix_splits + ga.own_splits, c->ws.part_rows);
       return;
     }
+    SeqGeom geo = geom(b);
+    geo.block_size = block;
     {
       // algorithmic bytes: what is shared once, as the caller expects it, the rest per sequence
-      const double tokens = (double)g.n_groups * expected + (double)S * (std::max(0, b->max_seq_len - expected) + block);
+      const int shared = std::min(g.prefix_len, b->max_seq_len);
+      const double tokens = (double)g.n_groups * shared + (double)S * (b->max_seq_len - shared + block);
       ProfScope prof(c, st, DFLASH_PROF_ATTN, tokens * 2 * m.n_kv_heads * m.head_dim * sizeof(T));
       group_attn_launch<T>(st, q, pool, geo, ga, m.head_dim, group_tables(), ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), !operand);
       check();
     }
+    if (sh.apart) return;
     ProfScope prof(c, st, DFLASH_PROF_ATTN_MERGE, 0.0);
-    const dim3 grid((n_rows + 3) / 4), threads(256);
-    if (operand)
-      hipLaunchKernelGGL((group_merge_kernel<T, true>), grid, threads, 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), out, ga, m.head_dim, n_rows);
-    else
-      hipLaunchKernelGGL((group_merge_kernel<T, false>), grid, threads, 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), out, ga, m.head_dim, n_rows);
+    ga.out = out;
+    hipLaunchKernelGGL(group_merge_kernel<T>, dim3((n_rows + 3) / 4), dim3(256), 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), ga, m.head_dim, n_rows);
     check();
   }
   int attend(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, const dflash_groups& g, int rows, bool causal, const void* q, void* out) {
-    group_tables_of(m, b, g, rows);
-    group_attention(m, pool, layer, b, g, rows, causal, static_cast<const T*>(q), static_cast<T*>(out), false);
+    const GroupShape sh = shape_of(m, b, g, rows);
+    if (!sh.apart) group_tables_of(sh, b, g, rows);
+    group_attention(sh, m, pool, layer, b, g, rows, causal, static_cast<const T*>(q), static_cast<T*>(out), false);
     return hip_err ? DFLASH_EHIP : DFLASH_OK;
   }
   void use_groups(const dflash_dims& m, const dflash_batch* b) {
     if (!c->groups.n_groups) return;
+    shape = shape_of(m, b, c->groups, blk(b));
+    if (shape.apart) return;   // the step's attention as it is without groups
     groups = &c->groups;
-    group_tables_of(m, b, c->groups, blk(b));
+    group_tables_of(shape, b, c->groups, blk(b));
   }
 
   // one Transformer layer on the M block rows held in ws.h.  gain_next (nullable): gain of the RMSNorm behind the layer, which may
@@ -1250,7 +1257,7 @@ void Engine<float>::resid(const float*, const float*, int, int, int, const float
 template <typename T>
 void Engine<T>::attention(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, bool causal) {
   const int S = b->n_seqs, B = blk(b), M = S * B;
-  if (groups) return group_attention(m, pool, layer, b, *groups, B, causal, ws<T>(c->ws.q), ws<T>(c->ws.o), true);
+  if (groups) return group_attention(shape, m, pool, layer, b, *groups, B, causal, ws<T>(c->ws.q), ws<T>(c->ws.o), true);
   const int max_tokens = std::min(b->max_seq_len + B, c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE);
   const int q_shift = attn_q_shift(m, B);
   const SplitPlan p = plan_splits(S, m.n_kv_heads << q_shift, max_tokens, c->k.attn_target_wgs);

@@ -34,6 +34,7 @@ struct Knobs {
   int moe_gather_min_rows;  // DFLASH_MOE_GATHER_MIN_ROWS: rows from which the routed-expert GEMMs get their rows copied into list order
   int moe_kept_kb;          // DFLASH_MOE_KEPT_KB: a target's expert matrices up to this size are taken to stay in the memory-side cache
   int moe_down_u;           // DFLASH_MOE_DOWN_U: k tiles per stage of the one-band down projection
+  int group_apart;          // DFLASH_GROUP_APART: sequences that share pages, 1 = each by itself, 2 = what they share once for all, any other value: by estimated time
   int fuse;                 // DFLASH_FUSE: few-row path, see dflash_ctx::fuse
   int resid_nw, resid_u;    // DFLASH_RESID_NW / _U: wavefronts per workgroup and k tiles per stage of the unsplit projection kernel
 };
@@ -57,6 +58,7 @@ inline Knobs read_knobs() {
   k.moe_gather_min_rows = env_int("DFLASH_MOE_GATHER_MIN_ROWS", 64);
   k.moe_kept_kb = env_int("DFLASH_MOE_KEPT_KB", 128 << 10);
   k.moe_down_u = env_int("DFLASH_MOE_DOWN_U", 1);
+  k.group_apart = env_int("DFLASH_GROUP_APART", 0);
   k.fuse = env_int("DFLASH_FUSE", 1);
   if (k.fuse != 1 && k.fuse != 2) k.fuse = 0;
   k.resid_nw = env_int("DFLASH_RESID_NW", 4);
@@ -119,6 +121,7 @@ inline bool attention_by_tiles(int tiles, int blocks, int head_groups, int cache
 // (6, 2) 36, (8, 4) 39; 32 x 16 behind 16384 and 800 (2, 1) 244, (3, 1) 209, (4, 1) 198; 4 x 16 behind 4096 and 64, 8, 16, 32: 21, 19, 27.
 struct GroupSplits {
   int prefix, own;
+  double us;      // estimated time of the launch
 };
 // Most ranges of both parts together for a call of `all_rows` query rows of all heads, whatever the lengths: the workspace holds that many partial rows each.
 constexpr int kGroupPartRows = 98304;
@@ -130,8 +133,7 @@ inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, i
   const int tried[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
   const int a = std::max(1, tiles * n_kv_heads), b = n_seqs * ((rows + 63) / 64) * n_kv_heads, pp = (prefix_tokens + 31) / 32, po = (own_tokens + 31) / 32;
   const int most = group_parts(all_rows);
-  GroupSplits best{1, 1};
-  double best_t = 1e30;
+  GroupSplits best{1, 1, 1e30};
   for (int np : tried) {
     if (np > 1 && (np * 4 > pp || np + 1 > most)) break;   // four pairs a range at least
     const int p = (pp + np - 1) / np, wgs = pp ? a * np : 0, on_cu = (wgs + 255) / 256;
@@ -141,10 +143,20 @@ inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, i
       const double longest = std::max(on_cu > 1 ? shared * on_cu * p : alone * on_cu * p, own_alone * o + own_fixed) + ends;
       const double all = (wgs * shared * p + b * ns * (own * 0.5 * o + own_fixed)) / 256 + filled;   // own parts: half of the longest one's keys on average
       const double t = std::max(longest, all) + round * ((wgs + b * ns + 511) / 512 - 1) + join * all_rows * (np + ns);
-      if (t < best_t) { best_t = t; best = {np, ns}; }
+      if (t < best.us) best = {np, ns, t};
     }
   }
   return best;
+}
+
+// Whether sequences that share pages are better off each by itself, in one launch without a plan and a merge (about 6 us of launches), for short contexts and small
+// batches.  `shared_us`: the estimate above; tokens of the longest sequence.
+inline bool group_apart(double shared_us, int n_seqs, int rows, int n_kv_heads, int tokens, bool bf16_mfma, int knob) {
+  if (knob == 1 || knob == 2) return knob == 1;
+  const int wgs = n_seqs * ((rows + 63) / 64) * n_kv_heads, pairs = (tokens + 31) / 32;
+  const double pair = bf16_mfma ? (rows <= 16 ? 0.3 : 0.6) : 0.4, fixed = bf16_mfma && rows > 16 ? 2.0 : 0.5;
+  const double longest = pair * pairs + fixed + 6.0, all = wgs * (pair * pairs + fixed) / 256 + 4.0;
+  return std::max(longest, all) < shared_us + 6.0;
 }
 
 // ---- GEMMs ----------------------------------------------------------------------------------------------

@@ -30,6 +30,7 @@ def _engine(dtype, target, draft, block, seqs, width, n_pages):
 # ---- attention ----------------------------------------------------------------------------------------------------------
 LAYOUTS = [("f32", 4, 4, 64), ("f32", 6, 2, 48), ("f32", 2, 1, 128), ("f32", 3, 1, 16), ("bf16", 32, 8, 128), ("bf16", 8, 8, 64), ("bf16", 12, 4, 96),
            ("bf16", 16, 1, 32), ("bf16", 10, 2, 80), ("bf16", 8, 1, 128), ("bf16", 6, 2, 16), ("bf16", 4, 2, 112), ("bf16", 6, 2, 48)]
+APART, ONCE = "1", "2"          # DFLASH_GROUP_APART: every sequence by itself; what a group shares once, by the plan, however small the call
 # (rows, causal, lengths, pages shared by each group, group starts)
 SHAPES = [
     (1, True, (0,), (0,), (0,)),                                        # one token, nothing cached
@@ -110,25 +111,27 @@ def _attend(torch, e, table, lens, starts, q, pool, layer, causal, prefix_len):
     return out
 
 
-def _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, causal, dtype, kv, hd, prefix_len, pool=0, layer=1):
+def _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, causal, dtype, kv, hd, prefix_len, pool=0, layer=1, way=ONCE):
     got = _attend(torch, e, table, lens, starts, q, pool, layer, causal, prefix_len).double().cpu()
     k, v = (x.double().cpu() for x in unpack(pools[pool], layer, kv, hd))
     ref, slack, wabs = attention64(q.double().cpu(), k, v, table, lens, causal, n_pages)
-    err, most = (got - ref).abs(), allowed(ref, slack, wabs, dtype, by_tiles(hd, rows * (q.shape[2] // kv), len(lens), len(starts)))
+    err, most = (got - ref).abs(), allowed(ref, slack, wabs, dtype, way != APART and by_tiles(hd, rows * (q.shape[2] // kv), len(lens), len(starts)))
     assert bool((err <= most).all()), (float((err - most).max()), float(err.max()))
     return got
 
 
+@pytest.mark.parametrize("way", [APART, ONCE])
 @pytest.mark.parametrize("shape", range(len(SHAPES)))
 @pytest.mark.parametrize("layout", range(len(LAYOUTS)))
-def test_attention_of_groups(layout, shape):
+def test_attention_of_groups(layout, shape, way, monkeypatch):
     torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
     dtype, heads, kv, hd = LAYOUTS[layout]
     rows, causal, lens, shared, starts = SHAPES[shape]
     rows = min(rows, 64 // (heads // kv))
     e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, shared, starts, 100 * layout + shape)
     for hint in (max(shared) * PAGE, 0):          # the hint moves work between launches, not results
-        _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, causal, dtype, kv, hd, hint, pool=shape % 2)
+        _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, causal, dtype, kv, hd, hint, pool=shape % 2, way=way)
     e.device_status()
     e.close()
 
@@ -137,18 +140,29 @@ def test_attention_of_groups(layout, shape):
     ("bf16", 8, 2, 128, 16, 9, 65, 300, True), ("bf16", 8, 2, 128, 16, 9, 65, 300, False), ("bf16", 8, 1, 128, 16, 3, 130, 40, True),
     ("bf16", 4, 1, 128, 1, 40, 257, 20, True), ("bf16", 4, 4, 64, 5, 17, 33, 90, True), ("bf16", 2, 1, 128, 4, 2, 520, 1100, True),
     ("f32", 4, 1, 64, 8, 11, 40, 200, True), ("bf16", 4, 1, 128, 16, 1, 0, 700, True)])
-def test_attention_over_long_contexts(dtype, heads, kv, hd, rows, S, pages, own, causal):
+def test_attention_over_long_contexts(dtype, heads, kv, hd, rows, S, pages, own, causal, monkeypatch):
     torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", ONCE)
     lens = [pages * PAGE + (own * (i + 1)) // S + (i % 3) for i in range(S)]
     e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, (pages,), (0,), 5)
     _compare(torch, e, pools, table, lens, (0,), n_pages, q, rows, causal, dtype, kv, hd, pages * PAGE)
     e.close()
 
 
+@pytest.mark.parametrize("dtype,heads,kv,hd,rows,lens", [("f32", 4, 4, 64, 8, (4000, 30)), ("bf16", 8, 2, 128, 16, (9000, 100, 3000))])
+def test_a_long_context_by_itself(dtype, heads, kv, hd, rows, lens, monkeypatch):
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", APART)
+    e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, (0,), (0,), 6)
+    _compare(torch, e, pools, table, lens, (0,), n_pages, q, rows, True, dtype, kv, hd, 0, way=APART)
+    e.close()
+
+
 @pytest.mark.parametrize("dtype,heads,kv,hd", [("f32", 4, 4, 64), ("bf16", 8, 2, 128)])
-def test_any_grouping_gives_the_same_rows(dtype, heads, kv, hd):
+def test_any_grouping_gives_the_same_rows(dtype, heads, kv, hd, monkeypatch):
     """Groups that do not match what is shared; starts that are not raise the status."""
     torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", ONCE)
     from paper_2602_06036_amd import binding as B
     rows, lens, shared, starts = 4, (70, 80, 66, 90, 33, 40), (4, 2), (0, 4)
     e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, shared, starts, 3)
@@ -164,17 +178,19 @@ def test_any_grouping_gives_the_same_rows(dtype, heads, kv, hd):
     e.close()
 
 
-@pytest.mark.parametrize("dtype,heads,kv,hd", [("f32", 4, 2, 64), ("bf16", 4, 2, 128), ("bf16", 4, 2, 32)])
-def test_missing_pages_and_nan_keys(dtype, heads, kv, hd):
+@pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("dtype,heads,kv,hd", [("f32", 4, 2, 64), ("bf16", 4, 2, 128), ("bf16", 4, 2, 32), ("bf16", 4, 2, 80), ("bf16", 64, 2, 128)])
+def test_missing_pages_and_nan_keys(dtype, heads, kv, hd, way, monkeypatch):
     """Entries outside the pool are keys that are not there, in the shared part of the table as behind it; a row without any is zeros; a NaN key
     makes the rows that see it NaN, and no others."""
     torch = _torch()
-    rows, lens, shared, starts = 3, (70, 84, 66, 20), (4, 0), (0, 3)
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    rows, lens, shared, starts = 3 if heads < 64 else 2, (70, 84, 66, 20), (4, 0), (0, 3)
     e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, shared, starts, 4)
     table[:3, 2] = -1
     table[1, 4] = n_pages
     table[3, :] = -1
-    got = _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, True, dtype, kv, hd, 64)
+    got = _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, True, dtype, kv, hd, 64, way=way)
     assert (got[3] == 0).all()
     at = torch.arange(PAGE * hd, device=e.device)
     for page, key, hit in ((table[0, 1], 5, (0, 1, 2)), (table[2, 4], 3, (2,))):      # in the shared pages; the second row of sequence 2's block
@@ -191,8 +207,10 @@ def test_missing_pages_and_nan_keys(dtype, heads, kv, hd):
     e.close()
 
 
-def test_attention_on_a_stream_and_in_a_graph():
+@pytest.mark.parametrize("way", [APART, ONCE])
+def test_attention_on_a_stream_and_in_a_graph(way, monkeypatch):
     torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
     from paper_2602_06036_amd import binding as B
     rows, lens, shared, starts = 4, (170, 180, 266, 190), (10,), (0,)
     e, pools, table, n_pages, q = _case(torch, "bf16", 8, 2, 128, rows, lens, shared, starts, 8)
@@ -490,10 +508,12 @@ def _shared_model(w, wt, wd, prompts, children, steps):
     return g, led, e.groups(starts, min(len(p) for p in prompts) // PAGE * PAGE), owner
 
 
-def test_forked_samples_step_as_the_oracle_does():
+@pytest.mark.parametrize("way", [ONCE, "0"])
+def test_forked_samples_step_as_the_oracle_does(way, monkeypatch):
     """fp32 model: two prompts, samples forked off them, then blocks drafted, verified, accepted and committed with the shared pages read once; the samples go
     different ways by their proposals.  Every sequence against the oracle's state of its own."""
     torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
     from oracle import dflash_oracle as O
     import paper_2602_06036_amd as dfl
     w = tiny_workload(seed=9, n_layers=2, draft_layers=1, vocab=512, block=8, n_seqs=6, ctx=(60, 60), taps=(0,))
@@ -537,10 +557,11 @@ def _copy(st):
 
 
 @pytest.mark.parametrize("temperature", [0.0, 0.8])
-def test_bf16_step_with_and_without_groups(temperature):
+def test_bf16_step_with_and_without_groups(temperature, monkeypatch):
     """The same forked batch stepped with the groups set and without: either within the bf16 model's 2e-2 of exact order-free arithmetic (as the parity tests have it), so
     4e-2 apart at most; and without again, bit for bit."""
     torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", ONCE)
     import paper_2602_06036_amd as dfl
     w = si.small_bf16_workload(n_seqs=7, ctx_min=20, ctx_max=150, seed=31, temperature=temperature)
     wt, wd = si.make_weights(w, 8)
