@@ -1437,13 +1437,13 @@ int check_rows(dflash_ctx* ctx, const dflash_ledger* l, int n, const int32_t* ro
     if (rows[i] < 0 || rows[i] >= l->n_rows) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: row %d outside [0,%d)", what, rows[i], l->n_rows);
   return DFLASH_OK;
 }
-bool has_twice(int n, const int32_t* a, int m, const int32_t* b) {   // a value twice in a, or in a and b
-  std::vector<int32_t> x(a, a + n);
-  std::sort(x.begin(), x.end());
-  if (std::adjacent_find(x.begin(), x.end()) != x.end()) return true;
-  for (int i = 0; i < m; ++i)
-    if (std::binary_search(x.begin(), x.end(), b[i])) return true;
-  return false;
+// marks every row of the list; false where one is marked already
+bool mark_rows(std::vector<uint8_t>& seen, int n, const int32_t* rows) {
+  for (int i = 0; i < n; ++i) {
+    if (seen[rows[i]]) return false;
+    seen[rows[i]] = 1;
+  }
+  return true;
 }
 
 }  // namespace
@@ -1783,17 +1783,31 @@ int dflash_pages_fork(dflash_ctx* ctx, const dflash_ledger* ledger, int32_t n, c
   if ((rc = check_ledger(ctx, ledger))) return rc;
   if (n < 0 || (n > 0 && (!parents || !children))) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_fork: bad count or null rows");
   if ((rc = check_rows(ctx, ledger, n, parents, "pages_fork")) || (rc = check_rows(ctx, ledger, n, children, "pages_fork"))) return rc;
+  if (n == 0) return DFLASH_OK;
+  std::vector<uint8_t> seen;
+  std::vector<int16_t> first;   // place of a parent's first child in the launch
   try {
-    if (has_twice(n, children, n, parents)) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_fork: a row is a child twice, or child and parent");
+    seen.resize(ledger->n_rows);
+    first.resize(ledger->n_rows, -1);
   } catch (const std::bad_alloc&) {
     return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_fork: out of host memory");
   }
+  bool once = mark_rows(seen, n, children);
+  for (int i = 0; i < n; ++i) once = once && !seen[parents[i]];
+  if (!once) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_fork: a row is a child twice, or child and parent");
   const Ledger l = device_ledger(ctx, ledger);
   for (int i = 0; i < n; i += kRowsPerLaunch) {
     const int k = std::min(n - i, kRowsPerLaunch);
-    RowPairs rows;
-    std::copy(parents + i, parents + i + k, rows.a);
-    std::copy(children + i, children + i + k, rows.b);
+    ForkRows rows;
+    std::copy(parents + i, parents + i + k, rows.parent);
+    std::copy(children + i, children + i + k, rows.child);
+    for (int j = 0; j < k; ++j) {
+      int16_t& f = first[rows.parent[j]];
+      if (f < 0) f = (int16_t)j;
+      rows.count[j] = 0;
+      ++rows.count[f];
+    }
+    for (int j = 0; j < k; ++j) first[rows.parent[j]] = -1;
     hipLaunchKernelGGL(pages_fork_kernel, dim3((l.mpps + 255) / 256, k), dim3(256), 0, (hipStream_t)stream, l, rows);
   }
   return launched(ctx, "pages_fork");
@@ -1806,11 +1820,14 @@ int dflash_pages_release(dflash_ctx* ctx, const dflash_ledger* ledger, int32_t n
   if ((rc = check_rows(ctx, ledger, n, rows, "pages_release"))) return rc;
   for (int i = 0; keep && i < n; ++i)
     if (keep[i] < 0) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_release: negative length %d", keep[i]);
+  if (n == 0) return DFLASH_OK;
+  std::vector<uint8_t> seen;
   try {
-    if (has_twice(n, rows, 0, nullptr)) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_release: a row is given twice");
+    seen.resize(ledger->n_rows);
   } catch (const std::bad_alloc&) {
     return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_release: out of host memory");
   }
+  if (!mark_rows(seen, n, rows)) return CTX_FAIL(ctx, DFLASH_EINVAL, "pages_release: a row is given twice");
   const Ledger l = device_ledger(ctx, ledger);
   for (int i = 0; i < n; i += kRowsPerLaunch) {
     const int k = std::min(n - i, kRowsPerLaunch);
