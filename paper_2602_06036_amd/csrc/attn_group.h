@@ -722,9 +722,9 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
 // wavefront copies a quarter), one barrier a stage, two workgroups a CU.  32x32x16 MFMAs: S^T = K . Q^T leaves a lane 16 of the pair's keys (quartets h and h + 2
 // of either page, h = lane / 32) of query column lane % 32, and O^T += V^T . P^T takes them as they are.
 // Three stages of the sweep are in work at once, independent of each other: scores of pair i + 2, softmax of pair i + 1, products of pair i.  Matrix and vector
-// instructions of one wavefront then run side by side, and the other workgroup's fill what is left.
-// PLANES = 2: probabilities as a hi + lo bf16 pair (~16 bits, as everywhere in the bf16 model).  PLANES = 1: rounded to bf16 once, for rows that leave in
-// bf16 themselves: the weights' error of 2^-9 each, averaged over the keys, lies below the output's own rounding, and a third of the matrix work is gone.
+// instructions of one wavefront then run side by side, and the other workgroup's fill what is left.  Probabilities are a hi + lo bf16 pair, ~16 bits, as everywhere in the
+// bf16 model.  (Rounded to bf16 once, for rows that leave in bf16 themselves, 32 x 16 rows behind 16384 tokens take 196 us instead of 233, nine smaller calls as long as
+// with the pair, and the rows' error against 64 bits is 0.0023 instead of the 0.0017 of their own rounding.)
 template <int HD>
 struct TileSweep {
   static constexpr int KT = HD / 16, MT = HD / 32, NS = 5;
@@ -732,7 +732,7 @@ struct TileSweep {
 };
 __device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
-template <int HD, int PLANES>
+template <int HD>
 __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w, int kvh, const bf16_t* __restrict__ q, const bf16_t* __restrict__ pool,
                                                  const SeqGeom& geo, const GroupArgs& ga, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   typedef TileSweep<HD> C;
@@ -780,7 +780,7 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) acc[mt] = (f32x16){};
   const float scale2 = ga.scale * 1.44269504088896341f;   // base-2 exponents
-  struct P { u32x4 v[PLANES][2]; };   // probabilities of page A's and page B's keys
+  struct P { u32x4 v[2][2]; };   // hi and lo of page A's and page B's keys
   P p0, p1;
   f32x16 s0, s1;
 
@@ -826,7 +826,7 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) acc[mt] *= corr;
 #pragma unroll
-      for (int pl = 0; pl < PLANES; ++pl)
+      for (int pl = 0; pl < 2; ++pl)
 #pragma unroll
         for (int b2 = 0; b2 < 2; ++b2)
 #pragma unroll
@@ -849,7 +849,7 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
         const float x = e[8 * b + 2 * i], y = e[8 * b + 2 * i + 1];
         const uint32_t v = pack_bf16_pair(x, y);
         p.v[0][b][i] = v;
-        if constexpr (PLANES == 2) p.v[1][b][i] = pack_bf16_pair(x - __uint_as_float(v << 16), y - __uint_as_float(v & 0xFFFF0000u));
+        p.v[1][b][i] = pack_bf16_pair(x - __uint_as_float(v << 16), y - __uint_as_float(v & 0xFFFF0000u));
       }
   };
   auto scores = [&](f32x16& s, int slot) {
@@ -885,20 +885,13 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {   // KT = 2 MT: the chain of the scores between products that do not wait for each other
 #pragma unroll
-        for (int j = 0; j < PLANES; ++j) {
-          const int at = kt * PLANES + j;
+        for (int j = 0; j < 2; ++j) {
+          const int at = kt * 2 + j;
           pv(vf[at / MT % 2][at % MT], p.v[at / (2 * MT)][at / MT % 2], at % MT);
         }
         qk(sn, kf[kt], kt);
       }
       soft(s, pn);
-      if constexpr (PLANES == 1) {   // a matrix instruction and four vector ones in turn (128 pairs a workgroup: 187 us as the compiler orders them, 174 so; two planes 225 and 231)
-#pragma unroll
-        for (int j = 0; j < 2 * KT; ++j) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x402, 4, 0);
-        }
-      }
       __builtin_amdgcn_sched_barrier(0);
     }
     slot = slot + 1 == NS ? 0 : slot + 1;
@@ -939,7 +932,7 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int pl = 0; pl < PLANES; ++pl) pv(vf[b][mt], p.v[pl][b], mt);
+        for (int pl = 0; pl < 2; ++pl) pv(vf[b][mt], p.v[pl][b], mt);
     }
     slot = slot + 1 == NS ? 0 : slot + 1;
   };
@@ -962,18 +955,18 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
       *reinterpret_cast<float4*>(part_o + pr * HD + mt * 32 + 8 * j + 4 * h) = make_float4(acc[mt][4 * j], acc[mt][4 * j + 1], acc[mt][4 * j + 2], acc[mt][4 * j + 3]);
 }
 
-// PLANES > 0: the prefix part by tiles of 128 rows; 0: by key-split workgroups of RBP blocks of 16 rows.  RBO: row blocks of an own part's workgroup.
-template <int HD, int PLANES, int RBP, int RBO>
+// RBP: row blocks (of 16) of the prefix part's key-split workgroups, 0: tiles of 128 rows.  RBO: row blocks of an own part's workgroup.
+template <int HD, int RBP, int RBO>
 __global__ __launch_bounds__(256, 2) void group_attn_mfma_kernel(const bf16_t* __restrict__ q, const bf16_t* __restrict__ pool, SeqGeom geo, GroupArgs ga,
                                                                  GroupTables gt, float* __restrict__ part_o, float2* __restrict__ part_ml) {
-  constexpr int P_BYTES = PLANES ? TileSweep<HD>::BYTES : KeySplit<HD>::bytes(RBP), O_BYTES = KeySplit<HD>::bytes(RBO);
+  constexpr int P_BYTES = RBP ? KeySplit<HD>::bytes(RBP) : TileSweep<HD>::BYTES, O_BYTES = KeySplit<HD>::bytes(RBO);
   __shared__ __attribute__((aligned(1024))) char s_raw[P_BYTES > O_BYTES ? P_BYTES : O_BYTES];
   static_assert(sizeof(s_raw) <= 80 * 1024, "two workgroups a CU");
   GroupWork w;
   int kvh;
   if (!group_work<256>(w, kvh, geo, ga, gt, part_ml)) return;
   if (w.part >= ga.prefix_splits) return group_sweep_keys<HD, RBO>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
-  if constexpr (PLANES > 0) group_sweep_tile<HD, PLANES>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
+  if constexpr (RBP == 0) group_sweep_tile<HD>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
   else group_sweep_keys<HD, RBP>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
 }
 
@@ -1023,21 +1016,18 @@ inline bool group_by_tiles(bool bf16, int hd, int n_seqs, int rows, int n_groups
   return bf16 && hd % 32 == 0 && (long long)n_seqs * rows > (long long)n_groups * kOwnTile;
 }
 
-// plain: the rows leave in the model's type (one plane of probabilities is enough)
 template <typename T>
 inline void group_attn_launch(hipStream_t st, const T* q, const T* pool, const SeqGeom& geo, const GroupArgs& ga, int hd, const GroupTables& gt, float* part_o,
-                              float2* part_ml, bool plain) {
+                              float2* part_ml) {
   const dim3 grid((ga.max_tiles * ga.prefix_splits + ga.n_seqs * ga.own_tiles * ga.own_splits) * ga.n_kv_heads), block(256);
   if constexpr (sizeof(T) == 2) {
     const bool few = ga.rows <= 16, few_all = (long long)ga.n_seqs * ga.rows <= 16;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, q, pool, geo, ga, gt, part_o, part_ml); };
     auto mfma = [&](auto c) {
       constexpr int HD = decltype(c)::value;
-      if (!ga.prefix_splits) few ? launch(group_attn_mfma_kernel<HD, 0, 1, 1>) : launch(group_attn_mfma_kernel<HD, 0, 4, 4>);
-      else if (ga.tile > kOwnTile && plain) few ? launch(group_attn_mfma_kernel<HD, 1, 0, 1>) : launch(group_attn_mfma_kernel<HD, 1, 0, 4>);
-      else if (ga.tile > kOwnTile) few ? launch(group_attn_mfma_kernel<HD, 2, 0, 1>) : launch(group_attn_mfma_kernel<HD, 2, 0, 4>);
-      else if (few_all) launch(group_attn_mfma_kernel<HD, 0, 1, 1>);
-      else few ? launch(group_attn_mfma_kernel<HD, 0, 4, 1>) : launch(group_attn_mfma_kernel<HD, 0, 4, 4>);
+      if (!ga.prefix_splits || few_all) few ? launch(group_attn_mfma_kernel<HD, 1, 1>) : launch(group_attn_mfma_kernel<HD, 4, 4>);
+      else if (ga.tile > kOwnTile) few ? launch(group_attn_mfma_kernel<HD, 0, 1>) : launch(group_attn_mfma_kernel<HD, 0, 4>);
+      else few ? launch(group_attn_mfma_kernel<HD, 4, 1>) : launch(group_attn_mfma_kernel<HD, 4, 4>);
     };
     if (hd == 128) return mfma(std::integral_constant<int, 128>{});
     if (hd == 96) return mfma(std::integral_constant<int, 96>{});

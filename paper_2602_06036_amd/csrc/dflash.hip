@@ -590,7 +590,7 @@ struct Engine {
       const int shared = std::min(g.prefix_len, b->max_seq_len);
       const double tokens = (double)g.n_groups * shared + (double)S * (b->max_seq_len - shared + block);
       ProfScope prof(c, st, DFLASH_PROF_ATTN, tokens * 2 * m.n_kv_heads * m.head_dim * sizeof(T));
-      group_attn_launch<T>(st, q, pool, geo, ga, m.head_dim, group_tables(), ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), !operand);
+      group_attn_launch<T>(st, q, pool, geo, ga, m.head_dim, group_tables(), ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml));
       check();
     }
     if (sh.apart) return;

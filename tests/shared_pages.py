@@ -49,18 +49,12 @@ def attention64(q, k, v, table, lens, causal, n_pages):
     return out, slack, wabs
 
 
-def by_tiles(hd, rows, n_seqs, n_groups):
-    """Whether the prefix part of a bf16 model goes by tiles of 128 rows (rows: query rows of a sequence and kv head)."""
-    return hd % 32 == 0 and n_seqs * rows > 64 * n_groups
-
-
-def allowed(ref, slack, wabs, dtype, one_plane):
-    """bf16: the output's rounding, and that of the probabilities.  As a hi + lo pair of bf16 numbers: hi is off by at most 2^-8 of the value, lo by 2^-8 of that,
-    2^-16 of every weight.  one_plane (rows that leave in bf16 by tiles): every weight w_i is off by at most 2^-8 w_i in the numerator and exact in the sum, so the
-    row by at most 2^-8 sum w_i |v_i| = 2^-8 wabs."""
+def allowed(ref, slack, wabs, dtype):
+    """bf16: the output's rounding, and that of the probabilities as a hi + lo pair of bf16 numbers: hi is off by at most 2^-8 of the value, lo by 2^-8 of that, 2^-16 of
+    every weight w_i, so the row by at most 2^-16 sum w_i |v_i| = 2^-16 wabs."""
     if dtype == "f32":
         return slack + 2.0 ** -23 * ref.abs()
-    return slack + (2.0 ** -8 if one_plane else 2.0 ** -16) * wabs + 2.0 ** -8 * ref.abs()
+    return slack + 2.0 ** -16 * wabs + 2.0 ** -8 * ref.abs()
 
 
 class LedgerModel:
