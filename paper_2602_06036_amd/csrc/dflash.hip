@@ -167,6 +167,7 @@ struct GroupShape {
   GroupSplits splits;
   bool apart;      // every sequence by itself
 };
+inline bool group_on_mfma(const dflash_dims& m) { return m.dtype == DFLASH_BF16 && m.head_dim % 32 == 0; }
 inline GroupShape group_shape(const dflash_dims& m, int S, int block_size, int n_groups, int prefix_tokens, int own_tokens) {
   GroupShape g;
   g.rows = block_size * (m.n_q_heads / m.n_kv_heads);
@@ -174,7 +175,7 @@ inline GroupShape group_shape(const dflash_dims& m, int S, int block_size, int n
   g.tiles = group_tile_slots(S, g.rows, g.tile, n_groups);
   g.own_tiles = (g.rows + kOwnTile - 1) / kOwnTile;
   g.splits = group_plan((int)((long long)S * g.rows + g.tile - 1) / g.tile, S, g.rows, m.n_kv_heads, prefix_tokens, own_tokens,
-                        S * block_size * m.n_q_heads);
+                        S * block_size * m.n_q_heads, group_on_mfma(m));
   return g;
 }
 
@@ -562,7 +563,7 @@ struct Engine {
   GroupShape shape_of(const dflash_dims& m, const dflash_batch* b, const dflash_groups& g, int block) {
     const int most = c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE, expected = std::min(g.prefix_len, most), tokens = std::min(b->max_seq_len + block, most);
     GroupShape sh = group_shape(m, b->n_seqs, block, g.n_groups, expected, std::max(block, tokens - expected));
-    sh.apart = group_apart(sh.splits.us, b->n_seqs, sh.rows, m.n_kv_heads, tokens, std::is_same<T, bf16_t>::value && m.head_dim % 32 == 0, c->k.group_apart);
+    sh.apart = group_apart(sh.splits.us, b->n_seqs, sh.rows, m.n_kv_heads, tokens, group_on_mfma(m), c->k.group_apart);
     return sh;
   }
   void group_tables_of(const GroupShape& sh, const dflash_batch* b, const dflash_groups& g, int block) {

@@ -126,10 +126,13 @@ struct GroupSplits {
 // Most ranges of both parts together for a call of `all_rows` query rows of all heads, whatever the lengths: the workspace holds that many partial rows each.
 constexpr int kGroupPartRows = 98304;
 inline int group_parts(int all_rows) { return std::max(2, std::min(64, kGroupPartRows / std::max(1, all_rows))); }
-inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, int prefix_tokens, int own_tokens, int all_rows) {
-  const double alone = 0.9, shared = 0.68, ends = 10.0, filled = 8.0, join = 1.5e-4;
+// The plain kernel (`mfma` false) takes longer by far, the less the fewer blocks of 16 rows its workgroups have (others share the keys).
+inline double group_blocks(long long rows) { return (double)std::min<long long>(4, (rows + 15) / 16) / 4; }
+inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, int prefix_tokens, int own_tokens, int all_rows, bool mfma) {
   const bool few = rows <= 16;
-  const double own = few ? 0.3 : 0.4, own_alone = few ? 0.3 : 0.6, own_fixed = few ? 0.5 : 2.0, round = few ? 2.0 : 10.0;
+  const double ends = 10.0, filled = 8.0, join = 1.5e-4, round = few ? 2.0 : mfma ? 10.0 : 4.0, plain = group_blocks((long long)n_seqs * rows), own_plain = group_blocks(rows);
+  const double alone = mfma ? 0.9 : 2.5 * plain, shared = mfma ? 0.68 : 1.9 * plain, own_fixed = few ? 0.5 : 2.0;
+  const double own = mfma ? (few ? 0.3 : 0.4) : 1.9 * own_plain, own_alone = mfma ? (few ? 0.3 : 0.6) : 2.5 * own_plain;
   const int tried[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
   const int a = std::max(1, tiles * n_kv_heads), b = n_seqs * ((rows + 63) / 64) * n_kv_heads, pp = (prefix_tokens + 31) / 32, po = (own_tokens + 31) / 32;
   const int most = group_parts(all_rows);
@@ -151,10 +154,10 @@ inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, i
 
 // Whether sequences that share pages are better off each by itself, in one launch without a plan and a merge (about 6 us of launches), for short contexts and small
 // batches.  `shared_us`: the estimate above; tokens of the longest sequence.
-inline bool group_apart(double shared_us, int n_seqs, int rows, int n_kv_heads, int tokens, bool bf16_mfma, int knob) {
+inline bool group_apart(double shared_us, int n_seqs, int rows, int n_kv_heads, int tokens, bool mfma, int knob) {
   if (knob == 1 || knob == 2) return knob == 1;
   const int wgs = n_seqs * ((rows + 63) / 64) * n_kv_heads, pairs = (tokens + 31) / 32;
-  const double pair = bf16_mfma ? (rows <= 16 ? 0.3 : 0.6) : 0.4, fixed = bf16_mfma && rows > 16 ? 2.0 : 0.5;
+  const double pair = mfma ? (rows <= 16 ? 0.3 : 0.6) : 2.5 * group_blocks(rows), fixed = mfma && rows > 16 ? 2.0 : 0.5;
   const double longest = pair * pairs + fixed + 6.0, all = wgs * (pair * pairs + fixed) / 256 + 4.0;
   return std::max(longest, all) < shared_us + 6.0;
 }

@@ -12,9 +12,9 @@ DRIVER = r"""
 #include <stdio.h>
 #include "plan.h"
 int main() {
-  int tiles, seqs, rows, heads, prefix, own, all;
-  while (scanf("%d %d %d %d %d %d %d", &tiles, &seqs, &rows, &heads, &prefix, &own, &all) == 7) {
-    const GroupSplits g = group_plan(tiles, seqs, rows, heads, prefix, own, all);
+  int tiles, seqs, rows, heads, prefix, own, all, mfma;
+  while (scanf("%d %d %d %d %d %d %d %d", &tiles, &seqs, &rows, &heads, &prefix, &own, &all, &mfma) == 8) {
+    const GroupSplits g = group_plan(tiles, seqs, rows, heads, prefix, own, all, mfma != 0);
     printf("%d %d %d\n", g.prefix, g.own, group_parts(all));
   }
 }
@@ -44,10 +44,10 @@ def test_ranges_fit_the_workspace_whatever_the_lengths(plans):
                     for extra in (0, seqs - 1):
                         for prefix in (0, 16, 100, 1029, 8192, 16384, 131072):
                             for own in (1, 40, 613, 1531, 16384):
-                                q.append((-(-seqs * rows // tile) + extra, seqs, rows, heads, prefix, own, seqs * rows * heads))
+                                q.append((-(-seqs * rows // tile) + extra, seqs, rows, heads, prefix, own, seqs * rows * heads, int(tile == 128)))
     for x, (np, ns, most) in zip(q, plans(q)):
         assert np >= 1 and ns >= 1 and np <= 32 and ns <= 32 and np + ns <= most <= 64, (x, np, ns, most)
         assert np == 1 or np * 4 * 32 <= x[4] + 31 * np, (x, np)          # four pairs of pages a range
     # 32 blocks of 16 rows behind 16384 shared tokens: more ranges than lengths that fill the block table give
-    a, b = plans([(16, 32, 64, 8, 16384, 1531, 16384), (16, 32, 64, 8, 17936, 17936, 16384)])
+    a, b = plans([(16, 32, 64, 8, 16384, 1531, 16384, 1), (16, 32, 64, 8, 17936, 17936, 16384, 1)])
     assert a[0] + a[1] <= a[2] and b[0] + b[1] <= b[2] and a[2] == b[2]
