@@ -730,7 +730,6 @@ struct TileSweep {
   static constexpr int KT = HD / 16, MT = HD / 32, NS = 5;
   static constexpr int PART = DF_PAGE * HD * 2, NI = PART / 1024, STAGE = 4 * PART, BYTES = NS * STAGE;   // PART: K or V of a page, NI copies of 1 KB
 };
-__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
 template <int HD>
 __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w, int kvh, const bf16_t* __restrict__ q, const bf16_t* __restrict__ pool,
@@ -775,7 +774,7 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
   asm volatile("" : "+v"(ids_next));
   for (int st = 0; st < NS - 1; ++st) fetch(st);
 
-  float m_run = -INFINITY, neg_m = 0.f, l_run = 0.f;
+  float m_run = -INFINITY, neg_m = INFINITY, l_run = 0.f;   // no maximum yet: the first pair's sums are infinite
   f32x16 acc[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) acc[mt] = (f32x16){};
@@ -811,37 +810,13 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
   auto pv = [&](const u32x4& v, const u32x4& p, int mt) {
     acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), acc[mt], 0, 0, 0);
   };
-  // Lazy reference maximum: it moves only when a row's has grown by more than 8 (in powers of two), decided from each lane's own scores, so the accumulators
-  // are rescaled once or twice a sweep.  Maxima are rounded up to whole numbers: the factor for what is there already is a power of two, which the probabilities
-  // on their way to the products take exactly.  (maximum, not fmax: NaN passes through, which the latter would buy with an instruction a score.)
-  auto raise = [&](const f32x16& s, P& p) {
-    const float a = max3(max3(s[0], s[1], s[2]), s[3], s[4]), b = max3(max3(s[5], s[6], s[7]), s[8], s[9]), c = max3(max3(s[10], s[11], s[12]), s[13], s[14]);
-    const float lmx = max3(max3(a, b, c), s[15], s[15]) * scale2;
-    if (__builtin_amdgcn_ballot_w64(lmx > m_run + 8.f) != 0ull) {
-      const LanePair x = lane_swap32(lmx, lmx);
-      const float mx = ceilf(fmaxf(x.lo, x.hi));
-      const bool grow = mx > m_run + 8.f;
-      const float corr = grow ? (m_run == -INFINITY ? 0.f : exp2f(m_run - mx)) : 1.f;
-      l_run *= corr;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) acc[mt] *= corr;
-#pragma unroll
-      for (int pl = 0; pl < 2; ++pl)
-#pragma unroll
-        for (int b2 = 0; b2 < 2; ++b2)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t v = p.v[pl][b2][i];
-            p.v[pl][b2][i] = pack_bf16_pair(__uint_as_float(v << 16) * corr, __uint_as_float(v & 0xFFFF0000u) * corr);
-          }
-      if (grow) { m_run = mx; neg_m = -mx; }
-    }
-  };
+  // Probabilities of a pair.  The reference maximum is that of the sweep's first pair and stays while the exponentials' sums of a lane's keys stay below 2^60: their
+  // relative precision does not depend on it, and a float and a bf16 hold 2^127.  So a pair costs no maximum, only a look at its sum.
   auto soft = [&](const f32x16& s, P& p) {
     float e[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, neg_m));
-    l_run += (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]))) + (((e[8] + e[9]) + (e[10] + e[11])) + ((e[12] + e[13]) + (e[14] + e[15])));
+    const float sum = (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]))) + (((e[8] + e[9]) + (e[10] + e[11])) + ((e[12] + e[13]) + (e[14] + e[15])));
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -851,6 +826,31 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
         p.v[0][b][i] = v;
         p.v[1][b][i] = pack_bf16_pair(x - __uint_as_float(v << 16), y - __uint_as_float(v & 0xFFFF0000u));
       }
+    return sum;
+  };
+  // ... and the rest of it, when the products before it are in the accumulators: a row whose sum has grown too large (or that has no maximum yet, or a NaN) gets its
+  // reference from this pair, by which everything there is is rescaled
+  auto settle = [&](const f32x16& s, P& p, float sum) {
+    if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p60f)) != 0ull) {
+      float mx = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+      const LanePair x = lane_swap32(mx, mx);
+      mx = fmaxf(x.lo, x.hi) * scale2;
+      if (mx > m_run + 8.f) {
+        const float corr = m_run == -INFINITY ? 0.f : exp2f(m_run - mx);
+        l_run *= corr;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[mt] *= corr;
+        m_run = mx;
+        neg_m = -mx;
+      }
+      const float again = neg_m;
+      if (m_run == -INFINITY) neg_m = 0.f;   // nothing above -inf yet: exp2(-inf - 0) = 0
+      sum = soft(s, p);
+      neg_m = again;
+    }
+    l_run += sum;
   };
   auto scores = [&](f32x16& s, int slot) {
     u32x4 kf[KT];
@@ -868,15 +868,12 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
   if (live) {
     scores(s0, 0);
     if (half_pair && n_pairs == 1) without_b(s0);
-    P none{};
-    raise(s0, none);
-    soft(s0, p0);
+    settle(s0, p0, soft(s0, p0));
     if (n_pairs > 1) scores(s1, 1);
   }
   int slot = 0;   // of stage i
   auto step = [&](P& p, const f32x16& s, P& pn, f32x16& sn) {   // products with p, softmax of s into pn, scores into sn
     if (live) {
-      raise(s, p);
       u32x4 kf[KT], vf[2][MT];
       __builtin_amdgcn_sched_barrier(0);
       read_v(vf, slot);
@@ -891,8 +888,9 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
         }
         qk(sn, kf[kt], kt);
       }
-      soft(s, pn);
+      const float sum = soft(s, pn);
       __builtin_amdgcn_sched_barrier(0);
+      settle(s, pn, sum);
     }
     slot = slot + 1 == NS ? 0 : slot + 1;
   };
@@ -938,9 +936,9 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
   };
   if (i + 1 < n_pairs) {
     if (half_pair) without_b(s1);
-    raise(s1, p0);
-    soft(s1, p1);
+    const float sum = soft(s1, p1);
     last(p0, false);
+    settle(s1, p1, sum);
     p0 = p1;
   }
   last(p0, half_pair);
