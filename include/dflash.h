@@ -226,7 +226,7 @@ int dflash_prefill(dflash_ctx *ctx, const dflash_batch *batch, const int32_t *to
  * calls below keep a block table and a count of who holds which page on the device; the step's calls take their batch from the
  * ledger's arrays (its first n_seqs rows).  Every call is enqueued on `stream`, reads nothing back and allocates nothing.  Page ids are
  * taken in ascending order for rows in ascending order: what a call does depends on the ledger alone.  Entries outside the pool count
- * as "no page". */
+ * as "no page".  They belong between steps, not between the calls of one: a step's K/V rows lie on the pages that it began with. */
 typedef struct {
   int32_t n_rows;       /* rows of the arrays below: sequences that run, that wait, and room for more */
   int32_t *block_table; /* (device) [n_rows, max_pages_per_seq] page ids, -1 = none */

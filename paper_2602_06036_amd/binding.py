@@ -242,12 +242,12 @@ class Engine:
         must outlive the struct)."""
         n = int(block_table.shape[0])
         for t, shape in ((block_table, (n, self.max_pages_per_seq)), (seq_lens, (n,)), (anchor, (n,)), (page_refs, (self.n_pages,))):
-            assert t.dtype == torch.int32 and tuple(t.shape) == shape and t.device == self.device, (t.dtype, tuple(t.shape), shape)
+            assert t.dtype == torch.int32 and tuple(t.shape) == shape and t.device == self.target_pool.device, (t.dtype, tuple(t.shape), shape)
         return Ledger(n, _ptr(block_table), _ptr(seq_lens), _ptr(anchor), _ptr(page_refs))
 
     def groups(self, group_starts: Optional[torch.Tensor], prefix_len: int) -> Groups:
         """Groups of consecutive sequences that begin with the same pages; group_starts None: the whole batch is one."""
-        assert group_starts is None or (group_starts.dtype == torch.int32 and group_starts.dim() == 1 and group_starts.device == self.device)
+        assert group_starts is None or (group_starts.dtype == torch.int32 and group_starts.dim() == 1 and group_starts.device == self.target_pool.device)
         return Groups(1 if group_starts is None else int(group_starts.shape[0]), int(prefix_len), _ptr(group_starts))
 
     def profile_enable(self, on: bool):
@@ -358,8 +358,8 @@ def dflash_pages_fork(e: Engine, ledger: Ledger, parents: Sequence[int], childre
 
 def dflash_pages_reserve(e: Engine, ledger: Ledger, tokens: torch.Tensor, granted: Optional[torch.Tensor] = None):
     """Pages of their own for the next tokens[s] tokens of rows 0 .. len(tokens) - 1; granted[s] = 1 where the row holds them."""
-    n = int(tokens.shape[0])
     assert tokens.dtype == torch.int32 and tokens.dim() == 1
+    n = int(tokens.shape[0])
     assert granted is None or (granted.dtype == torch.int32 and tuple(granted.shape) == (n,))
     _check(e.l.dflash_pages_reserve(e.ctx, C.byref(ledger), n, _ptr(tokens), _ptr(granted), _stream()), e.ctx)
 

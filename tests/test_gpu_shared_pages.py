@@ -360,6 +360,53 @@ def test_copied_rows_of_a_tail(tail):
     p.e.close()
 
 
+@pytest.mark.parametrize("way", [APART, ONCE])
+def test_pages_beyond_four_gigabytes(way, monkeypatch):
+    """A pool whose last pages lie more than 2^32 bytes (and 2^31 elements) behind its start: copied, moved and attended to."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    from paper_2602_06036_amd import binding as B
+    m, n_pages = dims(40, 16, 8, 128), 2000
+    e, pools = _engine("bf16", m, dims(1, 4, 1, 64), 4, 4, 6, n_pages)
+    assert pools[0].numel() > 1 << 31
+    dev, last = e.device, 39
+    table = np.full((4, 6), -1, np.int32)
+    table[0, :3], refs = [n_pages - 1, n_pages - 3, n_pages - 2], np.ones(n_pages, np.int32)     # everything in use but the pages below
+    refs[[1990, 1995]] = 0
+    g = torch.Generator(device=dev)
+    g.manual_seed(2)
+    for i in range(3):
+        pools[0][last, n_pages - 1 - i].copy_(torch.randn(pools[0][last, 0].shape, generator=g, device=dev))
+    t, n, a, r = (torch.from_numpy(x).to(dev) for x in (table, np.array([37, 0, 0, 0], np.int32), np.zeros(4, np.int32), refs))
+    led = e.ledger(t, n, a, r)
+    B.dflash_pages_fork(e, led, [0], [1])
+    B.dflash_pages_reserve(e, led, torch.tensor([2, 2, 0, 0], dtype=torch.int32, device=dev))
+    torch.cuda.synchronize()
+    e.device_status()
+    table[1] = table[0]
+    table[0, 2] = 1990                                                  # the first to ask takes the copy, the last keeps the page
+    assert np.array_equal(t.cpu().numpy(), table)
+    k, v = (x.double().cpu() for x in unpack(pools[0], last, 8, 128))
+    assert torch.equal(k[1990, :8], k[n_pages - 2, :8]) and torch.equal(v[1990, :8], v[n_pages - 2, :8]) and not k[1990, 8:].any()
+    q = torch.randn((2, 2, 16, 128), generator=g, device=dev).bfloat16()
+    for p in (1990, n_pages - 2):                                       # the two new rows of either sequence
+        pools[0][last, p].copy_(torch.randn(pools[0][last, 0].shape, generator=g, device=dev))
+    k, v = (x.double().cpu() for x in unpack(pools[0], last, 8, 128))
+    ref, slack, wabs = attention64(q.double().cpu(), k, v, table, (37, 37), True, n_pages)
+    out = _attend(torch, e, table[:2], (37, 37), (0,), q, 0, last, True, 32).double().cpu()
+    assert bool(((out - ref).abs() <= allowed(ref, slack, wabs, "bf16")).all())
+    r[:1000] = 0                                                        # holes: the high pages move down
+    B.dflash_pages_compact(e, led)
+    torch.cuda.synchronize()
+    moved = t.cpu().numpy()
+    assert (moved[:2, :3] < 1000).all() and (moved[2:] == -1).all()
+    k2, _ = (x.double().cpu() for x in unpack(pools[0], last, 8, 128))
+    for s in range(2):
+        for i in range(3):
+            assert torch.equal(k2[moved[s, i]], k[table[s, i]])
+    e.close()
+
+
 def test_too_few_pages_and_too_short_rows():
     torch = _torch()
     p = Pair(torch, "f32", dims(1, 2, 1, 32), dims(1, 2, 1, 32), 7, 6, 12, 6)
