@@ -149,6 +149,48 @@ def test_attention_over_long_contexts(dtype, heads, kv, hd, rows, S, pages, own,
     e.close()
 
 
+@pytest.mark.parametrize("hd", [32, 64, 96, 128])
+@pytest.mark.parametrize("pages", [1, 2, 3, 4, 5, 6, 7, 8, 9, 11, 12, 63, 64, 65, 67, 129, 131])
+def test_tiles_over_prefix_lengths(hd, pages, monkeypatch):
+    """One range of 1, 2, 3 .. pairs of pages, with and without a page B in the last one, and past the 32 pairs of a set of page ids."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", ONCE)
+    lens = [pages * PAGE + x for x in (3, 0, 19)]
+    e, pools, table, n_pages, q = _case(torch, "bf16", 4, 1, hd, 16, lens, (pages,), (0,), 7 * pages + hd)
+    _compare(torch, e, pools, table, lens, (0,), n_pages, q, 16, pages % 2 == 0, "bf16", 1, hd, 0)
+    e.close()
+
+
+@pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("dtype,hd", [("f32", 64), ("bf16", 128), ("bf16", 64), ("bf16", 80)])
+def test_scores_that_grow_and_keys_that_weigh_nothing(dtype, hd, way, monkeypatch):
+    """Contexts whose scores grow by thousands from page to page (the reference maximum moves, what was there is scaled to nothing), or begin far below the others; keys at
+    minus infinity weigh as if they were not there, also where they are all that a sweep has seen so far."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    rows, lens, shared, starts = 16, (160, 165, 190), (10,), (0,)
+    e, pools, table, n_pages, q = _case(torch, dtype, 4, 1, hd, rows, lens, shared, starts, 11)
+    saved = pools[0].clone()
+    at = torch.arange(PAGE * hd, device=e.device)
+    for factors in ((1, 2, 4, 8, 16, 32, 64, 128, 256, 512), (512, 64, 8, 1, 1, 1, 1, 1, 1, 1), (0.01,) * 8 + (100, 1)):
+        for i, f in enumerate(factors):
+            pools[0][1, int(table[0, i]), :, 0] = saved[1, int(table[0, i]), :, 0] * f
+        _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, True, dtype, 1, hd, 160)
+    # dim 0 of the queries is positive; the first three pages' keys are -inf there
+    q[..., 0] = 1.0
+    pools[0].copy_(saved)
+    without = table.copy()
+    without[:, :3] = -1
+    _compare(torch, e, pools, without, lens, starts, n_pages, q, rows, True, dtype, 1, hd, 160)
+    for i in range(3):
+        pools[0][1, int(table[0, i]), :, 0, (at // 128 == 0) & (at % 8 == 0)] = float("-inf")
+    got = _attend(torch, e, table, lens, starts, q, 0, 1, True, 160).double().cpu()
+    k, v = (x.double().cpu() for x in unpack(saved, 1, 1, hd))
+    want, slack, wabs = attention64(q.double().cpu(), k, v, without, lens, True, n_pages)
+    assert bool(((got - want).abs() <= allowed(want, slack, wabs, dtype)).all()), float((got - want).abs().max())
+    e.close()
+
+
 @pytest.mark.parametrize("dtype,heads,kv,hd,rows,lens", [("f32", 4, 4, 64, 8, (4000, 30)), ("bf16", 8, 2, 128, 16, (9000, 100, 3000))])
 def test_a_long_context_by_itself(dtype, heads, kv, hd, rows, lens, monkeypatch):
     torch = _torch()
