@@ -269,8 +269,9 @@ typedef struct {
                                   looked at: small calls attend sequence by sequence and do without */
 } dflash_groups;
 
-/* While set, dflash_draft_block and dflash_verify attend to the pages that a group has in common once for all rows of the group, instead of
- * once per sequence.  The struct is copied, group_starts must stay valid; null switches it off.  A batch must have at least n_groups sequences.
+/* While set, dflash_draft_block and dflash_verify may attend to the pages that a group has in common once for all rows of the group, instead of
+ * once per sequence, where that is estimated to be faster (few rows a sequence behind long prefixes: a block of 16 rows with 4 query heads a kv head keeps the matrix
+ * cores as busy by itself).  The struct is copied, group_starts must stay valid; null switches it off.  A batch must have at least n_groups sequences.
  * dflash_prefill does not look at it. */
 int dflash_set_groups(dflash_ctx *ctx, const dflash_groups *groups);
 

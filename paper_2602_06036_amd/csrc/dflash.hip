@@ -608,10 +608,17 @@ struct Engine {
   }
   void use_groups(const dflash_dims& m, const dflash_batch* b) {
     if (!c->groups.n_groups) return;
-    shape = shape_of(m, b, c->groups, blk(b));
+    const int B = blk(b), q_shift = attn_q_shift(m, B);
+    shape = shape_of(m, b, c->groups, B);
+    AttnArgs aa;
+    aa.n_q_heads = m.n_q_heads; aa.n_kv_heads = m.n_kv_heads; aa.head_dim = m.head_dim; aa.q_shift = q_shift;
+    if (q_shift >= 0 && attn_takes_mfma<T>(aa, B))
+      shape.apart = step_apart(shape.splits.us, b->n_seqs, m.n_kv_heads << q_shift,
+                               plan_splits(b->n_seqs, m.n_kv_heads << q_shift, std::min(b->max_seq_len + B, c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE), c->k.attn_target_wgs),
+                               c->k.group_apart);
     if (shape.apart) return;   // the step's attention as it is without groups
     groups = &c->groups;
-    group_tables_of(shape, b, c->groups, blk(b));
+    group_tables_of(shape, b, c->groups, B);
   }
 
   // one Transformer layer on the M block rows held in ws.h.  gain_next (nullable): gain of the RMSNorm behind the layer, which may

@@ -162,6 +162,16 @@ inline bool group_apart(double shared_us, int n_seqs, int rows, int n_kv_heads, 
   return std::max(longest, all) < shared_us + 6.0;
 }
 
+// The step's own MFMA attention of such a batch, every sequence by itself: its pages come out of the caches after the first one's reading, so it is bound by its 64-row
+// blocks' arithmetic, whatever share of them is rows.  Estimated time with its merge, against that of the groups (`shared_us`) with theirs and the plan.  Attention and merge
+// of a layer by itself and once for all, 8B shape: 32 x 16 rows behind 8192 shared and 300 own tokens 124 and 123 us, 2048 and 300 45 and 54, 16 x 16 behind 2048 and 600 41
+// and 45, 4 x 16 behind 16384 and 300 47 and 47; 32 x 4 behind 8192 and 300 120 and 58.
+inline bool step_apart(double shared_us, int n_seqs, int head_groups, SplitPlan p, int knob) {
+  if (knob == 1 || knob == 2) return knob == 1;
+  const int rounds = (n_seqs * head_groups * p.n_splits + 255) / 256;
+  return rounds * 0.42 * p.chunk / 32 + (p.chunk >= 512 ? 13.0 : 10.0) + (p.n_splits > 1 ? 7.0 : 0.0) < shared_us + 10.0;
+}
+
 // ---- GEMMs ----------------------------------------------------------------------------------------------
 // rows of partial results the split-K arena holds for a context of at most max_rows activation rows
 inline int arena_rows(int max_rows) { return std::max(1024, 4 * max_rows); }
