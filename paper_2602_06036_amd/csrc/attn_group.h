@@ -148,8 +148,33 @@ __device__ __forceinline__ bool group_work(GroupWork& w, int& kvh, const SeqGeom
   }
   const int chunk = ((n_tok - first + 31) / 32 + ga.own_splits - 1) / ga.own_splits * 32;
   w = {s * ga.rows + tile * kOwnTile, min(kOwnTile, ga.rows - tile * kOwnTile), geo.block_table + (size_t)s * geo.max_pages_per_seq,
-       min(first + split * chunk, n_tok), min(first + (split + 1) * chunk, n_tok), ga.causal ? len : -1, ga.prefix_splits + split};
+       min(first + split * chunk, n_tok), min(first + (split + 1) * chunk, n_tok), ga.causal && geo.block_size > 1 ? len : -1, ga.prefix_splits + split};   // (a single row sees every key)
   return true;
+}
+
+// ---- V rows of keys that some rows see and others do not (the block itself, under the causal mask) -------------------------------
+// A row's weight of a key that it does not see is 0, and its product with an infinity or a NaN would be NaN.  In the pairs that reach into the block such elements are
+// taken out of the products, and given to the rows that see them here: whatever the weight, it is above 0 and the sum becomes what they are.
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(bf16_t x) { return __uint_as_float((uint32_t)x << 16); }
+template <typename T, int DT>
+__device__ __forceinline__ void add_not_finite(f32x4 (&acc)[DT], const T* v, int n_keys, int pos, int last, int lane) {   // of a page's first keys, from position pos
+  n_keys = min(n_keys, last - pos + 1);
+  const T* at = v + (lane >> 4) * 16;
+#pragma unroll 1
+  for (int k = 0; k < n_keys; ++k, at += k & 3 ? 1 : 61)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = widen(at[dt * 256 + i * 4]);
+        acc[dt][i] += not_finite(x) ? x : 0.f;
+      }
+}
+// a pair of bf16 numbers without those that are not finite
+__device__ __forceinline__ uint32_t finite_pair(uint32_t x) {
+  return ((x & 0x7F80u) == 0x7F80u ? 0u : x & 0xFFFFu) | ((x & 0x7F800000u) == 0x7F800000u ? 0u : x & 0xFFFF0000u);
 }
 
 // ---- storage types: fragments of a page pair and their products ------------------------------------------------------------
@@ -207,6 +232,23 @@ struct PairFrags<bf16_t, HD> {
     for (int dt = 0; dt < DT; ++dt) {
       f.a[dt].x &= m0; f.a[dt].y &= m1;
       f.b[dt].x &= m2; f.b[dt].y &= m3;
+    }
+  }
+  static __device__ __forceinline__ bool not_all_finite(const Values& f) {
+    uint32_t odd = 0;
+    auto look = [&](uint32_t x) { odd |= finite_pair(x) ^ x; };
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      look(f.a[dt].x); look(f.a[dt].y);
+      look(f.b[dt].x); look(f.b[dt].y);
+    }
+    return odd != 0;
+  }
+  static __device__ __forceinline__ void drop_not_finite(Values& f) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      f.a[dt] = make_uint2(finite_pair(f.a[dt].x), finite_pair(f.a[dt].y));
+      f.b[dt] = make_uint2(finite_pair(f.b[dt].x), finite_pair(f.b[dt].y));
     }
   }
   static __device__ __forceinline__ void add(f32x4 (&acc)[DT], const Values& v, const float (&p)[8]) {
@@ -271,6 +313,24 @@ struct PairFrags<float, HD> {
     for (int dt = 0; dt < DT; ++dt) {
       f.a[dt] = make_float4(keep(0, f.a[dt].x), keep(1, f.a[dt].y), keep(2, f.a[dt].z), keep(3, f.a[dt].w));
       f.b[dt] = make_float4(keep(4, f.b[dt].x), keep(5, f.b[dt].y), keep(6, f.b[dt].z), keep(7, f.b[dt].w));
+    }
+  }
+  static __device__ __forceinline__ bool not_all_finite(const Values& f) {
+    uint32_t most = 0;
+    auto look = [&](float x) { most = max(most, __float_as_uint(x) & 0x7FFFFFFFu); };
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      look(f.a[dt].x); look(f.a[dt].y); look(f.a[dt].z); look(f.a[dt].w);
+      look(f.b[dt].x); look(f.b[dt].y); look(f.b[dt].z); look(f.b[dt].w);
+    }
+    return most >= 0x7F800000u;
+  }
+  static __device__ __forceinline__ void drop_not_finite(Values& f) {
+    auto drop = [&](float& x) { x = not_finite(x) ? 0.f : x; };
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      drop(f.a[dt].x); drop(f.a[dt].y); drop(f.a[dt].z); drop(f.a[dt].w);
+      drop(f.b[dt].x); drop(f.b[dt].y); drop(f.b[dt].z); drop(f.b[dt].w);
     }
   }
   static __device__ __forceinline__ void add(f32x4 (&acc)[DT], const Values& v, const float (&p)[8]) {
@@ -348,7 +408,8 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
   if (base < w.c1) F::keys(kf, page(max(id.a, 0)), page(id.b >= 0 ? id.b : max(id.a, 0)), lane);   // a page that may be read; its keys weigh nothing
   for (; base < w.c1; base += step) {
     const bool ok_a = id.a >= 0, ok_b = id.b >= 0;
-    F::values(vf, page(max(id.a, 0)), page(ok_b ? id.b : max(id.a, 0)), lane);
+    const T *page_a = page(max(id.a, 0)), *page_b = page(ok_b ? id.b : max(id.a, 0));
+    F::values(vf, page_a, page_b, lane);
     id = ids_of(base + step);
     f32x4 sa, sb;
     F::scores(sa, sb, kf, qf);
@@ -375,6 +436,11 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
       acc[dt][0] *= corr; acc[dt][1] *= corr; acc[dt][2] *= corr; acc[dt][3] *= corr;
     }
     if (there != 0xFFu) F::clear(vf, there);
+    if (w.own_len >= 0 && base + 32 > w.own_len && __builtin_amdgcn_ballot_w64(F::not_all_finite(vf)) != 0ull) {
+      F::drop_not_finite(vf);
+      add_not_finite(acc, page_a + DF_PAGE * HD, ok_a ? min(DF_PAGE, w.c1 - base) : 0, base, last, lane);
+      add_not_finite(acc, page_b + DF_PAGE * HD, ok_b ? min(DF_PAGE, w.c1 - base - DF_PAGE) : 0, base + DF_PAGE, last, lane);
+    }
     F::add(acc, vf, p);
   }
   float l = quarter_sum(l_run);
@@ -594,17 +660,37 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
   auto products = [&](const Pair& pr, int base) {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");   // V is there (the next pair's K may still be on its way)
     uint2* va = reinterpret_cast<uint2*>(s_raw + wave * (4 * PART) + 2 * PART) + lane;
-    if (base + 32 > w.c1 || !pr.ok_a || !pr.ok_b) {   // V of rows that were never written and of foreign pages: 0 * whatever is there must stay 0
+    if (base + 32 > n_all || !pr.ok_a || !pr.ok_b) {   // V of rows that were never written and of foreign pages: 0 * whatever is there must stay 0
       const int pos_a = base + 4 * g, pos_b = base + 16 + 4 * g;
       auto half = [&](bool ok, int p0) { return (ok && p0 < w.c1 ? 0x0000FFFFu : 0u) | (ok && p0 + 1 < w.c1 ? 0xFFFF0000u : 0u); };
       const unsigned a0 = half(pr.ok_a, pos_a), a1 = half(pr.ok_a, pos_a + 2), b0 = half(pr.ok_b, pos_b), b1 = half(pr.ok_b, pos_b + 2);
+      uint32_t odd = 0;
 #pragma unroll 1
       for (int dt = 0; dt < DT; ++dt) {
         uint2 a = va[dt * 64], b = va[PART / 8 + dt * 64];
-        va[dt * 64] = make_uint2(a.x & a0, a.y & a1);
-        va[PART / 8 + dt * 64] = make_uint2(b.x & b0, b.y & b1);
+        a = make_uint2(a.x & a0, a.y & a1);
+        b = make_uint2(b.x & b0, b.y & b1);
+        va[dt * 64] = a;
+        va[PART / 8 + dt * 64] = b;
+        odd |= (finite_pair(a.x) ^ a.x) | (finite_pair(a.y) ^ a.y) | (finite_pair(b.x) ^ b.x) | (finite_pair(b.y) ^ b.y);
       }
       asm volatile("" ::: "memory");
+      if (w.own_len >= 0 && __builtin_amdgcn_ballot_w64(odd != 0) != 0ull) {
+        const bf16_t* v = reinterpret_cast<const bf16_t*>(s_raw + wave * (4 * PART) + 2 * PART);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          add_not_finite(acc[rb], v, DF_PAGE, base, last[rb], lane);
+          add_not_finite(acc[rb], v + PART / 2, DF_PAGE, base + DF_PAGE, last[rb], lane);
+        }
+        asm volatile("" ::: "memory");
+#pragma unroll 1
+        for (int dt = 0; dt < DT; ++dt) {
+          const uint2 a = va[dt * 64], b = va[PART / 8 + dt * 64];
+          va[dt * 64] = make_uint2(finite_pair(a.x), finite_pair(a.y));
+          va[PART / 8 + dt * 64] = make_uint2(finite_pair(b.x), finite_pair(b.y));
+        }
+        asm volatile("" ::: "memory");
+      }
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {

@@ -208,8 +208,8 @@ inline size_t arrive_counters(size_t D) { return std::max<size_t>(1, D / 64); }
 
 struct Workspace {
   size_t status, arena, h, a, q, o, act, taps, fuse, ht, logits_d, logits_t, part_o, part_ml, stats_p, stats_q, amax, lsep, rope_t, rope_d, ssq, arrive, pf_lens, pf_plens, pf_table, pf_tokens, pf_end_row, pf_end_seq, pf_first, pf_anchor, pf_tiles, total;
-  size_t grp_tiles, grp_seqs, grp_common, pg_copies, pg_wants, pg_ids, pg_head;
-  size_t part_rows;   // rows of part_o and part_ml   // sequences that share pages: the groups' tables, the ledger's scratch
+  size_t grp_tiles, grp_seqs, grp_common, pg_copies, pg_wants, pg_ids, pg_head;   // sequences that share pages: the groups' tables, the ledger's scratch
+  size_t part_rows;   // rows of part_o and part_ml
   size_t moe_sel_e, moe_sel_w, moe_sel_pos, moe_row_of, moe_items, moe_a, moe_act, moe_y;   // routed-expert target only
 };
 Workspace workspace_layout(const dflash_dims& t, const dflash_dims& d, const dflash_runtime& rt, const Knobs& kn) {

@@ -250,6 +250,42 @@ def test_missing_pages_and_nan_keys(dtype, heads, kv, hd, way, monkeypatch):
 
 
 @pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("dtype,heads,kv,hd,rows", [("f32", 4, 2, 64, 12), ("f32", 4, 2, 128, 16), ("bf16", 4, 2, 128, 12), ("bf16", 4, 2, 32, 7), ("bf16", 4, 2, 80, 12),
+                                                    ("bf16", 8, 2, 96, 16), ("bf16", 64, 2, 128, 2)])
+def test_values_that_later_rows_see(dtype, heads, kv, hd, rows, way, monkeypatch):
+    """V rows of the block itself with infinities and NaN: under the causal mask the rows in front of them are what they were, those behind get them in the dims that have
+    them, and only there."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    lens, shared, starts = (70, 84, 64, 20, 127), (4, 0), (0, 3)
+    e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, shared, starts, 6)
+    got = _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, True, dtype, kv, hd, 64)
+    planted = {s: s * 3 % rows for s in range(4)} | {4: rows - 1}          # sequence -> slot
+    dims_of = ((0, hd - 1), (5, hd // 2))                                  # of kv head 0 and 1
+    at = torch.arange(PAGE * hd, device=e.device)
+    for s, slot in planted.items():
+        pos = lens[s] + slot
+        for h, bad in enumerate((float("nan"), float("-inf"))):
+            for d in dims_of[h]:
+                here = (at // (PAGE * 16) == d // 16) & (at // 64 % 4 == pos % PAGE // 4) & (at // 4 % 16 == d % 16) & (at % 4 == pos % 4)
+                assert int(here.sum()) == 1
+                pools[0][1, int(table[s, pos // PAGE]), h, 1, here] = bad
+    k, v = (x.double().cpu() for x in unpack(pools[0], 1, kv, hd))
+    out = _attend(torch, e, table, lens, starts, q, 0, 1, True, 64).double().cpu()
+    half = heads // kv
+    for s, slot in planted.items():
+        pos = lens[s] + slot
+        assert torch.isnan(v[table[s, pos // PAGE], pos % PAGE, 0, list(dims_of[0])]).all() and torch.isneginf(v[table[s, pos // PAGE], pos % PAGE, 1, list(dims_of[1])]).all()
+        want = got[s].clone()
+        for d in dims_of[0]:
+            want[slot:, :half, d] = float("nan")
+        for d in dims_of[1]:
+            want[slot:, half: 2 * half, d] = float("-inf")
+        assert torch.equal(torch.nan_to_num(out[s], nan=1e9), torch.nan_to_num(want, nan=1e9)), (s, slot)
+    e.close()
+
+
+@pytest.mark.parametrize("way", [APART, ONCE])
 def test_attention_on_a_stream_and_in_a_graph(way, monkeypatch):
     torch = _torch()
     monkeypatch.setenv("DFLASH_GROUP_APART", way)
