@@ -40,24 +40,35 @@ struct GroupTables {
 __host__ __device__ __forceinline__ int group_tile_slots(int n_seqs, int rows, int tile, int n_groups) { return (int)((long long)n_seqs * rows / tile) + n_groups; }
 
 // Groups -> tiles, a workgroup a sequence: which group it belongs to (the caller's starts as their running maximum, inside the batch; the first is 0), what it has in
-// common with the group's first sequence, and, of that one, the group's tiles.  n_groups = 1 needs no starts.
+// common with the group's first sequence, and, of that one, the group's tiles.  n_groups = 1 needs no starts.  A chain of
+// loads: the sequence's own entries are asked for while the starts are on their way (the launch in front of 32 x 1 rows behind 8192 tokens 4.1 -> 3.4 us).
 __global__ __launch_bounds__(256) void group_plan_kernel(SeqGeom geo, const int32_t* __restrict__ starts, int n_groups, int n_seqs, int rows, int tile, int expected,
                                                       GroupTables gt) {
+  constexpr int AHEAD = 4;   // entries of the sequence's row that a thread asks for before it knows the group
   __shared__ int s_next, s_start, s_end, s_after, s_pages;
   const int t = threadIdx.x, s = blockIdx.x, mpps = geo.max_pages_per_seq;
+  const int32_t* row = geo.block_table + (size_t)s * mpps;
+  const int len = geo.seq_lens[s];
+  int ids[AHEAD];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) ids[k] = row[min(t + 256 * k, mpps - 1)];
   if (t == 0) {
     s_next = s_after = n_groups;   // the first groups whose starts lie behind this sequence and behind the group's end
     s_start = 0;
     s_end = n_seqs;
     s_pages = mpps;
   }
+  auto first_behind = [&](int at, int* to) {   // of the groups whose starts lie behind `at`; a wavefront's lanes ask with one atomic
+    for (int i0 = 0; i0 < n_groups; i0 += 256) {
+      const int i = i0 + t;
+      const unsigned long long behind = __ballot(i > 0 && i < n_groups && starts[min(i, n_groups - 1)] > at);
+      if (behind && (t & 63) == 0) atomicMin(to, i + __ffsll(behind) - 1);
+      if (behind) break;
+    }
+  };
   __syncthreads();
   if (n_groups > 1) {
-    for (int i = 1 + t; i < n_groups; i += 256)
-      if (starts[i] > s) {
-        atomicMin(&s_next, i);
-        break;
-      }
+    first_behind(s, &s_next);
     __syncthreads();
     const int next = s_next;
     for (int i = t; i < n_groups; i += 256) {
@@ -67,21 +78,22 @@ __global__ __launch_bounds__(256) void group_plan_kernel(SeqGeom geo, const int3
       if (s == 0 && (i == 0 ? at != 0 : at < starts[i - 1] || at > n_seqs)) atomicOr(geo.status, DF_STATUS_CAPACITY);
     }
     __syncthreads();
-    for (int i = 1 + t; i < n_groups; i += 256)
-      if (starts[i] > s_end) {
-        atomicMin(&s_after, i);
-        break;
-      }
+    first_behind(s_end, &s_after);
   }
   const int g = s_next - 1, start = s_start, end = s_end;
-  const int32_t *lead = geo.block_table + (size_t)start * mpps, *row = geo.block_table + (size_t)s * mpps;
-  int most = min(mpps, min(max(geo.seq_lens[s], 0), max(geo.seq_lens[start], 0)) / DF_PAGE);
+  const int32_t* lead = geo.block_table + (size_t)start * mpps;
+  int most = min(mpps, min(max(len, 0), max(geo.seq_lens[start], 0)) / DF_PAGE);
   if (end - start == 1) most = min(most, expected / DF_PAGE);   // a sequence by itself is cut where its launch's ranges expect it
+  int theirs[AHEAD];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) theirs[k] = lead[min(t + 256 * k, mpps - 1)];
   int pages = most;
-  for (int p = t; p < pages; p += 256) {
-    const int id = lead[p];
-    if (id < 0 || id >= geo.n_pages || row[p] != id) pages = p;
-  }
+  auto look = [&](int p, int id, int mine) {
+    if (p < pages && (id < 0 || id >= geo.n_pages || mine != id)) pages = p;
+  };
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) look(t + 256 * k, theirs[k], ids[k]);
+  for (int p = t + 256 * AHEAD; p < pages; p += 256) look(p, lead[p], row[p]);
   if (pages < most) atomicMin(&s_pages, pages);
   __syncthreads();
   if (t == 0) {
