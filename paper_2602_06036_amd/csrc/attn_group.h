@@ -908,8 +908,8 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
   auto pv = [&](const u32x4& v, const u32x4& p, int mt) {
     acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), acc[mt], 0, 0, 0);
   };
-  // Probabilities of a pair.  The reference maximum is that of the sweep's first pair and stays while the exponentials' sums of a lane's keys stay below 2^60: their
-  // relative precision does not depend on it, and a float and a bf16 hold 2^127.  So a pair costs no maximum, only a look at its sum.
+  // Probabilities of a pair.  The reference maximum is that of the sweep's first pair and stays while the exponentials' sums of a lane's keys stay below 2^20: their
+  // relative precision does not depend on it, and values of 2^100 leave room for such weights.  So a pair costs no maximum, only a look at its sum.
   auto soft = [&](const f32x16& s, P& p) {
     float e[16];
 #pragma unroll
@@ -929,7 +929,7 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
   // ... and the rest of it, when the products before it are in the accumulators: a row whose sum has grown too large (or that has no maximum yet, or a NaN) gets its
   // reference from this pair, by which everything there is is rescaled
   auto settle = [&](const f32x16& s, P& p, float sum) {
-    if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p60f)) != 0ull) {
+    if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p20f)) != 0ull) {
       float mx = s[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);

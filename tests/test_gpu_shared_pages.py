@@ -286,6 +286,77 @@ def test_values_that_later_rows_see(dtype, heads, kv, hd, rows, way, monkeypatch
 
 
 @pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("dtype,hd", [("f32", 64), ("bf16", 128), ("bf16", 64), ("bf16", 80)])
+def test_large_values_behind_growing_scores(dtype, hd, way, monkeypatch):
+    """Weights that outgrow the first page's by up to 2^50 meet values of 2^90: the sums stay finite, as the rows are."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    rows, lens, shared, starts = 16, (160, 165, 190), (10,), (0,)
+    e, pools, table, n_pages, q = _case(torch, dtype, 4, 1, hd, rows, lens, shared, starts, 12)
+    pools[0][1, :, :, 1] *= 2.0 ** 90
+    for i in range(5, 10):
+        pools[0][1, int(table[0, i]), :, 0] *= 6
+    got = _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, True, dtype, 1, hd, 160)
+    assert torch.isfinite(got).all()
+    e.close()
+
+
+@pytest.mark.parametrize("dtype,heads,kv,hd,rows", [("f32", 2, 1, 16, 2), ("bf16", 4, 1, 32, 2), ("bf16", 2, 2, 48, 1)])
+def test_many_sequences_and_groups(dtype, heads, kv, hd, rows, monkeypatch):
+    """More sequences and more groups than a workgroup has threads, groups of no, one and many sequences."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", ONCE)
+    rng = np.random.RandomState(5)
+    lens = tuple(int(x) for x in rng.randint(0, 60, size=300))
+    for starts in (tuple([0, 0, 0] + sorted(int(x) for x in rng.randint(1, 300, size=277))), tuple(range(300)), (0, 290, 300)):
+        shared = tuple(int(x) for x in rng.randint(0, 4, size=len(starts)))
+        e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, shared, starts, len(starts))
+        _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, True, dtype, kv, hd, 32)
+        e.device_status()
+        e.close()
+
+
+def test_two_graphs_share_a_workspace(monkeypatch):
+    """Calls of different shapes captured into two graphs of one engine and replayed in turn, eager calls and the ledger's between them."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", ONCE)
+    from paper_2602_06036_amd import binding as B
+    rows, lens, shared, starts = 8, (170, 180, 266, 190, 40), (10, 0), (0, 4)
+    e, pools, table, n_pages, q = _case(torch, "bf16", 8, 2, 128, rows, lens, shared, starts, 9)
+    dev = e.device
+    t, n = torch.from_numpy(table).to(dev), torch.tensor(lens, dtype=torch.int32, device=dev)
+    zero, two = torch.zeros_like(n), torch.tensor(starts, dtype=torch.int32, device=dev)
+    refs = torch.from_numpy(np.bincount(table[table >= 0], minlength=n_pages).astype(np.int32)).to(dev)
+    led, tokens = e.ledger(t, n, zero, refs), torch.zeros(5, dtype=torch.int32, device=dev)
+    q3 = q[1:4, :1].contiguous()
+    outs = [torch.zeros_like(q), torch.zeros_like(q3)]
+    calls = [lambda out: B.dflash_group_attention(e, e.batch(n, t, zero, max(lens)), e.groups(two, 160), 0, 1, q, out),
+             lambda out: B.dflash_group_attention(e, e.batch(n[1:4], t[1:4], zero[1:4], max(lens)), e.groups(None, 0), 1, 0, q3, out, causal=False)]
+    graphs, side = [], torch.cuda.Stream()
+    for call, out in zip(calls, outs):
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=side):
+            call(out)
+        graphs.append(g)
+    for i in range(3):
+        q.mul_(-1.0)
+        q3.mul_(-1.0)
+        want = []
+        for call, out in zip(calls, outs):
+            want.append(torch.zeros_like(out))
+            call(want[-1])
+            out.zero_()
+        graphs[i % 2].replay()
+        B.dflash_pages_reserve(e, led, tokens)
+        graphs[1 - i % 2].replay()
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want):
+            assert torch.equal(out, w) and torch.isfinite(w).all()
+    e.close()
+
+
+@pytest.mark.parametrize("way", [APART, ONCE])
 def test_attention_on_a_stream_and_in_a_graph(way, monkeypatch):
     torch = _torch()
     monkeypatch.setenv("DFLASH_GROUP_APART", way)
