@@ -149,6 +149,19 @@ def test_attention_over_long_contexts(dtype, heads, kv, hd, rows, S, pages, own,
     e.close()
 
 
+@pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv,hd,rows", [(12, 1, 64, 7), (40, 1, 128, 3), (32, 1, 128, 16), (64, 1, 64, 16), (24, 2, 128, 9)])
+def test_more_than_64_rows_a_sequence(heads, kv, hd, rows, causal, way, monkeypatch):
+    """Own parts of several tiles, whose borders fall between the heads of a slot."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    lens, shared, starts = (70, 83, 64, 0, 31), (4, 0), (0, 3)
+    e, pools, table, n_pages, q = _case(torch, "bf16", heads, kv, hd, rows, lens, shared, starts, heads + rows)
+    _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, causal, "bf16", kv, hd, 64)
+    e.close()
+
+
 @pytest.mark.parametrize("hd", [32, 64, 96, 128])
 @pytest.mark.parametrize("pages", [1, 2, 3, 4, 5, 6, 7, 8, 9, 11, 12, 63, 64, 65, 67, 129, 131])
 def test_tiles_over_prefix_lengths(hd, pages, monkeypatch):
