@@ -146,7 +146,7 @@ inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, i
       const int o = (po + ns - 1) / ns;
       const double longest = std::max(on_cu > 1 ? shared * on_cu * p : alone * on_cu * p, own_alone * o + own_fixed) + ends;
       const double all = (wgs * shared * p + b * ns * (own * 0.5 * o + own_fixed)) / 256 + filled;   // own parts: half of the longest one's keys on average
-      const double behind = few && wgs >= 512 ? 6.0 : 0.0;   // short own parts run beside prefix ranges that leave them room, else after them
+      const double behind = wgs < 512 ? 0.0 : few ? 6.0 : 8.0;   // own parts run beside prefix ranges that leave them room, else after them
       const double t = std::max(longest, all) + round * ((wgs + b * ns + 511) / 512 - 1) + behind + join * all_rows * (np + ns);
       if (t < best.us) best = {np, ns, t};
     }
