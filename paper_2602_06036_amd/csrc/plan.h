@@ -118,8 +118,8 @@ inline bool attention_by_tiles(int tiles, int blocks, int head_groups, int cache
 // that has two workgroups; own parts `own_alone` and `own`, of few rows (up to 16: one block, bound by its pages) less.  Ramps and ends: `ends` for the longest workgroup, `filled`
 // where others fill them, `round` for each further round of own parts; `join` for a row of a further range, written and read.  Launches of 32 x 1 row behind 8192
 // shared and 326 own tokens, prefix ranges 4, 8, 16, 32: 60, 35, 24, 20; 16 x 16 rows behind 1968 and 600, ranges (prefix, own) (2, 1) 36, (4, 1) 30, (4, 2) 28,
-// (6, 2) 36, (8, 4) 39; 64 x 4 behind 4096 and 64, prefix ranges 4, 8: 39.7, 41.9, 32 x 4
-// behind 8192 and 500, 8, 14, 16: 41, 42, 48; 32 x 16 behind 16384 and 800 (2, 1) 244, (3, 1) 209, (4, 1) 198; 4 x 16 behind 4096 and 64, 8, 16, 32: 21, 19, 27.
+// (6, 2) 36, (8, 4) 39; 64 x 4 behind 4096 and 64, prefix ranges 4, 8: 39.7, 41.9; 32 x 4 behind 8192 and 500, 8, 14,
+// 16: 41, 42, 48; 32 x 16 behind 16384 and 800 (2, 1) 244, (3, 1) 209, (4, 1) 198; 4 x 16 behind 4096 and 64, 8, 16, 32: 21, 19, 27.
 struct GroupSplits {
   int prefix, own;
   double us;      // estimated time of the launch
@@ -146,7 +146,7 @@ inline GroupSplits group_plan(int tiles, int n_seqs, int rows, int n_kv_heads, i
       const int o = (po + ns - 1) / ns;
       const double longest = std::max(on_cu > 1 ? shared * on_cu * p : alone * on_cu * p, own_alone * o + own_fixed) + ends;
       const double all = (wgs * shared * p + b * ns * (own * 0.5 * o + own_fixed)) / 256 + filled;   // own parts: half of the longest one's keys on average
-      const double behind = wgs < 512 ? 0.0 : few ? 6.0 : 8.0;   // own parts run beside prefix ranges that leave them room, else after them
+      const double behind = wgs < 512 ? 0.0 : few ? 6.0 : 8.0;   // own parts run beside prefix ranges that leave them room, else after them (64 x 8 behind 4096 and 200: a call 83 us without, 78.5)
       const double t = std::max(longest, all) + round * ((wgs + b * ns + 511) / 512 - 1) + behind + join * all_rows * (np + ns);
       if (t < best.us) best = {np, ns, t};
     }
