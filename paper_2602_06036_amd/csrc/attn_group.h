@@ -152,7 +152,8 @@ __device__ __forceinline__ bool group_work(GroupWork& w, int& kvh, const SeqGeom
   }
   i -= n_prefix;
   const int split = i % ga.own_splits, tile = i / ga.own_splits % ga.own_tiles, s = i / (ga.own_splits * ga.own_tiles);
-  const int len = max(geo.seq_lens[s], 0), n_tok = min(len + geo.block_size, geo.max_pages_per_seq * DF_PAGE);
+  const int cap = geo.max_pages_per_seq * DF_PAGE;   // a length beyond the block-table row counts as that (whatever it is, its sum with the block stays a number of tokens)
+  const int len = min(max(geo.seq_lens[s], 0), cap), n_tok = min(len + geo.block_size, cap);
   int first = 0;
   if (ga.prefix_splits) {
     const int2 g = gt.group[s];

@@ -213,6 +213,28 @@ def test_a_long_context_by_itself(dtype, heads, kv, hd, rows, lens, monkeypatch)
     e.close()
 
 
+@pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("dtype,heads,kv,hd", [("f32", 4, 2, 64), ("bf16", 4, 2, 128), ("bf16", 4, 2, 80), ("bf16", 64, 2, 64)])
+def test_lengths_beyond_the_block_table(dtype, heads, kv, hd, way, monkeypatch):
+    """Lengths on the device that no block-table row covers, up to the largest integer: the rows see every page of their block-table row and nothing else."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    from paper_2602_06036_amd import binding as B
+    rows, lens, shared, starts = 2, (70, 84, 66, 20, 75), (4, 0), (0, 3)
+    e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, shared, starts, 13)
+    pools[0].copy_(torch.nan_to_num(pools[0], nan=0.5))          # pages that the longer lengths reach into
+    cap, dev = table.shape[1] * PAGE, e.device
+    for causal in (True, False):
+        given = (2 ** 31 - 1, 84, 2 ** 31 - 1 - rows, cap - 1, cap + 3)
+        t, n, out = torch.from_numpy(table).to(dev), torch.tensor(given, dtype=torch.int32, device=dev), torch.full_like(q, 7.0)
+        B.dflash_group_attention(e, e.batch(n, t, torch.zeros_like(n), 84), e.groups(torch.tensor(starts, dtype=torch.int32, device=dev), 64), 0, 1, q, out, causal=causal)
+        torch.cuda.synchronize()
+        k, v = (x.double().cpu() for x in unpack(pools[0], 1, kv, hd))
+        ref, slack, wabs = attention64(q.double().cpu(), k, v, table, given, causal, n_pages)
+        assert bool(((out.double().cpu() - ref).abs() <= allowed(ref, slack, wabs, dtype)).all())
+    e.close()
+
+
 @pytest.mark.parametrize("dtype,heads,kv,hd", [("f32", 4, 4, 64), ("bf16", 8, 2, 128)])
 def test_any_grouping_gives_the_same_rows(dtype, heads, kv, hd, monkeypatch):
     """Groups that do not match what is shared; starts that are not raise the status."""
