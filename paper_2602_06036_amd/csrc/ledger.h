@@ -33,7 +33,7 @@ __device__ __forceinline__ bool page_in(const Ledger& l, int id) { return id >= 
 // rows that are read are not written.
 __global__ __launch_bounds__(256) void pages_fork_kernel(Ledger l, ForkRows rows) {
   const int from = rows.parent[blockIdx.y], to = rows.child[blockIdx.y], count = rows.count[blockIdx.y], p = blockIdx.x * 256 + threadIdx.x;
-  const int n = l.seq_lens[from], held = (max(n, 0) + DF_PAGE - 1) / DF_PAGE;
+  const int n = l.seq_lens[from], held = n <= 0 ? 0 : (n - 1) / DF_PAGE + 1;   // (n + 15 need not fit)
   if (p == 0) {
     l.seq_lens[to] = n;
     l.anchor[to] = l.anchor[from];

@@ -591,6 +591,24 @@ def test_pages_beyond_four_gigabytes(way, monkeypatch):
     e.close()
 
 
+@pytest.mark.parametrize("length", [2 ** 31 - 1, 2 ** 31 - 15, 5 * PAGE, 4 * PAGE + 1, 4 * PAGE, 0, -3])
+def test_fork_of_any_length(length):
+    """Lengths beyond the block-table row, up to the largest integer: all of its pages are shared, and the status says so."""
+    torch = _torch()
+    from paper_2602_06036_amd import binding as B
+    p = Pair(torch, "f32", dims(1, 2, 1, 32), dims(1, 2, 1, 32), 3, 4, 12, 3)
+    p.reserve([4 * PAGE, 20])
+    p.set_lens([length, 20])
+    p.fork([0], [2])
+    if length > 4 * PAGE:
+        with pytest.raises(B.DFlashError) as err:
+            p.e.device_status()
+        assert err.value.code == B.DFLASH_ECAPACITY
+    else:
+        p.e.device_status()
+    p.e.close()
+
+
 def test_too_few_pages_and_too_short_rows():
     torch = _torch()
     p = Pair(torch, "f32", dims(1, 2, 1, 32), dims(1, 2, 1, 32), 7, 6, 12, 6)
