@@ -187,6 +187,7 @@ class Engine:
             self.target_blob = torch.empty(tb, dtype=torch.uint8, device=self.device)
             self.draft_blob = torch.empty(db, dtype=torch.uint8, device=self.device)
         self.ctx = None
+        self.groups_set = None                     # what dflash_set_groups was given last
 
     # ---- weights -------------------------------------------------------------------------------
     def pack_target_head(self, embed, lm_head, final_gain):
@@ -248,7 +249,9 @@ class Engine:
     def groups(self, group_starts: Optional[torch.Tensor], prefix_len: int) -> Groups:
         """Groups of consecutive sequences that begin with the same pages; group_starts None: the whole batch is one."""
         assert group_starts is None or (group_starts.dtype == torch.int32 and group_starts.dim() == 1 and group_starts.device == self.target_pool.device)
-        return Groups(1 if group_starts is None else int(group_starts.shape[0]), int(prefix_len), _ptr(group_starts))
+        g = Groups(1 if group_starts is None else int(group_starts.shape[0]), int(prefix_len), _ptr(group_starts))
+        g.keep = group_starts              # the struct holds an address only
+        return g
 
     def profile_enable(self, on: bool):
         _check(self.l.dflash_profile_enable(self.ctx, int(on)), self.ctx)
@@ -378,9 +381,10 @@ def dflash_pages_compact(e: Engine, ledger: Ledger, n_live: Optional[torch.Tenso
 
 
 def dflash_set_groups(e: Engine, groups: Optional[Groups]):
-    """From now on the step's attention reads what the sequences of a group share once (None: per sequence again).  The tensor behind
-    groups.group_starts must outlive its use."""
+    """From now on the step's attention reads what the sequences of a group share once (None: per sequence again).  The engine keeps the tensor behind
+    groups.group_starts until other groups or None are set; a captured graph needs it as long as the graph is replayed."""
     _check(e.l.dflash_set_groups(e.ctx, C.byref(groups) if groups is not None else None), e.ctx)
+    e.groups_set = groups
 
 
 def dflash_group_attention(e: Engine, batch: Batch, groups: Groups, pool: int, layer: int, q: torch.Tensor, out: torch.Tensor, causal: bool = True):

@@ -719,6 +719,41 @@ def test_refusals():
     p.e.close()
 
 
+def test_groups_that_are_set_keep_their_starts():
+    """The step's calls read the starts whenever they run: the tensor lives as long as the groups are set, and no longer; a refused call changes nothing."""
+    torch = _torch()
+    import gc
+    import weakref
+    from paper_2602_06036_amd import binding as B
+    m = dims(1, 2, 1, 32)
+    e, _ = _engine("f32", m, m, 4, 4, 4, 8)
+
+    def given(n, prefix=0):
+        starts = torch.arange(n, dtype=torch.int32, device=e.device)
+        return e.groups(starts, prefix), weakref.ref(starts)
+
+    def alive(ref):
+        gc.collect()
+        return ref() is not None
+
+    g, first = given(2)
+    B.dflash_set_groups(e, g)
+    del g
+    assert alive(first)
+    g, other = given(3, -1)
+    with pytest.raises(B.DFlashError):
+        B.dflash_set_groups(e, g)
+    del g
+    assert alive(first) and not alive(other)
+    g, second = given(3)
+    B.dflash_set_groups(e, g)
+    del g
+    assert alive(second) and not alive(first)
+    B.dflash_set_groups(e, None)
+    assert not alive(second)
+    e.close()
+
+
 # ---- in the step --------------------------------------------------------------------------------------------------------
 def _shared_model(w, wt, wd, prompts, children, steps):
     """A GpuModel whose sequences come out of prefilled prompts by forking; returns it with its ledger tensors."""
