@@ -909,8 +909,9 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
   auto pv = [&](const u32x4& v, const u32x4& p, int mt) {
     acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), acc[mt], 0, 0, 0);
   };
-  // Probabilities of a pair.  The reference maximum is that of the sweep's first pair and stays while the exponentials' sums of a lane's keys stay below 2^20: their
-  // relative precision does not depend on it, and values of 2^100 leave room for such weights.  So a pair costs no maximum, only a look at its sum.
+  // Probabilities of a pair.  The reference maximum is that of the sweep's first pair and stays while a lane's sum of exponentials, over all its keys so far, is at most
+  // 2^20: the relative precision does not depend on it, and a row's weights are then at most 2^21 in all, which leaves room for values of 2^100.  So a pair costs no maximum,
+  // only a look at the sum.
   auto soft = [&](const f32x16& s, P& p) {
     float e[16];
 #pragma unroll
@@ -927,22 +928,24 @@ __device__ __forceinline__ void group_sweep_tile(char* s_raw, const GroupWork& w
       }
     return sum;
   };
-  // ... and the rest of it, when the products before it are in the accumulators: a row whose sum has grown too large (or that has no maximum yet, or a NaN) gets its
-  // reference from this pair, by which everything there is is rescaled
+  // ... and the rest of it, when the products before it are in the accumulators: a row whose sum has grown too large (or that has no maximum yet) gets another
+  // reference, by which everything there is is rescaled: this pair's maximum, or, where that is not far above the old one and many keys have made the sum, one 2^16 above it
   auto settle = [&](const f32x16& s, P& p, float sum) {
-    if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p20f)) != 0ull) {
+    constexpr float most = 0x1p20f;
+    if (__builtin_amdgcn_ballot_w64(l_run + sum > most || sum != sum) != 0ull) {   // (nothing above -inf yet: the sum is infinite or a NaN)
       float mx = s[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-      const LanePair x = lane_swap32(mx, mx);
+      const LanePair x = lane_swap32(mx, mx), all = lane_swap32(l_run + sum, l_run + sum);
       mx = fmaxf(x.lo, x.hi) * scale2;
-      if (mx > m_run + 8.f) {
-        const float corr = m_run == -INFINITY ? 0.f : exp2f(m_run - mx);
+      if (m_run == -INFINITY ? mx > m_run : all.lo > most || all.hi > most) {
+        const float ref = mx > m_run + 8.f ? mx : m_run + 16.f;
+        const float corr = m_run == -INFINITY ? 0.f : exp2f(m_run - ref);
         l_run *= corr;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) acc[mt] *= corr;
-        m_run = mx;
-        neg_m = -mx;
+        m_run = ref;
+        neg_m = -ref;
       }
       const float again = neg_m;
       if (m_run == -INFINITY) neg_m = 0.f;   // nothing above -inf yet: exp2(-inf - 0) = 0

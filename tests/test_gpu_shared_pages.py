@@ -336,6 +336,29 @@ def test_large_values_behind_growing_scores(dtype, hd, way, monkeypatch):
     e.close()
 
 
+@pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("dtype,hd,key", [("bf16", 32, 7.75), ("bf16", 64, 11.0), ("bf16", 96, 13.375), ("bf16", 128, 15.5), ("bf16", 80, 12.25), ("f32", 64, 11.0)])
+def test_large_values_behind_a_long_context(dtype, hd, key, way, monkeypatch):
+    """One range of 513 pairs of pages whose first pair scores 15.8 powers of two below all others (8 * key / sqrt(hd) * log2 e): no pair is far above another, but together their
+    weights pass 2^29, and meet values of 2^100: the sums stay finite, as the rows are."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    rows, pages, starts = 16, 1025, (0,)
+    lens = (pages * PAGE + 3, pages * PAGE)
+    assert 15.7 < 8 * key / hd ** 0.5 * 1.4427 < 16
+    e, pools, table, n_pages, q = _case(torch, dtype, 4, 1, hd, rows, lens, (pages,), starts, 14)
+    pools[0][1, :, :, 1] = pools[0][1, :, :, 1].abs() * 2.0 ** 100
+    q.zero_()
+    q[..., 0] = 8.0
+    at = torch.arange(PAGE * hd, device=e.device)
+    first = (at // 128 == 0) & (at % 8 == 0)                 # dim 0 of K
+    for i in range(pages):
+        pools[0][1, int(table[0, i]), :, 0, first] = 0.0 if i < 2 else key
+    got = _compare(torch, e, pools, table, lens, starts, n_pages, q, rows, True, dtype, 1, hd, 0)
+    assert torch.isfinite(got).all()
+    e.close()
+
+
 @pytest.mark.parametrize("dtype,heads,kv,hd,rows", [("f32", 2, 1, 16, 2), ("bf16", 4, 1, 32, 2), ("bf16", 2, 2, 48, 1)])
 def test_many_sequences_and_groups(dtype, heads, kv, hd, rows, monkeypatch):
     """More sequences and more groups than a workgroup has threads, groups of no, one and many sequences."""
