@@ -361,15 +361,44 @@ struct PairFrags<float, HD> {
   }
 };
 
-// four dims of a finished row (m_hq: its place among the query rows of all heads)
+// four dims of a finished row (m_hq: its place among the query rows of all heads).  True: one of them is not finite, see below
 template <typename T>
-__device__ __forceinline__ void group_store(const GroupArgs& ga, size_t m_hq, int hd, int d, float4 o, float l) {
+__device__ __forceinline__ bool group_store(const GroupArgs& ga, size_t m_hq, int hd, int d, float4 o, float l) {
   const float by = l != 0.f ? l : INFINITY;   // no visible key: zeros
   o = make_float4(o.x / by, o.y / by, o.z / by, o.w / by);
   T* out = static_cast<T*>(ga.out);
   if (ga.operand) Act<T>::store4(out, (int)(m_hq / ga.n_q_heads), (int)(m_hq % ga.n_q_heads) * hd + d, ga.n_q_heads * hd, o);
   else if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out + m_hq * hd + d) = make_uint2(pack_bf16_pair(o.x, o.y), pack_bf16_pair(o.z, o.w));
   else *reinterpret_cast<float4*>(out + m_hq * hd + d) = o;
+  return l > 0.f && (not_finite(o.x) || not_finite(o.y) || not_finite(o.z) || not_finite(o.w));   // (a NaN among the scores: the row is NaN)
+}
+// Four dims of a finished row, some of them not finite: those whose V is not finite in a key that the row sees are what such elements add up to.  The products need not have made
+// that of them (a weight that is 0 in fp32; hi * inf + lo * inf with a lo of 0 or below it), and in which products they stand depends on how the keys are cut, which the row must not.
+template <typename T>
+__device__ __forceinline__ void group_store_not_finite(const SeqGeom& geo, const GroupArgs& ga, const T* pool, int m_hq, int hd, int d) {
+  const int m = m_hq / ga.n_q_heads, hq = m_hq % ga.n_q_heads, s = m / geo.block_size, cap = geo.max_pages_per_seq * DF_PAGE;
+  const int n_see = min(min(max(geo.seq_lens[s], 0), cap) + (ga.causal ? m % geo.block_size + 1 : geo.block_size), cap);
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int p = 0; p * DF_PAGE < n_see; ++p) {
+    const int id = geo.block_table[(size_t)s * geo.max_pages_per_seq + p];
+    if (id < 0 || id >= geo.n_pages) continue;
+    const T* v = pool + kv_head_base(ga.layer, geo.n_pages, id, ga.n_kv_heads, hq / (ga.n_q_heads / ga.n_kv_heads), hd) + DF_PAGE * hd + v_in_page(0, d);
+#pragma unroll
+    for (int k = 0; k < DF_PAGE; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = widen(v[k / 4 * 64 + i * 4 + k % 4]);
+        sum[i] += p * DF_PAGE + k < n_see && not_finite(x) ? x : 0.f;
+      }
+  }
+  T* out = static_cast<T*>(ga.out);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (!not_finite(sum[i])) continue;
+    if (ga.operand) Act<T>::store(out, m, hq * hd + d + i, ga.n_q_heads * hd, sum[i]);
+    else out[(size_t)m_hq * hd + d + i] = Store<T>::from(sum[i]);
+  }
 }
 
 // fp32, and bf16 with other head dims.  A wavefront sweeps 16 rows, pairs of pages straight from memory; the workgroup's four share its rows (up to 64) or, where there
@@ -483,8 +512,12 @@ __global__ __launch_bounds__(256, 2) void group_attn_kernel(const T* __restrict_
   }
   if (!valid) return;
   if (ga.out) {
+    bool again = false;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) group_store<T>(ga, m_hq, HD, dt * 16 + 4 * g, make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]), l);
+    for (int dt = 0; dt < DT; ++dt) again |= group_store<T>(ga, m_hq, HD, dt * 16 + 4 * g, make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]), l);
+    if (again)
+#pragma unroll 1
+      for (int dt = 0; dt < DT; ++dt) group_store_not_finite(geo, ga, pool, (int)m_hq, HD, dt * 16 + 4 * g);
     return;
   }
   const size_t pr = m_hq * (ga.prefix_splits + ga.own_splits) + w.part;
@@ -510,7 +543,8 @@ struct KeySplit {
   static constexpr int bytes(int rb) { return RING + rb * KT * 1024 > ROWS_AT(rb) + rb * 16 * 4 ? RING + rb * KT * 1024 : ROWS_AT(rb) + rb * 16 * 4; }
 };
 
-template <int HD, int RB>
+// DIRECT: the launch may be one whose rows are finished here (ga.out)
+template <int HD, int RB, bool DIRECT>
 __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w, int kvh, const bf16_t* __restrict__ q,
                                                  const bf16_t* __restrict__ pool, const SeqGeom& geo, const GroupArgs& ga, float* __restrict__ part_o,
                                                  float2* __restrict__ part_ml) {
@@ -791,6 +825,7 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
   }
   __syncthreads();
   const int parts = ga.prefix_splits + ga.own_splits;
+  bool again = false;
   for (int i = threadIdx.x; i < w.n_rows * (HD / 4); i += 64 * NW) {
     const int r = i / (HD / 4), d4 = i % (HD / 4);
     const size_t pr = (size_t)s_row[r] * parts + w.part;
@@ -807,13 +842,17 @@ __device__ __forceinline__ void group_sweep_keys(char* s_raw, const GroupWork& w
     };
     const float4 o = *reinterpret_cast<const float4*>(&s_o[0][r][d4 * 4]), o1 = *reinterpret_cast<const float4*>(&s_o[1][r][d4 * 4]);
     const float4 x = make_float4(o.x + o1.x, o.y + o1.y, o.z + o1.z, o.w + o1.w);
-    if (ga.out) {
-      group_store<bf16_t>(ga, s_row[r], HD, d4 * 4, x, sum().y);
-      continue;
-    }
+    if constexpr (DIRECT)
+      if (ga.out) {
+        again |= group_store<bf16_t>(ga, s_row[r], HD, d4 * 4, x, sum().y);
+        continue;
+      }
     *reinterpret_cast<float4*>(part_o + pr * HD + d4 * 4) = x;
     if (d4 == 0) part_ml[pr] = sum();
   }
+  if (again)
+#pragma unroll 1
+    for (int i = threadIdx.x; i < w.n_rows * (HD / 4); i += 64 * NW) group_store_not_finite(geo, ga, pool, s_row[i / (HD / 4)], HD, i % (HD / 4) * 4);
 }
 
 // ---- bf16, head dims 32, 64, 96 and 128: tiles of 128 query rows of the prefix part -----------------------------------------------------
@@ -1065,16 +1104,17 @@ __global__ __launch_bounds__(256, 2) void group_attn_mfma_kernel(const bf16_t* _
   GroupWork w;
   int kvh;
   if (!group_work<256>(w, kvh, geo, ga, gt, part_ml)) return;
-  if (w.part >= ga.prefix_splits) return group_sweep_keys<HD, RBO>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
+  constexpr bool DIRECT = RBP == RBO;   // (every sequence by itself: group_attn_launch)
+  if (w.part >= ga.prefix_splits) return group_sweep_keys<HD, RBO, DIRECT>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
   if constexpr (RBP == 0) group_sweep_tile<HD>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
-  else group_sweep_keys<HD, RBP>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
+  else group_sweep_keys<HD, RBP, DIRECT>(s_raw, w, kvh, q, pool, geo, ga, part_o, part_ml);
 }
 
 // Parts -> rows, a wavefront a row, four dims a lane, as many parts side by side as that leaves room for (two of 128 dims) and four times that on their way.  A part
 // without keys (its sum is exactly 0) is left out.
 template <typename T>
-__global__ __launch_bounds__(256) void group_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, GroupArgs ga, int hd,
-                                                          int n_rows) {
+__global__ __launch_bounds__(256) void group_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, const T* __restrict__ pool, SeqGeom geo, GroupArgs ga,
+                                                          int hd, int n_rows) {
   const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // m * n_q_heads + hq
   if (row >= n_rows) return;
   const int parts = ga.prefix_splits + ga.own_splits;
@@ -1108,7 +1148,7 @@ __global__ __launch_bounds__(256) void group_merge_kernel(const float* __restric
     o.x += __shfl_xor(o.x, k, 64); o.y += __shfl_xor(o.y, k, 64); o.z += __shfl_xor(o.z, k, 64); o.w += __shfl_xor(o.w, k, 64);
   }
   if (!mine || sub > 0) return;
-  group_store<T>(ga, row, hd, d, o, L);
+  if (group_store<T>(ga, row, hd, d, o, L)) group_store_not_finite(geo, ga, pool, row, hd, d);
 }
 
 // whether the prefix part goes by tiles of 128 rows: the groups have more rows, on average, than a key-split workgroup

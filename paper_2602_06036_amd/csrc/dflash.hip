@@ -597,7 +597,7 @@ struct Engine {
     if (sh.apart) return;
     ProfScope prof(c, st, DFLASH_PROF_ATTN_MERGE, 0.0);
     ga.out = out;
-    hipLaunchKernelGGL(group_merge_kernel<T>, dim3((n_rows + 3) / 4), dim3(256), 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), ga, m.head_dim, n_rows);
+    hipLaunchKernelGGL(group_merge_kernel<T>, dim3((n_rows + 3) / 4), dim3(256), 0, st, ws<float>(c->ws.part_o), ws<float2>(c->ws.part_ml), pool, geo, ga, m.head_dim, n_rows);
     check();
   }
   int attend(const dflash_dims& m, const T* pool, int layer, const dflash_batch* b, const dflash_groups& g, int rows, bool causal, const void* q, void* out) {

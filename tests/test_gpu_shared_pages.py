@@ -321,6 +321,50 @@ def test_values_that_later_rows_see(dtype, heads, kv, hd, rows, way, monkeypatch
 
 
 @pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,heads,kv,hd,rows", [("f32", 4, 2, 64, 12), ("bf16", 4, 2, 128, 12), ("bf16", 32, 2, 64, 4), ("bf16", 4, 2, 80, 12), ("bf16", 8, 2, 96, 1)])
+def test_values_that_are_not_finite_under_any_grouping(dtype, heads, kv, hd, rows, causal, way, monkeypatch):
+    """Infinities and NaN in V rows of committed keys, in the shared pages, behind them and next to the block, one of a key whose weight is 0 in fp32: the dims that have them
+    are what the definition says, in the rows that see them, however the batch is cut; the other dims are what they were."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    lens, shared, starts = (170, 184, 164, 120, 127), (6, 3), (0, 3)
+    e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, shared, starts, 15)
+    q[..., 0] = 8.0
+    at = torch.arange(PAGE * hd, device=e.device)
+
+    def element(pos, d):
+        return (at // (PAGE * 16) == d // 16) & (at // 64 % 4 == pos % PAGE // 4) & (at // 4 % 16 == d % 16) & (at % 4 == pos % 4)
+
+    far = (at // 128 == 0) & (at % 8 == 0) & (at // 8 % PAGE == 7)            # dim 0 of K of the key 7 of a page
+    pools[0][1, int(table[0, 2]), 0, 0, far] = -25.0 * hd ** 0.5              # its score: -200 and what the other dims give
+    ways = [(starts, 96), (starts, 0), ((0,), 48), ((0, 1, 2, 3, 4), 160), ((0, 2, 3), 96)]
+    before = [_compare(torch, e, pools, table, lens, g, n_pages, q, rows, causal, dtype, kv, hd, hint) for g, hint in ways]
+    inf, nan = float("inf"), float("nan")
+    #        sequence, position, dim, value: shared by 0 .. 2 (position < 96) or by 3 and 4 (< 48), else a sequence's own
+    plants = [(0, 2 * PAGE + 7, 1, inf), (0, 5, hd - 1, -inf), (0, 70, 6, inf), (0, 71, 6, -inf), (3, 30, 2, nan), (1, 100, 3, inf), (2, 163, 4, -inf), (2, 161, 5, inf), (4, 126, 7, inf)]
+    for s, pos, d, x in plants:
+        pools[0][1, int(table[s, pos // PAGE]), 0, 1, element(pos, d)] = x
+    want = {s: {} for s in range(5)}
+    for s, pos, d, x in plants:
+        for other in range(5):
+            if table[other, pos // PAGE] == table[s, pos // PAGE]:
+                want[other][d] = want[other].get(d, 0.0) + x
+    k, v = (x.double().cpu() for x in unpack(pools[0], 1, kv, hd))
+    ref, _, _ = attention64(q.double().cpu(), k, v, table, lens, causal, n_pages)
+    half = heads // kv
+    for (g, hint), old in zip(ways, before):
+        out = _attend(torch, e, table, lens, g, q, 0, 1, causal, hint).double().cpu()
+        for s in range(5):
+            exp = old[s].clone()
+            for d, x in want[s].items():
+                exp[:, :half, d] = x
+                assert torch.equal(torch.nan_to_num(ref[s, :, :half, d], nan=1e9), torch.nan_to_num(exp[:, :half, d], nan=1e9))
+            assert torch.equal(torch.nan_to_num(out[s], nan=1e9), torch.nan_to_num(exp, nan=1e9)), (g, hint, s)
+    e.close()
+
+
+@pytest.mark.parametrize("way", [APART, ONCE])
 @pytest.mark.parametrize("dtype,hd", [("f32", 64), ("bf16", 128), ("bf16", 64), ("bf16", 80)])
 def test_large_values_behind_growing_scores(dtype, hd, way, monkeypatch):
     """Weights that outgrow the first page's by up to 2^50 meet values of 2^90: the sums stay finite, as the rows are."""
