@@ -277,7 +277,9 @@ int dflash_set_groups(dflash_ctx *ctx, const dflash_groups *groups);
 
 /* That attention by itself: rows 0..rows-1 of every sequence of the batch, at positions seq_lens[s] .. seq_lens[s] + rows - 1, over the
  * K/V rows of one layer of a pool, their own (already there) included: causal != 0: row j sees positions up to seq_lens[s] + j, else all
- * seq_lens[s] + rows.  rows in [1, block_size] (1: plain decoding); batch->block_size is not looked at, batch->max_seq_len balances launches only.
+ * seq_lens[s] + rows.  rows in [1, block_size] (1: plain decoding).  The batch is one that the step's calls take (max_seq_len and a block within the block-table row); its
+ * block_size means nothing here, its max_seq_len balances launches only.  Entries outside the pool are keys that are not there; a sequence whose rows the block-table row does not
+ * cover raises the sticky device status, its rows see what there is.
  * q (device) [S, rows, n_q_heads, head_dim] after norm and rotation, out (device) the same shape; both in the model's dtype, contiguous, 16-byte
  * aligned.  Uses the workspace as the step's calls do. */
 int dflash_group_attention(dflash_ctx *ctx, const dflash_batch *batch, const dflash_groups *groups, int32_t pool, int32_t layer, int32_t rows,

@@ -235,6 +235,28 @@ def test_lengths_beyond_the_block_table(dtype, heads, kv, hd, way, monkeypatch):
     e.close()
 
 
+@pytest.mark.parametrize("way", [APART, ONCE])
+@pytest.mark.parametrize("dtype,heads,kv,hd,rows", [("f32", 2, 2, 64, 1), ("bf16", 8, 2, 128, 4), ("bf16", 4, 2, 80, 3), ("bf16", 64, 2, 64, 4)])
+def test_rows_beyond_the_block_table_raise_the_status(dtype, heads, kv, hd, rows, way, monkeypatch):
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", way)
+    from paper_2602_06036_amd import binding as B
+    lens, shared, starts = (40, 50), (2,), (0,)
+    e, pools, table, n_pages, q = _case(torch, dtype, heads, kv, hd, rows, lens, shared, starts, 16)
+    cap, dev = table.shape[1] * PAGE, e.device
+    t, out = torch.from_numpy(table).to(dev), torch.empty_like(q)
+    for last, fits in ((cap - rows, True), (cap - rows + 1, False), (2 ** 31 - 1, False), (50, True)):
+        n = torch.tensor((40, last), dtype=torch.int32, device=dev)
+        B.dflash_group_attention(e, e.batch(n, t, torch.zeros_like(n), 50), e.groups(None, 32), 0, 1, q, out)
+        if fits:
+            e.device_status()
+        else:
+            with pytest.raises(B.DFlashError) as err:
+                e.device_status()
+            assert err.value.code == B.DFLASH_ECAPACITY
+    e.close()
+
+
 @pytest.mark.parametrize("dtype,heads,kv,hd", [("f32", 4, 4, 64), ("bf16", 8, 2, 128)])
 def test_any_grouping_gives_the_same_rows(dtype, heads, kv, hd, monkeypatch):
     """Groups that do not match what is shared; starts that are not raise the status."""
