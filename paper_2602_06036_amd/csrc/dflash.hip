@@ -612,10 +612,11 @@ struct Engine {
     shape = shape_of(m, b, c->groups, B);
     AttnArgs aa;
     aa.n_q_heads = m.n_q_heads; aa.n_kv_heads = m.n_kv_heads; aa.head_dim = m.head_dim; aa.q_shift = q_shift;
-    if (q_shift >= 0 && attn_takes_mfma<T>(aa, B))
-      shape.apart = step_apart(shape.splits.us, b->n_seqs, m.n_kv_heads << q_shift,
-                               plan_splits(b->n_seqs, m.n_kv_heads << q_shift, std::min(b->max_seq_len + B, c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE), c->k.attn_target_wgs),
-                               c->k.group_apart);
+    const int tokens = std::min(b->max_seq_len + B, c->rt.max_pages_per_seq * DFLASH_PAGE_SIZE), head_groups = m.n_kv_heads << std::max(q_shift, 0);
+    const SplitPlan p = plan_splits(b->n_seqs, head_groups, tokens, c->k.attn_target_wgs);
+    shape.apart = q_shift >= 0 && attn_takes_mfma<T>(aa, B)
+                      ? step_apart(shape.splits.us, b->n_seqs, head_groups, p, c->k.group_apart)
+                      : step_apart_simple(shape.splits.us, b->n_seqs, shape.rows, m.n_kv_heads, m.head_dim, tokens, sizeof(T) == 2, p, c->k.group_apart);
     if (shape.apart) return;   // the step's attention as it is without groups
     groups = &c->groups;
     group_tables_of(shape, b, c->groups, B);
@@ -1289,11 +1290,8 @@ void Engine<T>::attention(const dflash_dims& m, const T* pool, int layer, const 
       hipLaunchKernelGGL(attn_short_simple_kernel<T>, dim3(B * (m.n_q_heads / m.n_kv_heads), m.n_kv_heads, S), dim3(256), 0, st, ws<T>(c->ws.q), pool,
                          geom(b), aa, ws<T>(c->ws.o));
     } else {
-      // query rows of a kv head over several workgroups while that leaves at most two of them a CU (each reads the
-      // chunk's keys for itself, so a launch that fills the chip keeps them together)
-      const int wgs = p.n_splits * m.n_kv_heads * S, rows = B * (m.n_q_heads / m.n_kv_heads);
-      const int groups = std::max(1, std::min(512 / wgs, (rows + 3) / 4));
-      hipLaunchKernelGGL(attn_partial_simple_kernel<T>, dim3(p.n_splits, m.n_kv_heads * groups, S), dim3(256), 0, st, ws<T>(c->ws.q), pool,
+      const int row_groups = simple_row_groups(p.n_splits * m.n_kv_heads * S, B * (m.n_q_heads / m.n_kv_heads));
+      hipLaunchKernelGGL(attn_partial_simple_kernel<T>, dim3(p.n_splits, m.n_kv_heads * row_groups, S), dim3(256), 0, st, ws<T>(c->ws.q), pool,
                          geom(b), aa, part_o, part_ml);
     }
     check();

@@ -174,6 +174,10 @@ inline bool step_apart(double shared_us, int n_seqs, int head_groups, SplitPlan 
   return rounds * 0.42 * p.chunk / 32 + (p.chunk >= 512 ? 13.0 : 10.0) + (p.n_splits > 1 ? 7.0 : 0.0) < shared_us + 10.0;
 }
 
+// Row groups of a launch of the plain attention kernel over n_splits ranges: query rows of a kv head go to several workgroups while that leaves at most two of them
+// a CU (each reads the range's keys for itself, so a launch that fills the chip keeps them together).
+inline int simple_row_groups(int wgs, int rows) { return std::max(1, std::min(512 / wgs, (rows + 3) / 4)); }
+
 // ---- GEMMs ----------------------------------------------------------------------------------------------
 // rows of partial results the split-K arena holds for a context of at most max_rows activation rows
 inline int arena_rows(int max_rows) { return std::max(1024, 4 * max_rows); }
@@ -392,6 +396,23 @@ inline bool fold_norm(int M, int D, int cols) { return small_f32(M, D) && (long 
 inline bool short_context(int rows, int head_dim, int max_tokens, bool bf16) {
   const int limit = !bf16 ? 1 << 16 : max_tokens <= 128 ? 512 * 112 : 1 << 17;
   return max_tokens <= 256 && (long long)rows * head_dim <= limit;
+}
+
+// step_apart where the step's own attention is the plain kernels (fp32, and bf16 head dims other than 64 and 128), which have nothing from what sequences share: a wavefront
+// sweeps its rows one after the other, 64 keys at a time, each as long as its loads take.  Times of 190 launches at 13 head dims are 6.3 us and `tile` a sweep within 5 %
+// on average (22 % at most).  The groups' merge and plan count for less than their 8 us, by what the estimate of their launch is too high at small head dims (0.95 of
+// the time at 128 dims of fp32, 1.3 at 64, about 2 at bf16's).
+// Verification of 200 batches of such models (1 to 40 sequences of 2 to 16 rows, 64 to 8000 shared and 20 to 800 own tokens), against the better of the two: 0.7 % slower on
+// average and 28 % at most, and 0.6 % and 33 % over 200 others; always without the groups 75 %, always with them 2.5 %, by the estimate of the groups' kernel sequence by
+// sequence, which does not run here, 12 % and 5.3 times at most.
+inline bool step_apart_simple(double shared_us, int n_seqs, int rows, int n_kv_heads, int head_dim, int tokens, bool bf16, SplitPlan p, int knob) {
+  if (knob == 1 || knob == 2) return knob == 1;
+  const int all_rows = n_seqs * rows * n_kv_heads, wgs = p.n_splits * n_seqs * n_kv_heads, at_once = 4 * simple_row_groups(wgs, rows);
+  const bool finished = short_context(all_rows, head_dim, tokens, bf16);   // a workgroup a row, a sweep a wavefront
+  const int sweeps = finished ? (all_rows + 511) / 512 : (rows + at_once - 1) / at_once * (p.chunk / 64);
+  const bool two = head_dim > 64;   // dims a lane
+  const double tile = bf16 ? (two ? 3.5 + 0.033 * head_dim : 2.8 + 0.026 * head_dim) : (two ? 1.8 + 0.0266 * head_dim : 2.85 + 0.012 * head_dim);
+  return 6.3 + sweeps * tile + (finished ? 0.0 : 6.5) < shared_us + (bf16 ? 0.0 : 5.0);
 }
 
 // Weight rows per tile of a four-band routed-expert item: 256 (eight wavefronts), or 128 (four) for the short matrices of an odd
