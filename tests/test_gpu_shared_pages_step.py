@@ -55,13 +55,36 @@ def _compare_step(w, prompts, children, bound):
     g.e.close()
 
 
-@pytest.mark.parametrize("dtype,heads,kv,hd,block", [("f32", 4, 4, 64, 8), ("f32", 6, 2, 48, 5), ("bf16", 8, 2, 128, 16), ("bf16", 8, 2, 64, 8), ("bf16", 4, 2, 96, 8), ("bf16", 4, 2, 80, 3)])
+@pytest.mark.parametrize("dtype,heads,kv,hd,block", [("f32", 4, 4, 64, 8), ("f32", 6, 2, 48, 5), ("bf16", 8, 2, 128, 16), ("bf16", 8, 2, 64, 8), ("bf16", 4, 2, 96, 8), ("bf16", 4, 2, 80, 3),
+                                                        ("bf16", 8, 1, 128, 16), ("bf16", 16, 2, 64, 16)])
 def test_step_attends_by_the_groups(dtype, heads, kv, hd, block, monkeypatch):
     """However small the batch, with the plan forced: every kernel of the groups, its rows as the operand of the O projection."""
     monkeypatch.setenv("DFLASH_GROUP_APART", ONCE)
     w = tiny_workload(seed=5, n_layers=2, draft_layers=1, vocab=512, block=block, n_seqs=7, ctx=(150, 150), taps=(0,), dtype=dtype, heads=heads, kv_heads=kv, hd=hd)
     prompts = [p[:n] for p, n in zip(si.make_prompts(w), (149, 77))]
     _compare_step(w, prompts, (4, 1), 1e-4 if dtype == "f32" else 2e-2)
+
+
+def test_step_of_fewer_rows_under_groups(monkeypatch):
+    """Groups set once, blocks of 16, 5, 2 and 16 rows chosen per step: every step within the model's distance of the same step without groups."""
+    torch = _torch()
+    monkeypatch.setenv("DFLASH_GROUP_APART", ONCE)
+    import paper_2602_06036_amd as dfl
+    w = tiny_workload(seed=9, n_layers=2, draft_layers=1, vocab=512, block=16, n_seqs=5, ctx=(150, 150), taps=(0,), dtype="bf16", heads=8, kv_heads=2, hd=128)
+    wt, wd = si.make_weights(w, 8)
+    g, led, groups, _ = _shared_model(w, wt, wd, [p[:n] for p, n in zip(si.make_prompts(w), (149, 77))], (2, 1), 4)
+    for block in (16, 5, 2, 16):
+        dfl.dflash_pages_reserve(g.e, led, torch.full((5,), block, dtype=torch.int32, device=g.dev))
+        snap = _snapshot(g)
+        prop = np.random.RandomState(block).randint(0, w.target.vocab - 1, size=(5, block - 1))
+        outs = []
+        for on in (True, False):
+            _restore(g, snap)
+            dfl.dflash_set_groups(g.e, groups if on else None)
+            outs.append(g.step(proposals=prop, block=block))
+        for k in ("logits_d", "logits_t"):
+            assert float(np.abs(outs[0][k] - outs[1][k]).max()) <= 4e-2 and not np.array_equal(outs[0][k], outs[1][k]), (block, k)
+    g.e.close()
 
 
 @pytest.mark.parametrize("dtype,heads,kv,hd,block,seqs,tokens", [("bf16", 8, 2, 128, 2, 40, 3000), ("bf16", 8, 2, 64, 2, 40, 3000), ("f32", 4, 4, 64, 4, 12, 1100), ("bf16", 8, 2, 96, 4, 9, 600)])
