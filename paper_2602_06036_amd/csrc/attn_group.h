@@ -5,7 +5,7 @@
 //     row r:  o = softmax(q K^T * scale) V over both parts = (sum of parts of 2^(m_i - m) o_i) / (sum of 2^(m_i - m) l_i),
 // m_i, l_i, o_i a part's reference maximum, sum of exponentials (base 2, scores times log2 e) and unnormalised output, m the largest of the maxima.  Both
 // parts are split along their keys into ranges of equal length, ranges in a fixed order in the sum, so a call repeats itself bit for bit.  A row that sees
-// no key is zeros; a NaN among its scores makes it NaN.
+// no key is zeros; a NaN among its scores makes it NaN; an infinity or NaN in a V row reaches the rows that see the key, and only them.
 //
 // What sequences share is found on the device, so a wrong grouping costs time and nothing else.
 //

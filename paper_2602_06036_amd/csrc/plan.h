@@ -120,6 +120,8 @@ inline bool attention_by_tiles(int tiles, int blocks, int head_groups, int cache
 // shared and 326 own tokens, prefix ranges 4, 8, 16, 32: 60, 35, 24, 20; 16 x 16 rows behind 1968 and 600, ranges (prefix, own) (2, 1) 36, (4, 1) 30, (4, 2) 28,
 // (6, 2) 36, (8, 4) 39; 64 x 4 behind 4096 and 64, prefix ranges 4, 8: 39.7, 41.9; 32 x 4 behind 8192 and 500, 8, 14,
 // 16: 41, 42, 48; 32 x 16 behind 16384 and 800 (2, 1) 244, (3, 1) 209, (4, 1) 198; 4 x 16 behind 4096 and 64, 8, 16, 32: 21, 19, 27.
+// All of these are of head dim 128, and so are the figures; other head dims get the same plan.  Estimates over times of the launch there: bf16 96 1.2, 32 1.8, by the plain
+// kernel fp32 128 0.95, 64 1.3, 16 2.1, bf16 80 1.8, 16 to 48 2.0 to 2.3.
 struct GroupSplits {
   int prefix, own;
   double us;      // estimated time of the launch
@@ -167,7 +169,7 @@ inline bool group_apart(double shared_us, int n_seqs, int rows, int n_kv_heads, 
 // The step's own MFMA attention of such a batch, every sequence by itself: its pages come out of the caches after the first one's reading, so it is bound by its 64-row
 // blocks' arithmetic, whatever share of them is rows.  Estimated time with its merge, against that of the groups (`shared_us`) with theirs and the plan.  Attention and merge
 // of a layer by itself and once for all, 8B shape: 32 x 16 rows behind 8192 shared and 300 own tokens 124 and 123 us, 2048 and 300 45 and 54, 16 x 16 behind 2048 and 600 41
-// and 45, 4 x 16 behind 16384 and 300 47 and 47; 32 x 4 behind 8192 and 300 120 and 58.
+// and 45, 4 x 16 behind 16384 and 300 47 and 47; 32 x 4 behind 8192 and 300 120 and 58.  (16 heads of 64, 32 x 16 behind 8192 and 300: 107 and 51, and it says apart: times a pair of head dim 128.)
 inline bool step_apart(double shared_us, int n_seqs, int head_groups, SplitPlan p, int knob) {
   if (knob == 1 || knob == 2) return knob == 1;
   const int rounds = (n_seqs * head_groups * p.n_splits + 255) / 256;
