@@ -260,8 +260,8 @@ int dflash_pages_release(dflash_ctx *ctx, const dflash_ledger *ledger, int32_t n
 int dflash_pages_compact(dflash_ctx *ctx, const dflash_ledger *ledger, int32_t *n_live, void *stream);
 
 /* How a batch is cut into groups of consecutive sequences whose block-table rows are expected to begin with the same pages.  What they do
- * have in common, committed and whole pages, is found on the device: any grouping gives the same attention, up to the order of its sums (infinities and NaN in
- * K and V rows included). */
+ * have in common, committed and whole pages, is found on the device: any grouping gives the same attention, up to the order of its sums; infinities and NaN in
+ * K and V rows included, but for a V row that is not finite of a key whose score is minus infinity. */
 typedef struct {
   int32_t n_groups;            /* in [1, n_seqs] */
   int32_t prefix_len;          /* (host) about how many tokens the sequences of a group have in common; balances launches, nothing else */
