@@ -286,6 +286,52 @@ int dflash_set_groups(dflash_ctx *ctx, const dflash_groups *groups);
 int dflash_group_attention(dflash_ctx *ctx, const dflash_batch *batch, const dflash_groups *groups, int32_t pool, int32_t layer, int32_t rows,
                            int32_t causal, const void *q, void *out, void *stream);
 
+/* ---- caches held in 4 or 8 bits ------------------------------------------------------------------
+ * A cache beside the context's pools that holds K and V rows of one model in 4 or 8 bits an element: for requests put aside and taken up again, and for attention
+ * that reads a quarter of the bytes.  Every 32 dims of a row of K or V (the last block padded with zeros) share a scale 2^(e - 127), one byte e, and have a code each:
+ * 4 bits (sign, two of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6) or 8 bits (sign, four of exponent, three of mantissa, up to 448).  e is the least at which the block's
+ * largest magnitude over its scale is at most 7 (464): no element is off by more than half a step of its code.  Codes round to nearest even.  A block with an infinity or
+ * NaN has e = 255 and reads as NaN.  data[layer][page][kv head][K codes | V codes | K scales | V scales]; with NB = ceil(head_dim / 32) blocks, b = block, d = dim in
+ * the block, key = 4 q + k of a page's 16:
+ *   K, 4 bits: [b][key][d / 2], even dim low         K, 8 bits: [d / 16][b][key][d % 16]
+ *   V, 4 bits: [q][d % 16][b][k], dim below 16 low   V, 8 bits, per pair of blocks: [q][d % 16][b % 2][k][d / 16]
+ *   scales: [key][NB, of three blocks 4]
+ * The calls below are enqueued on `stream`, read nothing back and allocate nothing; they belong to a batch whose seq_lens and block_table (row length max_pages_per_seq, as
+ * everywhere) speak of this cache's pages, 0..n_pages-1.  Rows whose page is none of those, and ranges that a call does not have, are skipped and raise the sticky
+ * device status.  Sequences of a call must not write to the same page. */
+typedef struct {
+  void *data;      /* (device) dflash_kvq_bytes() bytes, 256-byte aligned */
+  size_t bytes;    /* how many there are */
+  int32_t pool;    /* DFLASH_POOL_TARGET | DFLASH_POOL_DRAFT: whose layers, kv heads and head_dim the cache has */
+  int32_t n_pages; /* its pages */
+  int32_t k_bits, v_bits; /* 4 or 8 each */
+} dflash_kvq;
+
+/* 0 with a message in dflash_last_error(NULL) for dims or bits that there are not */
+size_t dflash_kvq_bytes(const dflash_dims *model, int32_t n_pages, int32_t k_bits, int32_t v_bits);
+
+/* Rows to the cache: k, v (device) [S, rows, n_kv_heads, head_dim] in the model's dtype (K after norm and rotation), contiguous, 16-byte aligned; row j of sequence s, for j <
+ * counts[s] (device, [S], nullable: all `rows`), goes to position seq_lens[s] + j of one layer.  Nothing else of a page changes.  seq_lens is not advanced. */
+int dflash_kvq_write(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, int32_t layer, int32_t rows, const int32_t *counts, const void *k,
+                     const void *v, void *stream);
+/* ... and back, from position starts[s] + j (device, [S]), rounded once to the model's dtype; rows behind counts[s] are left as they are.  batch->seq_lens is not looked at. */
+int dflash_kvq_read(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, int32_t layer, int32_t rows, const int32_t *starts, const int32_t *counts,
+                    void *k, void *v, void *stream);
+
+/* Attention over the cache: rows j < counts[s] (nullable: all `rows`) of sequence s at positions seq_lens[s] + j, whose own K/V rows are there already; causal != 0: row j sees
+ * positions up to seq_lens[s] + j, else all seq_lens[s] + counts[s].  rows >= 1, not bound to the context's block size: 1 is plain decoding, hundreds are a piece of a prompt.  The batch's
+ * max_seq_len bounds seq_lens (a longer sequence's last keys may be left out: sticky status).  Entries of the block table outside the cache are keys that are not there; a row that sees no key is zeros.  An infinity or NaN in a row of K or V
+ * reaches the rows that see the key, and only them.  q (device) [S, rows, n_q_heads, head_dim] after norm and rotation, out (device) the same shape; both in the model's dtype, contiguous,
+ * 16-byte aligned, not the same buffer; rows behind counts[s] are left as they are.  Uses the workspace as the step's calls do. */
+int dflash_kvq_attention(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, int32_t layer, int32_t rows, const int32_t *counts, int32_t causal,
+                         const void *q, void *out, void *stream);
+
+/* A request put aside: the first seq_lens[s] rows of every sequence, all layers of the context's pool `cache->pool`, on the pages of batch->block_table, go to the pages that
+ * table (device) [S, max_pages_per_seq] names in the cache; rows of a last page behind them become zeros.  batch->max_seq_len bounds the lengths.  dflash_kvq_unpack: the way back, from the cache's pages to
+ * the pool's (other ones as a rule): rows behind seq_lens[s] are left as they are. */
+int dflash_kvq_pack(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, const int32_t *table, void *stream);
+int dflash_kvq_unpack(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, const int32_t *table, void *stream);
+
 /* ---- per-launch timing (benchmarks) -------------------------------------------------------------
  * While enabled, every GEMM and attention launch is bracketed by a pair of HIP events on the caller's
  * stream (this slows the step down: time whole steps with profiling off).  dflash_profile_read

@@ -29,6 +29,7 @@ EXPORTS = [
     "dflash_prefill", "dflash_accept_sampled_noalloc", "dflash_kv_read", "dflash_kv_write", "dflash_profile_enable", "dflash_profile_read", "dflash_moe_stats", "dflash_moe_trace", "dflash_gemm_counts",
     "dflash_probe_hbm_read", "dflash_probe_mfma",
     "dflash_pages_fork", "dflash_pages_reserve", "dflash_pages_release", "dflash_pages_compact", "dflash_set_groups", "dflash_group_attention",
+    "dflash_kvq_bytes", "dflash_kvq_write", "dflash_kvq_read", "dflash_kvq_attention", "dflash_kvq_pack", "dflash_kvq_unpack",
 ]
 
 
@@ -60,6 +61,10 @@ class Ledger(C.Structure):
 
 class Groups(C.Structure):
     _fields_ = [("n_groups", C.c_int32), ("prefix_len", C.c_int32), ("group_starts", C.c_void_p)]
+
+
+class Kvq(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("bytes", C.c_size_t), ("pool", C.c_int32), ("n_pages", C.c_int32), ("k_bits", C.c_int32), ("v_bits", C.c_int32)]
 
 
 class DFlashError(RuntimeError):
@@ -115,9 +120,16 @@ def lib() -> C.CDLL:
         l.dflash_pages_compact.argtypes = [P, C.POINTER(Ledger), P, P]
         l.dflash_set_groups.argtypes = [P, C.POINTER(Groups)]
         l.dflash_group_attention.argtypes = [P, C.POINTER(Batch), C.POINTER(Groups), I, I, I, I, P, P, P]
+        l.dflash_kvq_bytes.restype = C.c_size_t
+        l.dflash_kvq_bytes.argtypes = [C.POINTER(Dims), I, I, I]
+        l.dflash_kvq_write.argtypes = [P, C.POINTER(Batch), C.POINTER(Kvq), I, I, P, P, P, P]
+        l.dflash_kvq_read.argtypes = [P, C.POINTER(Batch), C.POINTER(Kvq), I, I, P, P, P, P, P]
+        l.dflash_kvq_attention.argtypes = [P, C.POINTER(Batch), C.POINTER(Kvq), I, I, P, I, P, P, P]
+        l.dflash_kvq_pack.argtypes = [P, C.POINTER(Batch), C.POINTER(Kvq), P, P]
+        l.dflash_kvq_unpack.argtypes = [P, C.POINTER(Batch), C.POINTER(Kvq), P, P]
         for name in EXPORTS:
             if name not in ("dflash_target_blob_bytes", "dflash_draft_blob_bytes", "dflash_kv_pool_bytes",
-                            "dflash_workspace_bytes", "dflash_last_error"):
+                            "dflash_workspace_bytes", "dflash_last_error", "dflash_kvq_bytes"):
                 getattr(l, name).restype = C.c_int
         _lib = l
     return _lib
@@ -252,6 +264,20 @@ class Engine:
         g = Groups(1 if group_starts is None else int(group_starts.shape[0]), int(prefix_len), _ptr(group_starts))
         g.keep = group_starts              # the struct holds an address only
         return g
+
+    def kvq_bytes(self, pool: int, n_pages: int, k_bits: int, v_bits: int) -> int:
+        """Bytes of a cache of n_pages pages that holds K in k_bits and V in v_bits (4 or 8) bits an element."""
+        n = self.l.dflash_kvq_bytes(C.byref(self.td if pool == DFLASH_POOL_TARGET else self.dd), n_pages, k_bits, v_bits)
+        if n == 0:
+            _check(DFLASH_EINVAL)
+        return n
+
+    def kvq(self, data: torch.Tensor, pool: int, n_pages: int, k_bits: int, v_bits: int) -> Kvq:
+        """A cache held in 4 or 8 bits over the bytes of `data` (uint8, on the engine's device, kvq_bytes() of them; the struct keeps the tensor)."""
+        assert data.dtype == torch.uint8 and data.is_contiguous() and data.device == self.target_pool.device
+        q = Kvq(_ptr(data), data.numel(), int(pool), int(n_pages), int(k_bits), int(v_bits))
+        q.keep = data
+        return q
 
     def profile_enable(self, on: bool):
         _check(self.l.dflash_profile_enable(self.ctx, int(on)), self.ctx)
@@ -395,6 +421,60 @@ def dflash_group_attention(e: Engine, batch: Batch, groups: Groups, pool: int, l
     assert out.shape == q.shape and q.dtype == dt and out.dtype == dt
     _check(e.l.dflash_group_attention(e.ctx, C.byref(batch), C.byref(groups), pool, layer, int(q.shape[1]), int(causal), _ptr(q), _ptr(out), _stream()),
            e.ctx)
+
+
+# ---- caches held in 4 or 8 bits (same names as the C ABI) -----------------------------------------------
+def _rows_like(e: Engine, batch: Batch, cache: Kvq, heads: str, *tensors: torch.Tensor) -> int:
+    """Checks [S, rows, heads, head_dim] tensors in the model's dtype; rows."""
+    m = e.target if cache.pool == DFLASH_POOL_TARGET else e.draft
+    dt = torch.bfloat16 if e.dtype == "bf16" else torch.float32
+    for t in tensors:
+        assert t.dim() == 4 and tuple(t.shape) == (batch.n_seqs, tensors[0].shape[1], getattr(m, heads), m.head_dim) and t.dtype == dt, (tuple(t.shape), t.dtype)
+    return int(tensors[0].shape[1])
+
+
+def _counts(batch: Batch, *tensors: Optional[torch.Tensor]):
+    for t in tensors:
+        assert t is None or (t.dtype == torch.int32 and tuple(t.shape) == (batch.n_seqs,)), (t.dtype, tuple(t.shape))
+
+
+def dflash_kvq_write(e: Engine, batch: Batch, cache: Kvq, layer: int, k: torch.Tensor, v: torch.Tensor, counts: Optional[torch.Tensor] = None):
+    """Rows k, v [S, rows, n_kv_heads, head_dim] to positions seq_lens[s] .. + counts[s] - 1 (None: all rows) of one layer of the cache."""
+    rows = _rows_like(e, batch, cache, "n_kv_heads", k, v)
+    _counts(batch, counts)
+    _check(e.l.dflash_kvq_write(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _ptr(counts), _ptr(k), _ptr(v), _stream()), e.ctx)
+
+
+def dflash_kvq_read(e: Engine, batch: Batch, cache: Kvq, layer: int, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor,
+                    counts: Optional[torch.Tensor] = None):
+    """Positions starts[s] .. + counts[s] - 1 of one layer of the cache into rows k, v [S, rows, n_kv_heads, head_dim]."""
+    rows = _rows_like(e, batch, cache, "n_kv_heads", k, v)
+    _counts(batch, starts, counts)
+    _check(e.l.dflash_kvq_read(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _ptr(starts), _ptr(counts), _ptr(k), _ptr(v), _stream()), e.ctx)
+
+
+def dflash_kvq_attention(e: Engine, batch: Batch, cache: Kvq, layer: int, q: torch.Tensor, out: torch.Tensor, counts: Optional[torch.Tensor] = None,
+                         causal: bool = True):
+    """Attention of q [S, rows, n_q_heads, head_dim] at positions seq_lens[s] .. + counts[s] - 1 over one layer of the cache, into out (same shape)."""
+    rows = _rows_like(e, batch, cache, "n_q_heads", q, out)
+    _counts(batch, counts)
+    _check(e.l.dflash_kvq_attention(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _ptr(counts), int(causal), _ptr(q), _ptr(out), _stream()), e.ctx)
+
+
+def _page_table(e: Engine, batch: Batch, table: torch.Tensor):
+    assert table.dtype == torch.int32 and tuple(table.shape) == (batch.n_seqs, e.max_pages_per_seq), (table.dtype, tuple(table.shape))
+
+
+def dflash_kvq_pack(e: Engine, batch: Batch, cache: Kvq, table: torch.Tensor):
+    """The batch's cached rows, all layers, from the context's pool to the cache's pages `table` [S, max_pages_per_seq]."""
+    _page_table(e, batch, table)
+    _check(e.l.dflash_kvq_pack(e.ctx, C.byref(batch), C.byref(cache), _ptr(table), _stream()), e.ctx)
+
+
+def dflash_kvq_unpack(e: Engine, batch: Batch, cache: Kvq, table: torch.Tensor):
+    """... and from the cache's pages `table` to those of the batch's block table in the context's pool."""
+    _page_table(e, batch, table)
+    _check(e.l.dflash_kvq_unpack(e.ctx, C.byref(batch), C.byref(cache), _ptr(table), _stream()), e.ctx)
 
 
 # ---- machine probes (same names as the C ABI) -----------------------------------------------------------

@@ -22,6 +22,7 @@
 #include "gemm.h"
 #include "gemm_resid.h"
 #include "gemm_tiled.h"
+#include "kvq.h"
 #include "ledger.h"
 #include "misc.h"
 #include "moe.h"
@@ -1452,6 +1453,67 @@ bool mark_rows(std::vector<uint8_t>& seen, int n, const int32_t* rows) {
   return true;
 }
 
+// ---- caches held in 4 or 8 bits --------------------------------------------------------------------------
+size_t kvq_total(const dflash_dims& m, int n_pages, int k_bits, int v_bits) {
+  return (size_t)m.n_layers * n_pages * m.n_kv_heads * kvq_unit(kvq_blocks(m.head_dim), k_bits, v_bits);
+}
+const dflash_dims& kvq_model(const dflash_ctx* ctx, const dflash_kvq* q) { return q->pool == DFLASH_POOL_TARGET ? ctx->t : ctx->d; }
+KvqCache kvq_cache(const dflash_dims& m, const dflash_kvq* q) {
+  return KvqCache{static_cast<unsigned char*>(q->data), q->n_pages, m.n_kv_heads, m.head_dim, q->k_bits, q->v_bits};
+}
+int check_kvq(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q, const char* what) {
+  if (!q || !q->data) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: null cache", what);
+  if (q->pool != DFLASH_POOL_TARGET && q->pool != DFLASH_POOL_DRAFT) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: bad pool", what);
+  if ((q->k_bits != 4 && q->k_bits != 8) || (q->v_bits != 4 && q->v_bits != 8))
+    return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: k_bits %d and v_bits %d must be 4 or 8", what, q->k_bits, q->v_bits);
+  if (q->n_pages < 1) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: cache of %d pages", what, q->n_pages);
+  if ((uintptr_t)q->data & 255) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: the cache must be 256-byte aligned", what);
+  const size_t need = kvq_total(kvq_model(ctx, q), q->n_pages, q->k_bits, q->v_bits);
+  if (q->bytes < need) return CTX_FAIL(ctx, DFLASH_EWORKSPACE, "%s: the cache has %zu bytes, %zu needed", what, q->bytes, need);
+  if (b->n_seqs > 65535) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: more than 65535 sequences", what);
+  return DFLASH_OK;
+}
+int check_kvq_rows(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q, int layer, int rows, const char* what) {
+  const dflash_dims& m = kvq_model(ctx, q);
+  if (layer < 0 || layer >= m.n_layers) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: layer %d outside [0,%d)", what, layer, m.n_layers);
+  const int64_t cap = (int64_t)ctx->rt.max_pages_per_seq * DFLASH_PAGE_SIZE;
+  if (rows < 1) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: rows %d", what, rows);
+  if (rows > cap) return CTX_FAIL(ctx, DFLASH_ECAPACITY, "%s: %d rows, a block-table row covers %lld tokens", what, rows, (long long)cap);
+  if ((int64_t)rows * m.n_q_heads > INT32_MAX / 4) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: %d rows are too many", what, rows);
+  return DFLASH_OK;
+}
+int kvq_rows_checked(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q, int layer, int rows, const int32_t* first, const int32_t* counts, void* k, void* v,
+                     bool write, void* stream) {
+  const char* what = write ? "kvq_write" : "kvq_read";
+  int rc;
+  if ((rc = check_batch(ctx, b))) return rc;
+  if (b->n_seqs == 0) return DFLASH_OK;
+  if ((rc = check_kvq(ctx, b, q, what)) || (rc = check_kvq_rows(ctx, b, q, layer, rows, what))) return rc;
+  if (!first) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: null starts", what);
+  if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: k and v must be 16-byte aligned device buffers", what);
+  const dflash_dims& m = kvq_model(ctx, q);
+  const KvqRows a{kvq_cache(m, q), layer, b->n_seqs, rows, ctx->rt.max_pages_per_seq, first, counts, b->block_table, k, v,
+                  reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.status)};
+  (write ? kvq_write_launch : kvq_read_launch)(a, m.dtype == DFLASH_BF16, (hipStream_t)stream);
+  return launched(ctx, what);
+}
+int kvq_pages_checked(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q, const int32_t* table, bool pack, void* stream) {
+  const char* what = pack ? "kvq_pack" : "kvq_unpack";
+  int rc;
+  if ((rc = check_batch(ctx, b))) return rc;
+  if (b->n_seqs == 0) return DFLASH_OK;
+  if ((rc = check_kvq(ctx, b, q, what))) return rc;
+  if (!table) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: null table", what);
+  const int pages = (b->max_seq_len + DFLASH_PAGE_SIZE - 1) / DFLASH_PAGE_SIZE;
+  if (pages == 0) return DFLASH_OK;
+  const dflash_dims& m = kvq_model(ctx, q);
+  if (m.n_layers > 65535) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: more than 65535 layers", what);
+  const KvqPages a{kvq_cache(m, q), m.n_layers, b->n_seqs, pages, ctx->rt.max_pages_per_seq, ctx->rt.n_pages, b->seq_lens, b->block_table, table,
+                   q->pool == DFLASH_POOL_TARGET ? ctx->rt.target_kv_pool : ctx->rt.draft_kv_pool, reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.status)};
+  (pack ? kvq_pack_launch : kvq_unpack_launch)(a, m.dtype == DFLASH_BF16, (hipStream_t)stream);
+  return launched(ctx, what);
+}
+
 }  // namespace
 
 namespace {
@@ -1904,6 +1966,54 @@ int dflash_group_attention(dflash_ctx* ctx, const dflash_batch* batch, const dfl
   if (ctx->t.dtype == DFLASH_BF16)
     return Engine<bf16_t>{ctx, (hipStream_t)stream}.attend(m, static_cast<const bf16_t*>(kv), layer, batch, *groups, rows, causal != 0, q, out);
   return Engine<float>{ctx, (hipStream_t)stream}.attend(m, static_cast<const float*>(kv), layer, batch, *groups, rows, causal != 0, q, out);
+}
+
+// ---- caches held in 4 or 8 bits --------------------------------------------------------------------------
+size_t dflash_kvq_bytes(const dflash_dims* model, int32_t n_pages, int32_t k_bits, int32_t v_bits) {
+  if (check_dims(model, "model")) return 0;
+  if (n_pages < 1) return (void)fail(nullptr, DFLASH_EINVAL, "kvq: n_pages must be positive"), 0;
+  if ((k_bits != 4 && k_bits != 8) || (v_bits != 4 && v_bits != 8)) return (void)fail(nullptr, DFLASH_EINVAL, "kvq: k_bits and v_bits must be 4 or 8"), 0;
+  return kvq_total(*model, n_pages, k_bits, v_bits);
+}
+
+int dflash_kvq_write(dflash_ctx* ctx, const dflash_batch* batch, const dflash_kvq* cache, int32_t layer, int32_t rows, const int32_t* counts, const void* k,
+                     const void* v, void* stream) {
+  return kvq_rows_checked(ctx, batch, cache, layer, rows, batch ? batch->seq_lens : nullptr, counts, const_cast<void*>(k), const_cast<void*>(v), true, stream);
+}
+int dflash_kvq_read(dflash_ctx* ctx, const dflash_batch* batch, const dflash_kvq* cache, int32_t layer, int32_t rows, const int32_t* starts, const int32_t* counts,
+                    void* k, void* v, void* stream) {
+  return kvq_rows_checked(ctx, batch, cache, layer, rows, starts, counts, k, v, false, stream);
+}
+
+int dflash_kvq_attention(dflash_ctx* ctx, const dflash_batch* batch, const dflash_kvq* cache, int32_t layer, int32_t rows, const int32_t* counts, int32_t causal,
+                         const void* q, void* out, void* stream) {
+  int rc;
+  if ((rc = check_batch(ctx, batch))) return rc;
+  if (batch->n_seqs == 0) return DFLASH_OK;
+  if ((rc = check_kvq(ctx, batch, cache, "kvq_attention")) || (rc = check_kvq_rows(ctx, batch, cache, layer, rows, "kvq_attention"))) return rc;
+  if (!q || !out || q == out || (((uintptr_t)q | (uintptr_t)out) & 15)) return CTX_FAIL(ctx, DFLASH_EINVAL, "kvq_attention: q and out must be two 16-byte aligned device buffers");
+  const dflash_dims& m = kvq_model(ctx, cache);
+  KvqAttn a{};
+  a.c = kvq_cache(m, cache);
+  a.layer = layer; a.n_seqs = batch->n_seqs; a.rows = rows; a.causal = causal != 0; a.n_q_heads = m.n_q_heads; a.mpps = ctx->rt.max_pages_per_seq;
+  a.lens = batch->seq_lens; a.counts = counts; a.table = batch->block_table;
+  a.q = q; a.out = out;
+  a.scale = 1.0f / sqrtf((float)m.head_dim);
+  a.part_o = reinterpret_cast<float*>(ctx->wsp + ctx->ws.part_o);
+  a.part_ml = reinterpret_cast<float2*>(ctx->wsp + ctx->ws.part_ml);
+  a.status = reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.status);
+  const bool bf16 = m.dtype == DFLASH_BF16;
+  const int64_t most = std::min<int64_t>((int64_t)batch->max_seq_len + rows, (int64_t)ctx->rt.max_pages_per_seq * DFLASH_PAGE_SIZE);
+  if (!kvq_attn_plan(a, bf16, (int)most, ctx->ws.part_rows)) return CTX_FAIL(ctx, DFLASH_EINVAL, "kvq_attention: %d sequences of %d rows are too many for one launch", batch->n_seqs, rows);
+  kvq_attn_launch(a, bf16, (hipStream_t)stream);
+  return launched(ctx, "kvq_attention");
+}
+
+int dflash_kvq_pack(dflash_ctx* ctx, const dflash_batch* batch, const dflash_kvq* cache, const int32_t* table, void* stream) {
+  return kvq_pages_checked(ctx, batch, cache, table, true, stream);
+}
+int dflash_kvq_unpack(dflash_ctx* ctx, const dflash_batch* batch, const dflash_kvq* cache, const int32_t* table, void* stream) {
+  return kvq_pages_checked(ctx, batch, cache, table, false, stream);
 }
 
 static int kv_copy_checked(dflash_ctx* ctx, const dflash_batch* batch, int32_t pool, int32_t layer, int32_t seq, int32_t start, int32_t count,

@@ -1,0 +1,86 @@
+"""The 4- and 8-bit format of the test side against its definition, and the sizes and refusals that need no GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from tests import kvq_model as km
+
+
+def test_codes_round_to_the_nearest_value():
+    rng = np.random.RandomState(0)
+    for bits in (4, 8):
+        x = rng.standard_normal((64, 96)) * 2.0 ** rng.randint(-30, 30, (64, 1))
+        x[3] = 0
+        code, e = km.quantise(x, bits)
+        y = km.values(code, e, bits, 96)
+        blocks = np.abs(x).reshape(64, 3, 32).max(-1)
+        scale = 2.0 ** (e.astype(float) - 127)
+        limit = km.LARGEST[bits] + (1 if bits == 4 else 16)
+        assert (blocks <= limit * scale).all() and ((blocks > limit * scale / 2) | (blocks == 0)).all()
+        # no code is nearer
+        all_values = np.concatenate([-km.code_values(bits), km.code_values(bits)])
+        nearest = np.abs((x.reshape(64, 3, 32) / scale[..., None])[..., None] - all_values).min(-1)
+        assert np.allclose(np.abs(x - y).reshape(64, 3, 32), nearest * scale[..., None], rtol=1e-12, atol=0)
+
+
+def test_ties_go_to_even_codes():
+    x = np.zeros(32)
+    x[:9] = [6.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -5.0]
+    code, e = km.quantise(x, 4)
+    assert e[0] == 127 and list(code[0, :9]) == [7, 0, 2, 2, 4, 4, 6, 6, 14]
+
+
+def test_blocks_that_are_not_finite():
+    x = np.ones((3, 64))
+    x[0, 5], x[1, 40], x[2, 33] = np.nan, np.inf, -np.inf
+    for bits in (4, 8):
+        code, e = km.quantise(x, bits)
+        assert [list(r == 255) for r in e] == [[True, False], [False, True], [False, True]]
+        y = km.values(code, e, bits, 64)
+        assert np.isnan(y[0, :32]).all() and np.isfinite(y[0, 32:]).all() and np.isnan(y[1, 32:]).all()
+
+
+@pytest.mark.parametrize("hd", [16, 32, 48, 64, 80, 96, 112, 128])
+@pytest.mark.parametrize("kb,vb", [(4, 4), (8, 8), (8, 4), (4, 8)])
+def test_layout_uses_every_place_once(hd, kb, vb):
+    (k, ks), (v, vs), k_sc, v_sc = km.places(hd, kb, vb)
+    bits = np.concatenate([(k * 8 + ks).ravel(), (v * 8 + vs).ravel()])
+    assert len(np.unique(bits)) == len(bits) and bits.max() < 8 * k_sc.min()
+    scales = np.concatenate([k_sc.ravel(), v_sc.ravel()])
+    assert len(np.unique(scales)) == len(scales) and scales.max() < km.unit_bytes(hd, kb, vb)
+
+
+def _dims(B, **kw):
+    d = dict(n_layers=3, d_model=64, n_q_heads=8, n_kv_heads=2, head_dim=64, d_ffn=64, vocab=64, rope_theta=1e4, rms_eps=1e-6, qk_norm=0, dtype=B.DFLASH_BF16,
+             n_experts=0, top_k=0, d_expert=0)
+    d.update(kw)
+    return B.Dims(*[d[n] for n, _ in B.Dims._fields_])
+
+
+def test_sizes():
+    from paper_2602_06036_amd import binding as B
+    l = B.lib()
+    for hd in (16, 48, 64, 80, 96, 128):
+        for kb in (4, 8):
+            for vb in (4, 8):
+                d = _dims(B, head_dim=hd, n_q_heads=4)
+                assert l.dflash_kvq_bytes(C.byref(d), 7, kb, vb) == 3 * 7 * 2 * km.unit_bytes(hd, kb, vb)
+    # past 32 bits
+    d = _dims(B, n_layers=36, n_kv_heads=8, n_q_heads=32, head_dim=128, d_model=4096)
+    assert l.dflash_kvq_bytes(C.byref(d), 1 << 20, 4, 4) == 36 * (1 << 20) * 8 * 2176
+
+
+def test_refusals_without_a_context():
+    from paper_2602_06036_amd import binding as B
+    l = B.lib()
+    for n, kb, vb, word in ((0, 4, 4, b"n_pages"), (-3, 4, 4, b"n_pages"), (5, 3, 4, b"bits"), (5, 4, 16, b"bits"), (5, 0, 8, b"bits")):
+        assert l.dflash_kvq_bytes(C.byref(_dims(B)), n, kb, vb) == 0 and word in l.dflash_last_error(None)
+    assert l.dflash_kvq_bytes(None, 5, 4, 4) == 0
+    assert l.dflash_kvq_bytes(C.byref(_dims(B, head_dim=72)), 5, 4, 4) == 0 and b"head_dim" in l.dflash_last_error(None)
+    b, q = B.Batch(), B.Kvq()
+    assert l.dflash_kvq_write(None, C.byref(b), C.byref(q), 0, 1, None, None, None, None) == B.DFLASH_EINVAL
+    assert l.dflash_kvq_read(None, C.byref(b), C.byref(q), 0, 1, None, None, None, None, None) == B.DFLASH_EINVAL
+    assert l.dflash_kvq_attention(None, C.byref(b), C.byref(q), 0, 1, None, 1, None, None, None) == B.DFLASH_EINVAL
+    assert l.dflash_kvq_pack(None, C.byref(b), C.byref(q), None, None) == B.DFLASH_EINVAL
+    assert l.dflash_kvq_unpack(None, C.byref(b), C.byref(q), None, None) == B.DFLASH_EINVAL
