@@ -22,6 +22,8 @@ constexpr float kSlack = 8.f;   // probabilities up to 2^8 above the reference: 
 __device__ __forceinline__ uint32_t pair_of(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
 __device__ __forceinline__ uint32_t finite_half(uint32_t x, uint32_t exponent) { return (x & exponent) == exponent ? 0u : x; }
 __device__ __forceinline__ uint32_t finite_halves(uint32_t x) { return finite_half(x & 0xFFFFu, 0x7F80u) | finite_half(x & 0xFFFF0000u, 0x7F800000u); }
+// the largest, NaN if one is (such a row is NaN whatever its reference): one instruction a pair of numbers, where fmaxf first quiets signalling NaNs
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 __device__ __forceinline__ bool odd_bits(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
 
 // byte I of the scales of a lane's keys
@@ -191,27 +193,34 @@ struct Math<bf16_t, NB, KB, VB> {
       f.v[1][i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
     }
   }
-  // elements of keys that nobody sees (there: a bit a key) become 0, and so do those that are not finite; whether there were any of these
+  // elements of keys that nobody sees (there: a bit a key) become 0; whether any that are left are not finite
   static __device__ __forceinline__ bool clear(Values& f, unsigned there) {
     uint32_t odd = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t x = f.v[h][i] & ((there >> (2 * i) & 1 ? 0x0000FFFFu : 0u) | (there >> (2 * i) & 2 ? 0xFFFF0000u : 0u)), y = finite_halves(x);
-        odd |= x ^ y;
-        f.v[h][i] = y;
+        f.v[h][i] &= (there >> (2 * i) & 1 ? 0x0000FFFFu : 0u) | (there >> (2 * i) & 2 ? 0xFFFF0000u : 0u);
+        odd |= f.v[h][i] ^ finite_halves(f.v[h][i]);
       }
     return odd != 0;
+  }
+  // elements that are not finite become 0 in f, and 1 in `up` (plus infinity and NaN) and `down` (minus infinity and NaN)
+  static __device__ __forceinline__ void part(Values& f, Values& up, Values& down) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = f.v[h][i];
+        auto mark = [&](uint32_t half, bool minus) { return (half & 0x7F80u) == 0x7F80u && (half & 0x7Fu || (half >> 15 != 0) == minus) ? 0x3F80u : 0u; };
+        up.v[h][i] = mark(x & 0xFFFFu, false) | mark(x >> 16, false) << 16;
+        down.v[h][i] = mark(x & 0xFFFFu, true) | mark(x >> 16, true) << 16;
+        f.v[h][i] = finite_halves(x);
+      }
   }
   static __device__ __forceinline__ void add(f32x4& lo, f32x4& hi, const Values& v, const Probs& p) {
     lo = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v.v[0]), __builtin_bit_cast(bf16x8, p.p), lo, 0, 0, 0);
     hi = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v.v[1]), __builtin_bit_cast(bf16x8, p.p), hi, 0, 0, 0);
-  }
-  // one element as the products take it
-  static __device__ __forceinline__ float element(uint32_t code, float scale, bool up) {
-    const uint32_t w = VB == 4 ? kvq_bf16_of4<0>(code, scale) : kvq_bf16_of8<0>(code, scale);
-    return __uint_as_float(up ? w & 0xFFFF0000u : w << 16);
   }
 };
 
@@ -299,11 +308,21 @@ struct Math<float, NB, KB, VB> {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = there >> i & 1 ? f.v[h][i] : 0.f;
-        odd |= odd_bits(x);
-        f.v[h][i] = odd_bits(x) ? 0.f : x;
+        f.v[h][i] = there >> i & 1 ? f.v[h][i] : 0.f;
+        odd |= odd_bits(f.v[h][i]);
       }
     return odd;
+  }
+  static __device__ __forceinline__ void part(Values& f, Values& up, Values& down) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = f.v[h][i];
+        up.v[h][i] = odd_bits(x) && !(x < 0.f) ? 1.f : 0.f;
+        down.v[h][i] = odd_bits(x) && !(x > 0.f) ? 1.f : 0.f;
+        f.v[h][i] = odd_bits(x) ? 0.f : x;
+      }
   }
   static __device__ __forceinline__ void add(f32x4& lo, f32x4& hi, const Values& v, const Probs& p) {
 #pragma unroll
@@ -312,35 +331,7 @@ struct Math<float, NB, KB, VB> {
       hi = __builtin_amdgcn_mfma_f32_16x16x4f32(v.v[1][i], p.p[i], hi, 0, 0, 0);
     }
   }
-  static __device__ __forceinline__ float element(uint32_t code, float scale, bool up) {
-    const f32x2 v = VB == 4 ? kvq_f32_of4<0>(code, scale) : kvq_f32_of8<0>(code, scale);
-    return up ? v[1] : v[0];
-  }
 };
-
-// V elements that are not finite, of keys that some rows of a tile see and others do not (the block itself, under the causal mask): taken out of the products, where
-// a weight of 0 would make them NaN, and added here to the rows that see them, whose sums become what they are.
-template <typename M, int NB, int KB, int VB>
-__device__ __forceinline__ void add_not_finite(f32x4 (&acc)[2 * NB], const unsigned char* unit, int n_keys, int lane) {
-  constexpr int SROW = kvq_scale_row(NB);
-  const unsigned char* codes = unit + kvq_codes(NB, KB);
-  const unsigned char* scales = codes + kvq_codes(NB, VB) + DF_PAGE * SROW;
-#pragma unroll 1
-  for (int key = 0; key < n_keys; ++key)
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const float s = kvq_scale_clean(scales[key * SROW + b]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int n = 4 * (lane >> 4) + i, wide = NB - (b & ~1) < 2 ? 1 : 2;
-        const uint32_t code = VB == 4 ? codes[(((key >> 2) * 16 + n) * NB + b) * 4 + (key & 3)]
-                                      : *reinterpret_cast<const uint16_t*>(codes + (b >> 1) * 1024 + (((key >> 2) * 16 + n) * wide + (b & 1)) * 8 + (key & 3) * 2);
-        const float lo = M::element(code, s, false), hi = M::element(code, s, true);
-        acc[2 * b][i] += odd_bits(lo) ? lo : 0.f;
-        acc[2 * b + 1][i] += odd_bits(hi) ? hi : 0.f;
-      }
-    }
-}
 
 template <typename T> __device__ __forceinline__ void store_row4(T* p, f32x4 v);
 template <> __device__ __forceinline__ void store_row4<float>(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
@@ -367,8 +358,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kvq_attn_kernel(KvqAttn a) {
   using M = Math<T, NB, KB, VB>;
   using P = typename M::P;
   constexpr int UNIT = kvq_unit(NB, KB, VB), LD = NB * 32 + 4;
+  constexpr bool Q_LDS = RB == 4 || (std::is_same<T, float>::value && RB == 2);   // the queries beside 64 rows' sums are too many for the registers
+  // A wavefront's ring of page pairs as they lie in memory, filled by direct-to-LDS copies: what is on its way costs no registers.
+  constexpr int PAIR = 2 * UNIT, D = kWaves * PAIR * 3 <= 53248 ? 3 : 2, NI = 2 * ((UNIT + 1023) / 1024);   // depth, copies a pair
+  constexpr int RING = kWaves * PAIR * D, MERGE = kWaves * 16 * LD * 4;
+  __shared__ typename M::Query s_q[Q_LDS ? RB : 1][64];
   __shared__ float s_m[kWaves][RB * 16], s_l[kWaves][RB * 16];
-  __shared__ __attribute__((aligned(16))) float s_o[kWaves][16][LD];
+  __shared__ __attribute__((aligned(1024))) unsigned char s_raw[RING > MERGE ? RING : MERGE];   // the ring, then the wavefronts' outputs
+  float (*s_o)[16][LD] = reinterpret_cast<float (*)[16][LD]>(s_raw);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
   const int H = a.c.n_kv_heads, hd = a.c.hd, group = a.n_q_heads / H;
   int i = blockIdx.x;
@@ -389,16 +386,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kvq_attn_kernel(KvqAttn a) {
   if (c0 >= end && split > 0) return;
   if (rows.outgrown && split == 0 && kvh == 0 && tile == 0 && threadIdx.x == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
 
-  typename M::Query q[RB];
+  typename M::Query q[Q_LDS ? 1 : RB];
   int row_end[RB];
   const T* q_base = static_cast<const T*>(a.q);
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int r = rb * 16 + col, row = row0 + min(r, n_rows - 1), j = row / group, h = row % group;
     const T* p = q_base + ((size_t)(s * (size_t)a.rows + j) * a.n_q_heads + kvh * group + h) * hd;
-    M::query(q[rb], r < n_rows ? p : nullptr, hd, lane);
     row_end[rb] = rows.end(a, j);
+    if constexpr (Q_LDS) {
+      if (wave == rb % kWaves) {
+        typename M::Query f;
+        M::query(f, r < n_rows ? p : nullptr, hd, lane);
+        s_q[rb][lane] = f;
+      }
+    } else {
+      M::query(q[rb], r < n_rows ? p : nullptr, hd, lane);
+    }
   }
+  if constexpr (Q_LDS) __syncthreads();
+  auto query = [&](int rb) -> const typename M::Query& {
+    if constexpr (Q_LDS) return s_q[rb][lane];
+    else return q[rb];
+  };
   f32x4 acc[RB][2 * NB];
   typename M::Sum sum[RB];
   float m_run[RB];
@@ -419,96 +429,155 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kvq_attn_kernel(KvqAttn a) {
   const size_t page_bytes = (size_t)H * UNIT;
   const float scale2 = a.scale * 1.44269504088896340736f;
 
-  auto id_of = [&](int page) { return table[min(page, last_page)]; };
   auto valid = [&](int id) { return id >= 0 && id < a.c.n_pages; };
-  auto unit_of = [&](int id) { return layer + (size_t)(valid(id) ? id : 0) * page_bytes; };
-  struct Pair { P a, b; };
-  auto load = [&](Pair& x, int ia, int ib) {
-    const unsigned char *ua = unit_of(ia), *ub = unit_of(ib);
-    x.a.load_k(ua, lane);
-    x.b.load_k(ub, lane);
-    x.a.load_v(ua, lane);
-    x.b.load_v(ub, lane);
+  // ids of 32 pairs at a time, lane l has page l of them; the next ones are asked for when a set has been used up, and waited for in a branch of their own: where every turn
+  // used a register that a load may still be on its way to, the compiler would have every turn wait for all copies
+  auto load_ids = [&](int p) { return table[min(2 * p + lane, last_page)]; };
+  int ids = load_ids(p0), ids_next = load_ids(p0 + 32), fresh = 0;
+  auto id_of = [&](int p, int i) { return __builtin_amdgcn_readlane((p - p0) & 32 ? ids_next : ids, ((p - p0) & 31) * 2 + i); };
+  const unsigned ring = (unsigned)(size_t)&s_raw[0] + (unsigned)wave * (PAIR * D);
+  const unsigned char* my_ring = s_raw + wave * (PAIR * D);
+  const unsigned voff = lane * 16;
+  auto copy = [&](const unsigned char* from, unsigned at) {   // 1 KB, or as far as the page goes
+    const unsigned dst = __builtin_amdgcn_readfirstlane(ring + at);
+    unsigned keep_m0;   // whatever the compiler keeps in m0 is put back
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_nop 0\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep_m0) : "s"(dst), "v"(voff), "s"(from) : "memory");
   };
-  auto work = [&](const Pair& x, int base, int ia, int ib, auto edge_c) {
-    constexpr bool EDGE = decltype(edge_c)::value;
-    const bool ok_a = !EDGE || valid(ia), ok_b = !EDGE || valid(ib);
+  auto fetch = [&](int p, int slot) {   // pages that are not there alias a readable one and weigh nothing
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int id = id_of(p, i);
+      const unsigned char* unit = layer + (size_t)(valid(id) ? id : 0) * page_bytes;
+#pragma unroll
+      for (int c = 0; c < UNIT; c += 1024) {
+        if (UNIT - c >= 1024) copy(unit + c, slot * PAIR + i * UNIT + c);
+        else if (lane < (UNIT - c) / 16) copy(unit + c, slot * PAIR + i * UNIT + c);
+      }
+    }
+  };
+  // a lane's eight keys of a pair in front of `stop`, a bit each
+  auto there = [&](bool ok_a, bool ok_b, int base, int stop) {
+    const int left = stop - base - 4 * g, a4 = ok_a ? min(max(left, 0), 4) : 0, b4 = ok_b ? min(max(left - DF_PAGE, 0), 4) : 0;
+    return ((1u << a4) - 1) | ((1u << b4) - 1) << 4;
+  };
+  auto work = [&](const unsigned char* pair, int base, bool ok_a, bool ok_b, bool edge) {   // edge: some row does not see some key
     typename M::Probs pr[RB];
+    f32x4 sa[RB], sb[RB];
     {
+      P page;
       typename M::Keys ka, kb;
-      M::keys(ka, x.a);
-      M::keys(kb, x.b);
+      page.load_k(pair, lane);
+      M::keys(ka, page);
+      page.load_k(pair + UNIT, lane);
+      M::keys(kb, page);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const f32x4 sa = M::scores(ka, q[rb]), sb = M::scores(kb, q[rb]);
-        float v[8], p[8];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          v[k] = sa[k];
-          v[4 + k] = sb[k];
-          if (EDGE) {
-            if (!ok_a || base + 4 * g + k >= row_end[rb]) v[k] = -INFINITY;
-            if (!ok_b || base + 16 + 4 * g + k >= row_end[rb]) v[4 + k] = -INFINITY;
-          }
-        }
-        float mx = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7]))) * scale2;
-        if (__ballot(mx > m_run[rb] + kSlack)) {   // (from minus infinity: the first keys)
-          mx = fmaxf(quarter_max(mx), m_run[rb]);
-          const float f = m_run[rb] == mx ? 1.f : __builtin_amdgcn_exp2f(m_run[rb] - mx);
-          m_run[rb] = mx;
-          M::scale_sum(sum[rb], f);
-#pragma unroll
-          for (int t = 0; t < 2 * NB; ++t) acc[rb][t] *= f;
-        }
-        const float mb = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], scale2, -mb));
-        M::probs(pr[rb], p);
-        M::sum(sum[rb], pr[rb], p);
+        if constexpr (Q_LDS) asm volatile("" ::: "memory");   // one row block's queries at a time
+        const typename M::Query& f = query(rb);
+        sa[rb] = M::scores(ka, f);
+        sb[rb] = M::scores(kb, f);
       }
     }
-    unsigned there = 0;
-    if (EDGE) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float v[8], p[8];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        if (ok_a && base + 4 * g + k < end) there |= 1u << k;
-        if (ok_b && base + 16 + 4 * g + k < end) there |= 16u << k;
+        v[k] = sa[rb][k];
+        v[4 + k] = sb[rb][k];
       }
+      if (edge) {
+        const int left = row_end[rb] - base - 4 * g, left_a = ok_a ? left : 0, left_b = ok_b ? left - DF_PAGE : 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          v[k] = k < left_a ? v[k] : -INFINITY;
+          v[4 + k] = k < left_b ? v[4 + k] : -INFINITY;
+        }
+      }
+      float mx = scale2 * max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[5], v[6], v[7]));
+      if (__ballot(mx > m_run[rb] + kSlack)) {   // (from minus infinity: the first keys)
+        mx = fmaxf(quarter_max(mx), m_run[rb]);
+        const float f = m_run[rb] == mx ? 1.f : __builtin_amdgcn_exp2f(m_run[rb] - mx);
+        m_run[rb] = mx;
+        M::scale_sum(sum[rb], f);
+#pragma unroll
+        for (int t = 0; t < 2 * NB; ++t) acc[rb][t] *= f;
+      }
+      const float mb = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], scale2, -mb));
+      M::probs(pr[rb], p);
+      M::sum(sum[rb], pr[rb], p);
     }
-    bool odd = false;
+    P pa, pb;
+    pa.load_v(pair, lane);
+    pb.load_v(pair + UNIT, lane);
     unrolled<NB>([&](auto b_c) {
       constexpr int b = decltype(b_c)::value;
       typename M::Values v;
-      M::template values<b>(v, x.a, x.b);
-      if (EDGE) odd |= M::clear(v, there);
+      M::template values<b>(v, pa, pb);
+      if (edge && __ballot(M::clear(v, there(ok_a, ok_b, base, end)))) {
+        // V elements that are not finite, of keys that some rows see and others do not: a weight of 0 would make them NaN.  They leave the products, and how
+        // many of them a row sees, by sign, are products too: one is enough.
+        typename M::Values up, down;
+        M::part(v, up, down);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const unsigned sees = there(ok_a, ok_b, base, row_end[rb]);
+          float see[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) see[k] = sees >> k & 1 ? 1.f : 0.f;
+          typename M::Probs seen;
+          M::probs(seen, see);
+          f32x4 n[4] = {};
+          M::add(n[0], n[1], up, seen);
+          M::add(n[2], n[3], down, seen);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              acc[rb][2 * b + h][i] += n[h][i] > 0.f ? INFINITY : 0.f;
+              acc[rb][2 * b + h][i] += n[2 + h][i] > 0.f ? -INFINITY : 0.f;
+            }
+        }
+      }
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) M::add(acc[rb][2 * b], acc[rb][2 * b + 1], v, pr[rb]);
     });
-    if (EDGE && __ballot(odd)) {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        if (ok_a) add_not_finite<M, NB, KB, VB>(acc[rb], unit_of(ia), min(max(row_end[rb] - base, 0), DF_PAGE), lane);
-        if (ok_b) add_not_finite<M, NB, KB, VB>(acc[rb], unit_of(ib), min(max(row_end[rb] - base - DF_PAGE, 0), DF_PAGE), lane);
-      }
-    }
   };
   if (p0 < p1) {
-    Pair cur, next;
-    int ia = id_of(2 * p0), ib = id_of(2 * p0 + 1), na = id_of(2 * p0 + 2), nb = id_of(2 * p0 + 3);
-    load(cur, ia, ib);
-    for (int p = p0; p < p1; ++p) {
-      const int base = c0 + p * 32;
-      const int fa = id_of(2 * p + 4), fb = id_of(2 * p + 5);
-      load(next, na, nb);
-      if (base + 32 > all_see || base + 32 > c1 || !valid(ia) || !valid(ib)) work(cur, base, ia, ib, std::true_type());
-      else work(cur, base, ia, ib, std::false_type());
-      cur = next;
-      ia = na;
-      ib = nb;
-      na = fa;
-      nb = fb;
+    const int n = p1 - p0;
+    int asked = 0, slot = 0;   // pairs asked for, the ring's slot of the pair at hand
+    for (; asked < D - 1 && asked < n; ++asked) fetch(p0 + asked, asked);
+    asm volatile("" : "+v"(ids), "+v"(ids_next));
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+      if ((k & 31) == 0 && k) fresh = load_ids(p0 + k + 32);
+      if ((k & 31) == 16 && k > 16) {
+        asm volatile("" : "+v"(fresh));
+        if (k & 32) ids = fresh;
+        else ids_next = fresh;
+      }
+      if (asked < n) {   // the slot that the pair before this one has left
+        fetch(p0 + asked, slot == 0 ? D - 1 : slot - 1);
+        ++asked;
+        __builtin_amdgcn_s_waitcnt(0x0F70 | ((D - 1) * NI & 15) | ((D - 1) * NI >> 4 << 14));   // vmcnt: this pair's copies have landed
+      } else if (D > 2 && k + 1 < n) {
+        __builtin_amdgcn_s_waitcnt(0x0F70 | (NI & 15) | (NI >> 4 << 14));
+      } else {
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+      }
+      asm volatile("" ::: "memory");
+      const int base = c0 + (p0 + k) * 32;
+      const bool ok_a = valid(id_of(p0 + k, 0)), ok_b = valid(id_of(p0 + k, 1));
+      const unsigned char* pair = my_ring + slot * PAIR;
+      work(pair, base, ok_a, ok_b, base + 32 > all_see || base + 32 > c1 || !ok_a || !ok_b);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the pair has been read before its slot is filled again
+      slot = slot + 1 == D ? 0 : slot + 1;
     }
   }
+  __syncthreads();   // the wavefronts' outputs overlay the ring
 
   // ---- the wavefronts' results become one ----
 #pragma unroll
