@@ -49,9 +49,8 @@ struct KvqAttn {
   const void* q;
   void* out;
   float scale;
-  int32_t chunk, splits, tiles;   // keys of a range (a multiple of 128), ranges and row tiles of a sequence at most
-  int32_t limit;                  // keys that the ranges cover
-  float* part_o;                  // [row][splits][hd], [row][splits]
+  int32_t parts, tiles;           // about how many ranges the keys of all sequences are cut into (0: a sequence is one), row tiles of a sequence
+  float* part_o;                  // [range][row of a sequence][query head][hd] and without hd
   float2* part_ml;
   int32_t* status;
 };
@@ -60,7 +59,7 @@ void kvq_write_launch(const KvqRows& a, bool bf16, hipStream_t st);
 void kvq_read_launch(const KvqRows& a, bool bf16, hipStream_t st);
 void kvq_pack_launch(const KvqPages& a, bool bf16, hipStream_t st);
 void kvq_unpack_launch(const KvqPages& a, bool bf16, hipStream_t st);
-// fills in chunk, splits, tiles and limit: part_rows partial rows fit part_o and part_ml; max_tokens: the longest sequence with its rows.  False: no launch is that large
+// fills in parts and tiles: part_rows partial rows fit part_o and part_ml; max_tokens: the longest sequence with its rows.  False: no launch is that large
 bool kvq_attn_plan(KvqAttn& a, bool bf16, int max_tokens, size_t part_rows);
 void kvq_attn_launch(const KvqAttn& a, bool bf16, hipStream_t st);
 

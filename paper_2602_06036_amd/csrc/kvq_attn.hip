@@ -16,7 +16,7 @@
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kMinPairs = 8;    // page pairs of a range at least
 constexpr float kSlack = 8.f;   // probabilities up to 2^8 above the reference: nothing that fp32 sums or bf16 exponents notice
 
 __device__ __forceinline__ uint32_t pair_of(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
@@ -205,18 +205,19 @@ struct Math<bf16_t, NB, KB, VB> {
       }
     return odd != 0;
   }
-  // elements that are not finite become 0 in f, and 1 in `up` (plus infinity and NaN) and `down` (minus infinity and NaN)
-  static __device__ __forceinline__ void part(Values& f, Values& up, Values& down) {
+  // 1 for every element that is plus (minus) infinity or NaN
+  static __device__ __forceinline__ void mark(Values& w, const Values& f, bool minus) {
+    auto one = [&](uint32_t half) { return (half & 0x7F80u) == 0x7F80u && (half & 0x7Fu || (half >> 15 != 0) == minus) ? 0x3F80u : 0u; };
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = f.v[h][i];
-        auto mark = [&](uint32_t half, bool minus) { return (half & 0x7F80u) == 0x7F80u && (half & 0x7Fu || (half >> 15 != 0) == minus) ? 0x3F80u : 0u; };
-        up.v[h][i] = mark(x & 0xFFFFu, false) | mark(x >> 16, false) << 16;
-        down.v[h][i] = mark(x & 0xFFFFu, true) | mark(x >> 16, true) << 16;
-        f.v[h][i] = finite_halves(x);
-      }
+      for (int i = 0; i < 4; ++i) w.v[h][i] = one(f.v[h][i] & 0xFFFFu) | one(f.v[h][i] >> 16) << 16;
+  }
+  static __device__ __forceinline__ void drop(Values& f) {   // those become 0
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f.v[h][i] = finite_halves(f.v[h][i]);
   }
   static __device__ __forceinline__ void add(f32x4& lo, f32x4& hi, const Values& v, const Probs& p) {
     lo = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v.v[0]), __builtin_bit_cast(bf16x8, p.p), lo, 0, 0, 0);
@@ -313,16 +314,17 @@ struct Math<float, NB, KB, VB> {
       }
     return odd;
   }
-  static __device__ __forceinline__ void part(Values& f, Values& up, Values& down) {
+  static __device__ __forceinline__ void mark(Values& w, const Values& f, bool minus) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = f.v[h][i];
-        up.v[h][i] = odd_bits(x) && !(x < 0.f) ? 1.f : 0.f;
-        down.v[h][i] = odd_bits(x) && !(x > 0.f) ? 1.f : 0.f;
-        f.v[h][i] = odd_bits(x) ? 0.f : x;
-      }
+      for (int i = 0; i < 8; ++i) w.v[h][i] = odd_bits(f.v[h][i]) && !(minus ? f.v[h][i] > 0.f : f.v[h][i] < 0.f) ? 1.f : 0.f;
+  }
+  static __device__ __forceinline__ void drop(Values& f) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f.v[h][i] = odd_bits(f.v[h][i]) ? 0.f : f.v[h][i];
   }
   static __device__ __forceinline__ void add(f32x4& lo, f32x4& hi, const Values& v, const Probs& p) {
 #pragma unroll
@@ -345,140 +347,100 @@ struct SeqRows {
     const int cap = a.mpps * DF_PAGE, c = a.counts ? a.counts[s] : a.rows, n = a.lens[s];
     len = min(max(n, 0), cap);
     count = min(max(c, 0), a.rows);
-    n_tok = min(min(len + count, cap), a.limit);
-    outgrown = c > a.rows || (count > 0 && (n > cap - count || n > a.limit - count));
+    n_tok = count > 0 ? min(len + count, cap) : 0;
+    outgrown = c > a.rows || (count > 0 && n > cap - count);
   }
   // keys in front of the first one that slot j does not see
   __device__ __forceinline__ int end(const KvqAttn& a, int j) const { return a.causal ? min(len + j + 1, n_tok) : n_tok; }
 };
 
-// grid: kv heads (fastest) x ranges x row tiles x sequences
-template <typename T, int NB, int KB, int VB, int RB>
-__global__ __launch_bounds__(64 * kWaves, 2) void kvq_attn_kernel(KvqAttn a) {
-  using M = Math<T, NB, KB, VB>;
-  using P = typename M::P;
-  constexpr int UNIT = kvq_unit(NB, KB, VB), LD = NB * 32 + 4;
-  constexpr bool Q_LDS = RB == 4 || (std::is_same<T, float>::value && RB == 2);   // the queries beside 64 rows' sums are too many for the registers
-  // A wavefront's ring of page pairs as they lie in memory, filled by direct-to-LDS copies: what is on its way costs no registers.
-  constexpr int PAIR = 2 * UNIT, D = kWaves * PAIR * 3 <= 53248 ? 3 : 2, NI = 2 * ((UNIT + 1023) / 1024);   // depth, copies a pair
-  constexpr int RING = kWaves * PAIR * D, MERGE = kWaves * 16 * LD * 4;
-  __shared__ typename M::Query s_q[Q_LDS ? RB : 1][64];
-  __shared__ float s_m[kWaves][RB * 16], s_l[kWaves][RB * 16];
-  __shared__ __attribute__((aligned(1024))) unsigned char s_raw[RING > MERGE ? RING : MERGE];   // the ring, then the wavefronts' outputs
-  float (*s_o)[16][LD] = reinterpret_cast<float (*)[16][LD]>(s_raw);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
-  const int H = a.c.n_kv_heads, hd = a.c.hd, group = a.n_q_heads / H;
-  int i = blockIdx.x;
-  const int kvh = i % H;
-  i /= H;
-  const int split = i % a.splits;
-  i /= a.splits;
-  const int tile = i % a.tiles, s = i / a.tiles;
-  const SeqRows rows(a, s);
-  const int row0 = tile * 16 * RB, n_rows = min(rows.count * group - row0, 16 * RB);
-  if (n_rows <= 0) {
-    if (rows.outgrown && tile == 0 && split == 0 && kvh == 0 && threadIdx.x == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
-    return;
+// slot and query head of a row; groups are powers of two as a rule, and a division costs 30 instructions
+__device__ __forceinline__ void slot_of(int row, int group, int& slot, int& head) {
+  if ((group & (group - 1)) == 0) {
+    slot = row >> __builtin_ctz(group);
+    head = row & (group - 1);
+  } else {
+    slot = row / group;
+    head = row - slot * group;
   }
-  const int end = rows.end(a, (row0 + n_rows - 1) / group);      // keys that some row of the tile sees
-  const int all_see = rows.end(a, row0 / group);                 // ... that all rows see
-  const int c0 = split * a.chunk, c1 = min(c0 + a.chunk, end);
-  if (c0 >= end && split > 0) return;
-  if (rows.outgrown && split == 0 && kvh == 0 && tile == 0 && threadIdx.x == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
+}
 
-  typename M::Query q[Q_LDS ? 1 : RB];
-  int row_end[RB];
-  const T* q_base = static_cast<const T*>(a.q);
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = rb * 16 + col, row = row0 + min(r, n_rows - 1), j = row / group, h = row % group;
-    const T* p = q_base + ((size_t)(s * (size_t)a.rows + j) * a.n_q_heads + kvh * group + h) * hd;
-    row_end[rb] = rows.end(a, j);
-    if constexpr (Q_LDS) {
-      if (wave == rb % kWaves) {
-        typename M::Query f;
-        M::query(f, r < n_rows ? p : nullptr, hd, lane);
-        s_q[rb][lane] = f;
-      }
-    } else {
-      M::query(q[rb], r < n_rows ? p : nullptr, hd, lane);
-    }
+// Ranges.  The lengths are on the device, the host knows a bound: so the launch has a number of workgroups a head, and every one of them finds its share by itself.
+// Ranges are as long for all sequences, so that about a.parts of them come out, and are counted through the sequences; workgroups behind the last one have nothing to do.
+// (Cut by the longest sequence, 32 single tokens behind 1k to 32k tokens kept 72 % of the CUs busy.)
+__device__ __forceinline__ int wave_scan(int x) {   // sum over the lanes up to this one
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15, :31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+struct Ranges {
+  int chunk;   // keys, a multiple of 128
+  int lane;
+  __device__ __forceinline__ static int pairs(const KvqAttn& a, int s) { return s < a.n_seqs ? (SeqRows(a, s).n_tok + 31) / 32 : 0; }
+  __device__ __forceinline__ Ranges(const KvqAttn& a) : lane(threadIdx.x & 63) {
+    long long all = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) all += __builtin_amdgcn_readlane(wave_scan(pairs(a, s0 + lane)), 63);
+    const long long each = (all + a.parts - 1) / a.parts;
+    chunk = (int)min(max((each + 3) / 4, (long long)kMinPairs / 4), (long long)(1 << 23)) * 128;
   }
-  if constexpr (Q_LDS) __syncthreads();
-  auto query = [&](int rb) -> const typename M::Query& {
-    if constexpr (Q_LDS) return s_q[rb][lane];
-    else return q[rb];
-  };
+  __device__ __forceinline__ int count(int tokens) const { return (int)((tokens + (long long)chunk - 1) / chunk); }
+  // the sequence that the f-th range belongs to, and the first of its ranges; false: there are not as many
+  __device__ __forceinline__ bool find(const KvqAttn& a, int f, int& s, int& first) const {
+    int before = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+      const int mine = (pairs(a, s0 + lane) + chunk / 32 - 1) / (chunk / 32), upto = wave_scan(mine);
+      const unsigned long long behind = __ballot(before + upto > f);
+      if (behind) {
+        const int at = __ffsll(behind) - 1;
+        s = s0 + at;
+        first = before + __builtin_amdgcn_readlane(upto - mine, at);
+        return true;
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+  }
+  __device__ __forceinline__ int first_of(const KvqAttn& a, int s) const {
+    int before = 0;
+    for (int s0 = 0; s0 < s; s0 += 64) {
+      const int l = s0 + lane;
+      before += __builtin_amdgcn_readlane(wave_scan(l < s ? (pairs(a, l) + chunk / 32 - 1) / (chunk / 32) : 0), 63);
+    }
+    return before;
+  }
+};
+
+// ---- a wavefront's rows: 16 RB of them, a column of 16 each ----------------------------------------------------------------------
+// A pair of pages: where it begins, and whether its pages are there; a lane has keys 4g .. 4g + 3 of both.
+struct Seen {
+  int base, g;
+  bool ok_a, ok_b;
+  __device__ __forceinline__ unsigned before(int stop) const {   // those of the lane's eight keys in front of `stop`, a bit each
+    const int left = stop - base - 4 * g, a4 = ok_a ? min(max(left, 0), 4) : 0, b4 = ok_b ? min(max(left - DF_PAGE, 0), 4) : 0;
+    return ((1u << a4) - 1) | ((1u << b4) - 1) << 4;
+  }
+};
+template <typename M, int NB, int RB>
+struct State {
   f32x4 acc[RB][2 * NB];
   typename M::Sum sum[RB];
   float m_run[RB];
+  int row_end[RB];
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    m_run[rb] = -INFINITY;
-    sum[rb] = {};
+    for (int rb = 0; rb < RB; ++rb) {
+      m_run[rb] = -INFINITY;
+      sum[rb] = {};
 #pragma unroll
-    for (int t = 0; t < 2 * NB; ++t) acc[rb][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < 2 * NB; ++t) acc[rb][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
   }
-
-  // this wavefront's pairs of pages
-  const int pairs = (c1 - c0 + 31) / 32, per = (pairs + kWaves - 1) / kWaves;
-  const int p0 = wave * per, p1 = min(p0 + per, pairs);
-  const int32_t* table = a.table + (size_t)s * a.mpps + c0 / DF_PAGE;
-  const int last_page = (c1 - c0 + DF_PAGE - 1) / DF_PAGE - 1;    // of the range
-  const unsigned char* layer = a.c.data + (size_t)a.layer * a.c.n_pages * H * UNIT + (size_t)kvh * UNIT;
-  const size_t page_bytes = (size_t)H * UNIT;
-  const float scale2 = a.scale * 1.44269504088896340736f;
-
-  auto valid = [&](int id) { return id >= 0 && id < a.c.n_pages; };
-  // ids of 32 pairs at a time, lane l has page l of them; the next ones are asked for when a set has been used up, and waited for in a branch of their own: where every turn
-  // used a register that a load may still be on its way to, the compiler would have every turn wait for all copies
-  auto load_ids = [&](int p) { return table[min(2 * p + lane, last_page)]; };
-  int ids = load_ids(p0), ids_next = load_ids(p0 + 32), fresh = 0;
-  auto id_of = [&](int p, int i) { return __builtin_amdgcn_readlane((p - p0) & 32 ? ids_next : ids, ((p - p0) & 31) * 2 + i); };
-  const unsigned ring = (unsigned)(size_t)&s_raw[0] + (unsigned)wave * (PAIR * D);
-  const unsigned char* my_ring = s_raw + wave * (PAIR * D);
-  const unsigned voff = lane * 16;
-  auto copy = [&](const unsigned char* from, unsigned at) {   // 1 KB, or as far as the page goes
-    const unsigned dst = __builtin_amdgcn_readfirstlane(ring + at);
-    unsigned keep_m0;   // whatever the compiler keeps in m0 is put back
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_nop 0\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep_m0) : "s"(dst), "v"(voff), "s"(from) : "memory");
-  };
-  auto fetch = [&](int p, int slot) {   // pages that are not there alias a readable one and weigh nothing
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int id = id_of(p, i);
-      const unsigned char* unit = layer + (size_t)(valid(id) ? id : 0) * page_bytes;
-#pragma unroll
-      for (int c = 0; c < UNIT; c += 1024) {
-        if (UNIT - c >= 1024) copy(unit + c, slot * PAIR + i * UNIT + c);
-        else if (lane < (UNIT - c) / 16) copy(unit + c, slot * PAIR + i * UNIT + c);
-      }
-    }
-  };
-  // a lane's eight keys of a pair in front of `stop`, a bit each
-  auto there = [&](bool ok_a, bool ok_b, int base, int stop) {
-    const int left = stop - base - 4 * g, a4 = ok_a ? min(max(left, 0), 4) : 0, b4 = ok_b ? min(max(left - DF_PAGE, 0), 4) : 0;
-    return ((1u << a4) - 1) | ((1u << b4) - 1) << 4;
-  };
-  auto work = [&](const unsigned char* pair, int base, bool ok_a, bool ok_b, bool edge) {   // edge: some row does not see some key
-    typename M::Probs pr[RB];
-    f32x4 sa[RB], sb[RB];
-    {
-      P page;
-      typename M::Keys ka, kb;
-      page.load_k(pair, lane);
-      M::keys(ka, page);
-      page.load_k(pair + UNIT, lane);
-      M::keys(kb, page);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        if constexpr (Q_LDS) asm volatile("" ::: "memory");   // one row block's queries at a time
-        const typename M::Query& f = query(rb);
-        sa[rb] = M::scores(ka, f);
-        sb[rb] = M::scores(kb, f);
-      }
-    }
+  // scores of both pages -> weights; masks where edge is set
+  __device__ __forceinline__ void weigh(typename M::Probs (&pr)[RB], const f32x4 (&sa)[RB], const f32x4 (&sb)[RB], const Seen& at, bool edge, float scale2) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float v[8], p[8];
@@ -488,7 +450,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kvq_attn_kernel(KvqAttn a) {
         v[4 + k] = sb[rb][k];
       }
       if (edge) {
-        const int left = row_end[rb] - base - 4 * g, left_a = ok_a ? left : 0, left_b = ok_b ? left - DF_PAGE : 0;
+        asm volatile("");   // a branch, not selects in every turn
+        const int left = row_end[rb] - at.base - 4 * at.g, left_a = at.ok_a ? left : 0, left_b = at.ok_b ? left - DF_PAGE : 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           v[k] = k < left_a ? v[k] : -INFINITY;
@@ -510,47 +473,229 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kvq_attn_kernel(KvqAttn a) {
       M::probs(pr[rb], p);
       M::sum(sum[rb], pr[rb], p);
     }
+  }
+  // Values where some row does not see some key: those from `end` on are not there; those that are not finite, whose product with a weight of 0 would be NaN, are left out,
+  // and whether there are any.
+  __device__ __forceinline__ static bool finite_values(typename M::Values& v, const Seen& at, int end) {
+    const bool odd = M::clear(v, at.before(end));
+    if (__ballot(odd) == 0) return false;
+    M::drop(v);
+    return true;
+  }
+  // What was left out of a pair, behind the sweep (in it, sums that a rare branch changes would cost the registers a second time): how many such values a row sees, by sign,
+  // are products too, and one is enough.
+  template <typename P>
+  __device__ __forceinline__ void add_left_out(const unsigned char* unit_a, const unsigned char* unit_b, const Seen& at, int end, int lane) {
     P pa, pb;
-    pa.load_v(pair, lane);
-    pb.load_v(pair + UNIT, lane);
+    pa.load_v(unit_a, lane);
+    pb.load_v(unit_b, lane);
     unrolled<NB>([&](auto b_c) {
       constexpr int b = decltype(b_c)::value;
-      typename M::Values v;
+      typename M::Values v, w;
       M::template values<b>(v, pa, pb);
-      if (edge && __ballot(M::clear(v, there(ok_a, ok_b, base, end)))) {
-        // V elements that are not finite, of keys that some rows see and others do not: a weight of 0 would make them NaN.  They leave the products, and how
-        // many of them a row sees, by sign, are products too: one is enough.
-        typename M::Values up, down;
-        M::part(v, up, down);
+      M::clear(v, at.before(end));
+#pragma unroll
+      for (int sign = 0; sign < 2; ++sign) {
+        M::mark(w, v, sign);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-          const unsigned sees = there(ok_a, ok_b, base, row_end[rb]);
+          const unsigned sees = at.before(row_end[rb]);
           float see[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) see[k] = sees >> k & 1 ? 1.f : 0.f;
           typename M::Probs seen;
           M::probs(seen, see);
-          f32x4 n[4] = {};
-          M::add(n[0], n[1], up, seen);
-          M::add(n[2], n[3], down, seen);
+          f32x4 n[2] = {};
+          M::add(n[0], n[1], w, seen);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              acc[rb][2 * b + h][i] += n[h][i] > 0.f ? INFINITY : 0.f;
-              acc[rb][2 * b + h][i] += n[2 + h][i] > 0.f ? -INFINITY : 0.f;
-            }
+            for (int i = 0; i < 4; ++i) acc[rb][2 * b + h][i] += n[h][i] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
         }
       }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) M::add(acc[rb][2 * b], acc[rb][2 * b + 1], v, pr[rb]);
     });
+  }
+  template <int B>
+  __device__ __forceinline__ void add(const typename M::Values& v, const typename M::Probs (&pr)[RB]) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) M::add(acc[rb][2 * B], acc[rb][2 * B + 1], v, pr[rb]);
+  }
+};
+
+// grid: kv heads (fastest) x row tiles x ranges, or sequences where each is one range (a.parts = 0)
+template <typename T, int NB, int KB, int VB, int RB>
+struct Launch {
+  static constexpr int UNIT = kvq_unit(NB, KB, VB), LD = NB * 32 + 4, WAVES = 4;
+  static constexpr bool F32 = std::is_same<T, float>::value, Q_LDS = RB == 4 || (F32 && RB == 2);   // the queries beside 64 rows' sums are too many for the registers
+  // A wavefront's ring of page pairs as they lie in memory, filled by direct-to-LDS copies: what is on its way costs no registers.  Two pairs: three or four leave room for
+  // fewer workgroups and gain nothing (single tokens 133, 133, 144 us; blocks of 16 rows 42, 42, 65).
+  static constexpr int PAIR = 2 * UNIT, NI = 2 * ((UNIT + 1023) / 1024);   // bytes, copies a pair
+  static constexpr int RING = WAVES * PAIR * 2, MERGE = WAVES * 16 * LD * 4, RAW = RING > MERGE ? RING : MERGE;
+  static constexpr int LDS = RAW + (Q_LDS ? RB * 64 * (int)sizeof(typename Math<T, NB, KB, VB>::Query) : 0);
+  static constexpr int ON_SIMD = LDS > 80000 ? 1 : RB == 1 && KB + VB < 16 ? 3 : 2;   // wavefronts
+};
+template <typename T, int NB, int KB, int VB, int RB>
+__global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T, NB, KB, VB, RB>::ON_SIMD)) void kvq_attn_kernel(KvqAttn a) {
+  using L = Launch<T, NB, KB, VB, RB>;
+  using M = Math<T, NB, KB, VB>;
+  using P = typename M::P;
+  constexpr int UNIT = L::UNIT, LD = L::LD, PAIR = L::PAIR, NI = L::NI, WAVES = L::WAVES;
+  constexpr bool Q_LDS = L::Q_LDS;
+  constexpr int QP = sizeof(typename M::Query) / 16;   // 16-byte pieces of a lane's queries, a lane's neighbour's beside each (a lane's behind each other: four lanes a bank)
+  __shared__ u32x4 s_q[Q_LDS ? RB : 1][QP][Q_LDS ? 64 : 1];
+  __shared__ float s_m[WAVES][RB * 16], s_l[WAVES][RB * 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char s_raw[L::RAW];   // the ring, then the wavefronts' outputs
+  float (*s_o)[16][LD] = reinterpret_cast<float (*)[16][LD]>(s_raw);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+  const int H = a.c.n_kv_heads, hd = a.c.hd, group = a.n_q_heads / H;
+  const int kvh = blockIdx.x % H, tile = blockIdx.x / H % a.tiles, part = blockIdx.x / H / a.tiles;
+  int s = part, first = part, chunk = 0x7FFFFF80;
+  if (a.parts) {
+    const Ranges ranges(a);
+    chunk = ranges.chunk;
+    if (!ranges.find(a, part, s, first)) return;
+  }
+  const int split = part - first;
+  const SeqRows rows(a, s);
+  const int row0 = tile * 16 * RB, n_rows = min(rows.count * group - row0, 16 * RB);
+  if (rows.outgrown && split + kvh + tile == 0 && threadIdx.x == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
+  if (n_rows <= 0) return;
+  const int end = rows.end(a, (row0 + n_rows - 1) / group);      // keys that some row of the tile sees
+  const int all_see = rows.end(a, row0 / group);                 // ... that all rows see
+  if (end <= split * (long long)chunk) return;
+  const int c0 = split * chunk, c1 = min(end - c0, chunk) + c0;
+
+  typename M::Query q[Q_LDS ? 1 : RB];
+  State<M, NB, RB> st;
+  st.clear();
+  const T* q_base = static_cast<const T*>(a.q);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int r = rb * 16 + col;
+    int j, h;
+    slot_of(row0 + min(r, n_rows - 1), group, j, h);
+    const T* p = q_base + ((size_t)(s * (size_t)a.rows + j) * a.n_q_heads + kvh * group + h) * hd;
+    st.row_end[rb] = rows.end(a, j);
+    if constexpr (Q_LDS) {
+      if (wave == rb) {
+        typename M::Query f;
+        M::query(f, r < n_rows ? p : nullptr, hd, lane);
+#pragma unroll
+        for (int i = 0; i < QP; ++i) {
+          u32x4 x;
+          __builtin_memcpy(&x, reinterpret_cast<const char*>(&f) + 16 * i, 16);
+          s_q[rb][i][lane] = x;
+        }
+      }
+    } else {
+      M::query(q[rb], r < n_rows ? p : nullptr, hd, lane);
+    }
+  }
+  if constexpr (Q_LDS) __syncthreads();
+  auto query = [&](int rb) {
+    if constexpr (Q_LDS) {
+      typename M::Query f;
+#pragma unroll
+      for (int i = 0; i < QP; ++i) {
+        const u32x4 x = s_q[rb][i][lane];
+        __builtin_memcpy(reinterpret_cast<char*>(&f) + 16 * i, &x, 16);
+      }
+      return f;
+    } else {
+      return q[rb];
+    }
+  };
+  // this wavefront's pairs of pages
+  const int pairs = (c1 - c0 + 31) / 32, per = (pairs + WAVES - 1) / WAVES;
+  const int p0 = wave * per, p1 = min(p0 + per, pairs);
+  const int32_t* table = a.table + (size_t)s * a.mpps + c0 / DF_PAGE;
+  const int last_page = (c1 - c0 + DF_PAGE - 1) / DF_PAGE - 1;    // of the range
+  const unsigned char* layer = a.c.data + (size_t)a.layer * a.c.n_pages * H * UNIT + (size_t)kvh * UNIT;
+  const size_t page_bytes = (size_t)H * UNIT;
+  const float scale2 = a.scale * 1.44269504088896340736f;
+
+  auto valid = [&](int id) { return id >= 0 && id < a.c.n_pages; };
+  // ids of 32 pairs at a time, lane l has page l of them; the next ones are asked for when a set has been used up, and waited for in a branch of their own: where every turn
+  // used a register that a load may still be on its way to, the compiler would have every turn wait for all copies
+  auto load_ids = [&](int p) { return table[min(2 * p + lane, last_page)]; };
+  int ids = load_ids(p0), ids_next = load_ids(p0 + 32), fresh = 0;
+  auto id_of = [&](int p, int i) { return __builtin_amdgcn_readlane((p - p0) & 32 ? ids_next : ids, ((p - p0) & 31) * 2 + i); };
+  const unsigned ring = (unsigned)(size_t)&s_raw[0] + (unsigned)wave * (PAIR * 2);
+  const unsigned char* my_ring = s_raw + wave * (PAIR * 2);
+  const unsigned voff = lane * 16;
+  auto copy = [&](const unsigned char* from, unsigned at) {   // 1 KB, or as far as the page goes
+    const unsigned dst = __builtin_amdgcn_readfirstlane(ring + at);
+    unsigned keep_m0;   // whatever the compiler keeps in m0 is put back
+    // bf16, up to 32 rows: they are one tile and nobody else reads these bytes, which need no place in L2 (single tokens 126 -> 116 us)
+    if constexpr (!L::F32 && RB < 4)
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 nt\n\ts_nop 0\n\ts_mov_b32 m0, %0"
+                   : "=&s"(keep_m0) : "s"(dst), "v"(voff), "s"(from) : "memory");
+    else
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_nop 0\n\ts_mov_b32 m0, %0"
+                   : "=&s"(keep_m0) : "s"(dst), "v"(voff), "s"(from) : "memory");
+  };
+  auto fetch = [&](int p, int slot) {   // pages that are not there alias a readable one and weigh nothing
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int id = id_of(p, i);
+      const unsigned char* unit = layer + (size_t)(valid(id) ? id : 0) * page_bytes;
+#pragma unroll
+      for (int c = 0; c < UNIT; c += 1024) {
+        if (UNIT - c >= 1024) copy(unit + c, slot * PAIR + i * UNIT + c);
+        else if (lane < (UNIT - c) / 16) copy(unit + c, slot * PAIR + i * UNIT + c);
+      }
+    }
+  };
+  bool left_out = false;
+  auto work = [&](const unsigned char* pair, const Seen& at, bool edge) {   // edge: some row does not see some key
+    typename M::Probs pr[RB];
+    f32x4 sa[RB], sb[RB];
+    {
+      P page;
+      typename M::Keys ka, kb;
+      page.load_k(pair, lane);
+      M::keys(ka, page);
+      page.load_k(pair + UNIT, lane);
+      M::keys(kb, page);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        if constexpr (Q_LDS) asm volatile("" ::: "memory");   // one row block's queries at a time
+        const typename M::Query f = query(rb);
+        sa[rb] = M::scores(ka, f);
+        sb[rb] = M::scores(kb, f);
+      }
+    }
+    P pa, pb;
+    pa.load_v(pair, lane);
+    pb.load_v(pair + UNIT, lane);
+    st.weigh(pr, sa, sb, at, edge, scale2);
+    typename M::Values v[L::F32 ? 1 : NB];   // bf16: all blocks, and one branch for the edge; fp32: block by block
+    auto block = [&](auto b_c) -> typename M::Values& { return v[L::F32 ? 0 : decltype(b_c)::value]; };
+    unrolled<NB>([&](auto b_c) {
+      constexpr int b = decltype(b_c)::value;
+      M::template values<b>(block(b_c), pa, pb);
+      if constexpr (L::F32) {
+        if (edge) {
+          asm volatile("");
+          left_out |= st.finite_values(block(b_c), at, end);
+        }
+        st.template add<b>(block(b_c), pr);
+      }
+    });
+    if constexpr (!L::F32) {
+      if (edge) {
+        asm volatile("");
+#pragma unroll
+        for (int b = 0; b < NB; ++b) left_out |= st.finite_values(v[b], at, end);
+      }
+      unrolled<NB>([&](auto b_c) { st.template add<decltype(b_c)::value>(block(b_c), pr); });
+    }
   };
   if (p0 < p1) {
     const int n = p1 - p0;
-    int asked = 0, slot = 0;   // pairs asked for, the ring's slot of the pair at hand
-    for (; asked < D - 1 && asked < n; ++asked) fetch(p0 + asked, asked);
     asm volatile("" : "+v"(ids), "+v"(ids_next));
+    int slot = 0;   // of the ring, of the pair at hand
+    fetch(p0, 0);
 #pragma unroll 1
     for (int k = 0; k < n; ++k) {
       if ((k & 31) == 0 && k) fresh = load_ids(p0 + k + 32);
@@ -559,12 +704,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kvq_attn_kernel(KvqAttn a) {
         if (k & 32) ids = fresh;
         else ids_next = fresh;
       }
-      if (asked < n) {   // the slot that the pair before this one has left
-        fetch(p0 + asked, slot == 0 ? D - 1 : slot - 1);
-        ++asked;
-        __builtin_amdgcn_s_waitcnt(0x0F70 | ((D - 1) * NI & 15) | ((D - 1) * NI >> 4 << 14));   // vmcnt: this pair's copies have landed
-      } else if (D > 2 && k + 1 < n) {
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (NI & 15) | (NI >> 4 << 14));
+      if (k + 1 < n) {   // into the slot that the pair before this one has left
+        fetch(p0 + k + 1, slot ^ 1);
+        __builtin_amdgcn_s_waitcnt(0x0F70 | NI);   // vmcnt: this pair's copies have landed
       } else {
         __builtin_amdgcn_s_waitcnt(0x0F70);
       }
@@ -572,100 +714,147 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kvq_attn_kernel(KvqAttn a) {
       const int base = c0 + (p0 + k) * 32;
       const bool ok_a = valid(id_of(p0 + k, 0)), ok_b = valid(id_of(p0 + k, 1));
       const unsigned char* pair = my_ring + slot * PAIR;
-      work(pair, base, ok_a, ok_b, base + 32 > all_see || base + 32 > c1 || !ok_a || !ok_b);
+      work(pair, Seen{base, g, ok_a, ok_b}, base + 32 > all_see || !ok_a || !ok_b);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the pair has been read before its slot is filled again
-      slot = slot + 1 == D ? 0 : slot + 1;
+      slot ^= 1;
     }
+    if (left_out)
+#pragma unroll 1
+      for (int k = 0; k < n; ++k) {
+        const int base = c0 + (p0 + k) * 32, ia = table[min(2 * (p0 + k), last_page)], ib = table[min(2 * (p0 + k) + 1, last_page)];
+        if (base + 32 > all_see || !valid(ia) || !valid(ib))
+          st.template add_left_out<P>(layer + (size_t)(valid(ia) ? ia : 0) * page_bytes, layer + (size_t)(valid(ib) ? ib : 0) * page_bytes, Seen{base, g, valid(ia), valid(ib)}, end, lane);
+      }
   }
   __syncthreads();   // the wavefronts' outputs overlay the ring
 
   // ---- the wavefronts' results become one ----
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const float l = M::total(sum[rb]);
+    const float l = M::total(st.sum[rb]);
     if (g == 0) {
-      s_m[wave][rb * 16 + col] = m_run[rb];
+      s_m[wave][rb * 16 + col] = st.m_run[rb];
       s_l[wave][rb * 16 + col] = l;
     }
   }
-  const int parts = (end + a.chunk - 1) / a.chunk;
+  const bool whole = end <= chunk;   // the only range: nothing to merge
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     if (rb * 16 >= n_rows) break;
     if (rb) __syncthreads();
 #pragma unroll
-    for (int t = 0; t < 2 * NB; ++t) *reinterpret_cast<f32x4*>(&s_o[wave][col][t * 16 + 4 * g]) = acc[rb][t];
+    for (int t = 0; t < 2 * NB; ++t) *reinterpret_cast<f32x4*>(&s_o[wave][col][t * 16 + 4 * g]) = st.acc[rb][t];
     __syncthreads();
-    const int r = threadIdx.x >> 4, row = row0 + rb * 16 + r;
+    constexpr int LANES = WAVES * 4;   // of a row
+    const int r = threadIdx.x / LANES;
     if (rb * 16 + r < n_rows) {
-      float m_all = -INFINITY, l = 0.f, f[kWaves];
+      float m_all = -INFINITY, l = 0.f, f[WAVES];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) m_all = fmaxf(m_all, s_m[w][rb * 16 + r]);
+      for (int w = 0; w < WAVES; ++w) m_all = fmaxf(m_all, s_m[w][rb * 16 + r]);
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < WAVES; ++w) {
         const float m = s_m[w][rb * 16 + r];
         f[w] = m == m_all ? 1.f : __builtin_amdgcn_exp2f(m - m_all);   // (no key in any: all are minus infinity and all sums 0)
         l += f[w] * s_l[w][rb * 16 + r];
       }
-      const int j = row / group, h = kvh * group + row % group;
-      const size_t at = (s * (size_t)a.rows + j) * a.n_q_heads + h;
-      const bool whole = parts <= 1;
+      int j, h;
+      slot_of(row0 + rb * 16 + r, group, j, h);
+      h += kvh * group;
+      const size_t at = (s * (size_t)a.rows + j) * a.n_q_heads + h, in_part = (part * (size_t)a.rows + j) * a.n_q_heads;
       const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-      for (int d = 4 * (threadIdx.x & 15); d < hd; d += 64) {
+      for (int d = 4 * (threadIdx.x % LANES); d < hd; d += 4 * LANES) {
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][r][d]) * f[w];
+        for (int w = 0; w < WAVES; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][r][d]) * f[w];
         o *= inv;
         if (whole) store_row4(static_cast<T*>(a.out) + at * hd + d, o);
-        else *reinterpret_cast<f32x4*>(a.part_o + (at * a.splits + split) * hd + d) = o;
+        else *reinterpret_cast<f32x4*>(a.part_o + (in_part + h) * hd + d) = o;
       }
-      if (!whole && (threadIdx.x & 15) == 0) a.part_ml[at * a.splits + split] = make_float2(m_all, l);
+      if (!whole && threadIdx.x % LANES == 0) a.part_ml[in_part + h] = make_float2(m_all, l);
     }
   }
 }
 
-// A row's ranges in their order: 32 lanes a row, four dims each.
-template <typename T, int RB16>
-__global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a, long long n_rows) {
-  const long long at = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (at >= n_rows) return;
-  const int hq = (int)(at % a.n_q_heads), group = a.n_q_heads / a.c.n_kv_heads;
-  const int j = (int)(at / a.n_q_heads % a.rows), s = (int)(at / a.n_q_heads / a.rows);
+// A row's ranges: 32 lanes (four dims a lane) a row, or eight times 32, which take every eighth range and are joined in their order (few rows of many ranges: 1024 rows of
+// up to 12, 8.7 -> 5.4 us; 8192 rows of up to 5 are better off with 32 lanes, 16.6 -> 5.5 us).  grid: rows of a sequence and heads / (8 / GROUPS), sequences.
+template <typename T, int ROWS, int GROUPS>
+__global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
+  __shared__ float s_m[8], s_l[8];
+  __shared__ __attribute__((aligned(16))) float s_o[GROUPS][132];
+  const int s = blockIdx.y, of = threadIdx.x >> 5, at = GROUPS == 8 ? blockIdx.x : blockIdx.x * 8 + of;
+  const int j = at / a.n_q_heads, h = at % a.n_q_heads, group = a.n_q_heads / a.c.n_kv_heads;
   const SeqRows rows(a, s);
+  const Ranges ranges(a);
+  const int first = ranges.first_of(a, s);
   if (j >= rows.count) return;
-  const int row = j * group + hq % group, tile = row / (16 * RB16);
-  const int last = min((tile + 1) * 16 * RB16, rows.count * group) - 1;
-  const int parts = (rows.end(a, last / group) + a.chunk - 1) / a.chunk;
+  const int tile = (j * group + h % group) / ROWS, last = min((tile + 1) * ROWS, rows.count * group) - 1;
+  const int parts = ranges.count(rows.end(a, last / group));   // of the row's tile
   if (parts <= 1) return;
   const int d = 4 * (threadIdx.x & 31), hd = a.c.hd;
-  const float2* ml = a.part_ml + at * a.splits;
-  float m_all = -INFINITY;
-  for (int p = 0; p < parts; ++p) m_all = fmaxf(m_all, ml[p].x);
+  const size_t step = (size_t)a.rows * a.n_q_heads, from = (first * (size_t)a.rows + j) * a.n_q_heads + h;
+  float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  for (int p = 0; p < parts; ++p) {
-    const float2 x = ml[p];
-    const float f = x.x == m_all ? 1.f : __builtin_amdgcn_exp2f(x.x - m_all);
-    l += f * x.y;
-    if (d < hd) o += *reinterpret_cast<const f32x4*>(a.part_o + (at * a.splits + p) * hd + d) * f;
+  constexpr int AHEAD = 4;
+  for (int p0 = GROUPS == 8 ? of : 0; p0 < parts; p0 += GROUPS * AHEAD) {
+    float2 x[AHEAD];
+    f32x4 y[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int p = min(p0 + i * GROUPS, parts - 1);
+      x[i] = a.part_ml[from + p * step];
+      y[i] = *reinterpret_cast<const f32x4*>(a.part_o + (from + p * step) * hd + min(d, hd - 4));
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (p0 + i * GROUPS >= parts) break;
+      const float top = fmaxf(m, x[i].x), f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), fx = x[i].x == top ? 1.f : __builtin_amdgcn_exp2f(x[i].x - top);
+      m = top;
+      l = f * l + fx * x[i].y;
+      o = o * f + y[i] * fx;
+    }
   }
-  if (d < hd) store_row4(static_cast<T*>(a.out) + at * hd + d, o * (l == 0.f ? 0.f : 1.f / l));
+  if constexpr (GROUPS == 8) {
+    *reinterpret_cast<f32x4*>(&s_o[of][d]) = o;
+    if (d == 0) {
+      s_m[of] = m;
+      s_l[of] = l;
+    }
+    __syncthreads();
+    if (of) return;
+    float m_all = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m_all = fmaxf(m_all, s_m[i]);
+    l = 0.f;
+    o = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = s_m[i] == m_all ? 1.f : __builtin_amdgcn_exp2f(s_m[i] - m_all);
+      l += f * s_l[i];
+      o += *reinterpret_cast<const f32x4*>(&s_o[i][d]) * f;
+    }
+  }
+  if (d < hd) store_row4(static_cast<T*>(a.out) + ((s * (size_t)a.rows + j) * a.n_q_heads + h) * hd + d, o * (l == 0.f ? 0.f : 1.f / l));
 }
 
-int row_blocks(bool bf16, int rows) { return rows <= 16 ? 1 : rows <= 32 || !bf16 ? 2 : 4; }
+int tile_rows(bool bf16, int rows) { return rows <= 16 ? 16 : rows <= 32 || !bf16 ? 32 : 64; }
 
 template <typename T, int NB, int KB, int VB>
-void launch(const KvqAttn& a, int rb, hipStream_t st) {
-  const dim3 grid((unsigned)((long long)a.n_seqs * a.tiles * a.splits * a.c.n_kv_heads)), block(64 * kWaves);
-  const long long rows = (long long)a.n_seqs * a.rows * a.n_q_heads;
-  const dim3 merge((unsigned)((rows + 7) / 8));
+void launch(const KvqAttn& a, int tile, hipStream_t st) {
+  const dim3 grid((unsigned)((long long)(a.n_seqs + a.parts) * a.tiles * a.c.n_kv_heads));
+  auto join = [&](auto rows_c) {
+    constexpr int ROWS = decltype(rows_c)::value;
+    const int rows = a.rows * a.n_q_heads;
+    if (!a.parts) return;
+    if ((long long)rows * a.n_seqs < 4096) hipLaunchKernelGGL((kvq_merge_kernel<T, ROWS, 8>), dim3(rows, a.n_seqs), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((kvq_merge_kernel<T, ROWS, 1>), dim3((rows + 7) / 8, a.n_seqs), dim3(256), 0, st, a);
+  };
   auto go = [&](auto rb_c) {
     constexpr int RB = decltype(rb_c)::value;
-    hipLaunchKernelGGL((kvq_attn_kernel<T, NB, KB, VB, RB>), grid, block, 0, st, a);
-    if (a.splits > 1) hipLaunchKernelGGL((kvq_merge_kernel<T, RB>), merge, dim3(256), 0, st, a, rows);
+    hipLaunchKernelGGL((kvq_attn_kernel<T, NB, KB, VB, RB>), grid, dim3(64 * Launch<T, NB, KB, VB, RB>::WAVES), 0, st, a);
+    join(std::integral_constant<int, 16 * RB>());
   };
-  if (rb == 1) go(std::integral_constant<int, 1>());
-  else if (rb == 2) go(std::integral_constant<int, 2>());
+  if (tile == 16) go(std::integral_constant<int, 1>());
+  else if (tile == 32) go(std::integral_constant<int, 2>());
   else if constexpr (std::is_same<T, bf16_t>::value) go(std::integral_constant<int, 4>());
 }
 template <typename T, int NB>
@@ -686,20 +875,18 @@ void launch_type(const KvqAttn& a, int rb, hipStream_t st) {
 }  // namespace
 
 bool kvq_attn_plan(KvqAttn& a, bool bf16, int max_tokens, size_t part_rows) {
-  const int rows = a.rows * (a.n_q_heads / a.c.n_kv_heads), rb = row_blocks(bf16, rows);
-  a.tiles = (rows + 16 * rb - 1) / (16 * rb);
-  const long long wgs = (long long)a.n_seqs * a.c.n_kv_heads * a.tiles;
-  const long long room = std::max<long long>(1, (long long)(part_rows / ((size_t)a.n_seqs * a.rows * a.n_q_heads)));
-  const long long want = std::max<long long>(1, (2048 + wgs - 1) / wgs), most = std::max(1, max_tokens / 256);
-  const int splits = (int)std::min(std::min(want, most), room);
-  a.chunk = std::max(128, (int)(((long long)max_tokens + splits - 1) / splits + 127) / 128 * 128);
-  a.splits = std::max(1, (max_tokens + a.chunk - 1) / a.chunk);
-  a.limit = (int)std::min<long long>((long long)a.splits * a.chunk, 0x7FFFFFFF);
-  return wgs * a.splits <= 0x7FFFFFFFll && ((long long)a.n_seqs * a.rows * a.n_q_heads + 7) / 8 <= 0x7FFFFFFFll;
+  const int rows = a.rows * (a.n_q_heads / a.c.n_kv_heads), tile = tile_rows(bf16, rows);
+  a.tiles = (rows + tile - 1) / tile;
+  const long long heads = (long long)a.c.n_kv_heads * a.tiles, room = (long long)(part_rows / ((size_t)a.rows * a.n_q_heads)) - a.n_seqs;
+  const int wgs = tile == 16 ? 1536 : 512;   // twice as many as the card holds (single tokens 640: 120 us, 1536: 116, 4096: 123), or as many (blocks of 16 rows 256: 40, 512: 38, 1024: 44)
+  const long long parts = std::min(wgs / heads, room);
+  // Sequences are half as long as the longest, say: with enough of them no range would be cut.
+  a.parts = parts > 0 && parts * 2 > a.n_seqs && max_tokens > 32 * kMinPairs ? (int)parts : 0;
+  return (a.n_seqs + a.parts) * heads <= 0x7FFFFFFFll;
 }
 
 void kvq_attn_launch(const KvqAttn& a, bool bf16, hipStream_t st) {
-  const int rb = row_blocks(bf16, a.rows * (a.n_q_heads / a.c.n_kv_heads));
-  if (bf16) launch_type<bf16_t>(a, rb, st);
-  else launch_type<float>(a, rb, st);
+  const int tile = tile_rows(bf16, a.rows * (a.n_q_heads / a.c.n_kv_heads));
+  if (bf16) launch_type<bf16_t>(a, tile, st);
+  else launch_type<float>(a, tile, st);
 }
