@@ -276,7 +276,8 @@ class Engine:
         """A cache held in 4 or 8 bits over the bytes of `data` (uint8, on the engine's device, kvq_bytes() of them; the struct keeps the tensor)."""
         assert data.dtype == torch.uint8 and data.is_contiguous() and data.device == self.target_pool.device
         q = Kvq(_ptr(data), data.numel(), int(pool), int(n_pages), int(k_bits), int(v_bits))
-        q.keep = data
+        m = self.target if pool == DFLASH_POOL_TARGET else self.draft
+        q.keep, q.heads, q.dtype = data, (m.n_kv_heads, m.n_q_heads, m.head_dim), torch.bfloat16 if self.dtype == "bf16" else torch.float32
         return q
 
     def profile_enable(self, on: bool):
@@ -424,57 +425,55 @@ def dflash_group_attention(e: Engine, batch: Batch, groups: Groups, pool: int, l
 
 
 # ---- caches held in 4 or 8 bits (same names as the C ABI) -----------------------------------------------
-def _rows_like(e: Engine, batch: Batch, cache: Kvq, heads: str, *tensors: torch.Tensor) -> int:
-    """Checks [S, rows, heads, head_dim] tensors in the model's dtype; rows."""
-    m = e.target if cache.pool == DFLASH_POOL_TARGET else e.draft
-    dt = torch.bfloat16 if e.dtype == "bf16" else torch.float32
-    for t in tensors:
-        assert t.dim() == 4 and tuple(t.shape) == (batch.n_seqs, tensors[0].shape[1], getattr(m, heads), m.head_dim) and t.dtype == dt, (tuple(t.shape), t.dtype)
-    return int(tensors[0].shape[1])
+def _rows_like(batch: Batch, cache: Kvq, which: int, a: torch.Tensor, b: torch.Tensor) -> int:
+    """Checks two [S, rows, heads, head_dim] tensors in the model's dtype (which: 0 kv heads, 1 query heads); rows.  (Small calls are bound by what happens here.)"""
+    sh, dt = a.shape, cache.dtype
+    assert len(sh) == 4 and sh[0] == batch.n_seqs and sh[2] == cache.heads[which] and sh[3] == cache.heads[2], tuple(sh)
+    assert b.shape == sh and a.dtype is dt and b.dtype is dt, (tuple(b.shape), a.dtype, b.dtype)
+    return sh[1]
 
 
-def _counts(batch: Batch, *tensors: Optional[torch.Tensor]):
-    for t in tensors:
-        assert t is None or (t.dtype == torch.int32 and tuple(t.shape) == (batch.n_seqs,)), (t.dtype, tuple(t.shape))
+def _count_ptr(batch: Batch, t: Optional[torch.Tensor]) -> Optional[int]:
+    if t is None:
+        return None
+    assert t.dtype is torch.int32 and t.dim() == 1 and t.shape[0] == batch.n_seqs, (t.dtype, tuple(t.shape))
+    return _ptr(t)
 
 
 def dflash_kvq_write(e: Engine, batch: Batch, cache: Kvq, layer: int, k: torch.Tensor, v: torch.Tensor, counts: Optional[torch.Tensor] = None):
     """Rows k, v [S, rows, n_kv_heads, head_dim] to positions seq_lens[s] .. + counts[s] - 1 (None: all rows) of one layer of the cache."""
-    rows = _rows_like(e, batch, cache, "n_kv_heads", k, v)
-    _counts(batch, counts)
-    _check(e.l.dflash_kvq_write(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _ptr(counts), _ptr(k), _ptr(v), _stream()), e.ctx)
+    rows = _rows_like(batch, cache, 0, k, v)
+    _check(e.l.dflash_kvq_write(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _count_ptr(batch, counts), _ptr(k), _ptr(v), _stream()), e.ctx)
 
 
 def dflash_kvq_read(e: Engine, batch: Batch, cache: Kvq, layer: int, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor,
                     counts: Optional[torch.Tensor] = None):
     """Positions starts[s] .. + counts[s] - 1 of one layer of the cache into rows k, v [S, rows, n_kv_heads, head_dim]."""
-    rows = _rows_like(e, batch, cache, "n_kv_heads", k, v)
-    _counts(batch, starts, counts)
-    _check(e.l.dflash_kvq_read(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _ptr(starts), _ptr(counts), _ptr(k), _ptr(v), _stream()), e.ctx)
+    rows = _rows_like(batch, cache, 0, k, v)
+    _check(e.l.dflash_kvq_read(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _count_ptr(batch, starts), _count_ptr(batch, counts), _ptr(k), _ptr(v),
+                               _stream()), e.ctx)
 
 
 def dflash_kvq_attention(e: Engine, batch: Batch, cache: Kvq, layer: int, q: torch.Tensor, out: torch.Tensor, counts: Optional[torch.Tensor] = None,
                          causal: bool = True):
     """Attention of q [S, rows, n_q_heads, head_dim] at positions seq_lens[s] .. + counts[s] - 1 over one layer of the cache, into out (same shape)."""
-    rows = _rows_like(e, batch, cache, "n_q_heads", q, out)
-    _counts(batch, counts)
-    _check(e.l.dflash_kvq_attention(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _ptr(counts), int(causal), _ptr(q), _ptr(out), _stream()), e.ctx)
+    rows = _rows_like(batch, cache, 1, q, out)
+    _check(e.l.dflash_kvq_attention(e.ctx, C.byref(batch), C.byref(cache), layer, rows, _count_ptr(batch, counts), causal, _ptr(q), _ptr(out), _stream()), e.ctx)
 
 
-def _page_table(e: Engine, batch: Batch, table: torch.Tensor):
-    assert table.dtype == torch.int32 and tuple(table.shape) == (batch.n_seqs, e.max_pages_per_seq), (table.dtype, tuple(table.shape))
+def _page_table(e: Engine, batch: Batch, table: torch.Tensor) -> int:
+    assert table.dtype is torch.int32 and table.shape == (batch.n_seqs, e.max_pages_per_seq), (table.dtype, tuple(table.shape))
+    return _ptr(table)
 
 
 def dflash_kvq_pack(e: Engine, batch: Batch, cache: Kvq, table: torch.Tensor):
     """The batch's cached rows, all layers, from the context's pool to the cache's pages `table` [S, max_pages_per_seq]."""
-    _page_table(e, batch, table)
-    _check(e.l.dflash_kvq_pack(e.ctx, C.byref(batch), C.byref(cache), _ptr(table), _stream()), e.ctx)
+    _check(e.l.dflash_kvq_pack(e.ctx, C.byref(batch), C.byref(cache), _page_table(e, batch, table), _stream()), e.ctx)
 
 
 def dflash_kvq_unpack(e: Engine, batch: Batch, cache: Kvq, table: torch.Tensor):
     """... and from the cache's pages `table` to those of the batch's block table in the context's pool."""
-    _page_table(e, batch, table)
-    _check(e.l.dflash_kvq_unpack(e.ctx, C.byref(batch), C.byref(cache), _ptr(table), _stream()), e.ctx)
+    _check(e.l.dflash_kvq_unpack(e.ctx, C.byref(batch), C.byref(cache), _page_table(e, batch, table), _stream()), e.ctx)
 
 
 # ---- machine probes (same names as the C ABI) -----------------------------------------------------------
