@@ -314,15 +314,15 @@ size_t dflash_kvq_bytes(const dflash_dims *model, int32_t n_pages, int32_t k_bit
  * counts[s] (device, [S], nullable: all `rows`), goes to position seq_lens[s] + j of one layer.  Nothing else of a page changes.  seq_lens is not advanced. */
 int dflash_kvq_write(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, int32_t layer, int32_t rows, const int32_t *counts, const void *k,
                      const void *v, void *stream);
-/* ... and back, from position starts[s] + j (device, [S]), rounded once to the model's dtype; rows behind counts[s] are left as they are.  batch->seq_lens is not looked at. */
+/* ... and back, from position starts[s] + j (device, [S]), rounded once to the model's dtype (a number beyond its largest becomes an infinity); rows behind counts[s] are left as they are.  batch->seq_lens is not looked at. */
 int dflash_kvq_read(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, int32_t layer, int32_t rows, const int32_t *starts, const int32_t *counts,
                     void *k, void *v, void *stream);
 
 /* Attention over the cache: rows j < counts[s] (nullable: all `rows`) of sequence s at positions seq_lens[s] + j, whose own K/V rows are there already; causal != 0: row j sees
  * positions up to seq_lens[s] + j, else all seq_lens[s] + counts[s].  rows >= 1, not bound to the context's block size: 1 is plain decoding, hundreds are a piece of a prompt.  The batch's
- * max_seq_len bounds seq_lens (a longer sequence's last keys may be left out: sticky status).  Entries of the block table outside the cache are keys that are not there; a row that sees no key is zeros.  An infinity or NaN in a row of K or V
+ * max_seq_len balances launches only.  Entries of the block table outside the cache are keys that are not there; a row that sees no key is zeros.  An infinity or NaN in a row of K or V
  * reaches the rows that see the key, and only them.  q (device) [S, rows, n_q_heads, head_dim] after norm and rotation, out (device) the same shape; both in the model's dtype, contiguous,
- * 16-byte aligned, not the same buffer; rows behind counts[s] are left as they are.  Uses the workspace as the step's calls do. */
+ * 16-byte aligned, apart from each other; rows behind counts[s] are left as they are.  Uses the workspace as the step's calls do. */
 int dflash_kvq_attention(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, int32_t layer, int32_t rows, const int32_t *counts, int32_t causal,
                          const void *q, void *out, void *stream);
 

@@ -1482,6 +1482,10 @@ int check_kvq_rows(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q, 
   if ((int64_t)rows * m.n_q_heads > INT32_MAX / 4) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: %d rows are too many", what, rows);
   return DFLASH_OK;
 }
+bool overlap(const void* a, const void* b, size_t bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y ? y - x < bytes : x - y < bytes;
+}
 int kvq_rows_checked(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q, int layer, int rows, const int32_t* first, const int32_t* counts, void* k, void* v,
                      bool write, void* stream) {
   const char* what = write ? "kvq_write" : "kvq_read";
@@ -1492,6 +1496,7 @@ int kvq_rows_checked(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q
   if (!first) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: null starts", what);
   if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: k and v must be 16-byte aligned device buffers", what);
   const dflash_dims& m = kvq_model(ctx, q);
+  if (!write && overlap(k, v, (size_t)b->n_seqs * rows * m.n_kv_heads * m.head_dim * esize(m.dtype))) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: k and v overlap", what);
   const KvqRows a{kvq_cache(m, q), layer, b->n_seqs, rows, ctx->rt.max_pages_per_seq, first, counts, b->block_table, k, v,
                   reinterpret_cast<int32_t*>(ctx->wsp + ctx->ws.status)};
   (write ? kvq_write_launch : kvq_read_launch)(a, m.dtype == DFLASH_BF16, (hipStream_t)stream);
@@ -1991,8 +1996,9 @@ int dflash_kvq_attention(dflash_ctx* ctx, const dflash_batch* batch, const dflas
   if ((rc = check_batch(ctx, batch))) return rc;
   if (batch->n_seqs == 0) return DFLASH_OK;
   if ((rc = check_kvq(ctx, batch, cache, "kvq_attention")) || (rc = check_kvq_rows(ctx, batch, cache, layer, rows, "kvq_attention"))) return rc;
-  if (!q || !out || q == out || (((uintptr_t)q | (uintptr_t)out) & 15)) return CTX_FAIL(ctx, DFLASH_EINVAL, "kvq_attention: q and out must be two 16-byte aligned device buffers");
+  if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 15)) return CTX_FAIL(ctx, DFLASH_EINVAL, "kvq_attention: q and out must be 16-byte aligned device buffers");
   const dflash_dims& m = kvq_model(ctx, cache);
+  if (overlap(q, out, (size_t)batch->n_seqs * rows * m.n_q_heads * m.head_dim * esize(m.dtype))) return CTX_FAIL(ctx, DFLASH_EINVAL, "kvq_attention: q and out overlap");
   KvqAttn a{};
   a.c = kvq_cache(m, cache);
   a.layer = layer; a.n_seqs = batch->n_seqs; a.rows = rows; a.causal = causal != 0; a.n_q_heads = m.n_q_heads; a.mpps = ctx->rt.max_pages_per_seq;

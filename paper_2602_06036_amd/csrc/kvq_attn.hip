@@ -878,8 +878,12 @@ bool kvq_attn_plan(KvqAttn& a, bool bf16, int max_tokens, size_t part_rows) {
   const int rows = a.rows * (a.n_q_heads / a.c.n_kv_heads), tile = tile_rows(bf16, rows);
   a.tiles = (rows + tile - 1) / tile;
   const long long heads = (long long)a.c.n_kv_heads * a.tiles, room = (long long)(part_rows / ((size_t)a.rows * a.n_q_heads)) - a.n_seqs;
-  const int wgs = tile == 16 ? 1536 : 512;   // twice as many as the card holds (single tokens 640: 120 us, 1536: 116, 4096: 123), or as many (blocks of 16 rows 256: 40, 512: 38, 1024: 44)
-  const long long parts = std::min(wgs / heads, room);
+  // Twice as many workgroups as the card holds (single tokens, 640: 114 us, 1536: 111, 2176: 111), or as many: a few that come behind the others cost a round (blocks of
+  // 16 rows, 384: 35 us, 448: 33, 512: 38), so half a range a sequence, by which there are more of them, is left out where sequences have several.
+  const int wgs = tile == 16 ? 1536 : 512;
+  long long parts = wgs / heads;
+  if (tile > 16 && 2 * parts >= 3 * a.n_seqs) parts -= a.n_seqs / 2;
+  parts = std::min(parts, room);
   // Sequences are half as long as the longest, say: with enough of them no range would be cut.
   a.parts = parts > 0 && parts * 2 > a.n_seqs && max_tokens > 32 * kMinPairs ? (int)parts : 0;
   return (a.n_seqs + a.parts) * heads <= 0x7FFFFFFFll;

@@ -224,6 +224,65 @@ def test_attention_of_split_ranges(dtype, heads, kv, hd, bits, rows):
         assert x.torch.equal(again, out)
 
 
+@pytest.mark.parametrize("dtype,heads,kv,hd,bits,rows", [("bf16", 2, 1, 128, (4, 4), 1), ("bf16", 4, 2, 64, (8, 8), 9), ("bf16", 2, 1, 96, (4, 8), 33), ("f32", 2, 1, 32, (8, 4), 2),
+                                                         ("f32", 2, 1, 128, (4, 8), 20)])
+def test_attention_of_long_ranges(dtype, heads, kv, hd, bits, rows):
+    """A hint of no tokens: nothing is cut, and a wavefront has more pages than it asks the ids of at once; a page is missing in the middle."""
+    lens, counts = (9100, 40), (rows, rows)
+    x = Setup(dtype, heads, kv, hd, bits, 2, [n + rows for n in lens], seed=hd)
+    x.table[0, 77] = -1
+    x.poison(lens, counts)
+    x.upload()
+    q, out = x.rows((2, rows, heads, hd), 0.7), x.rows((2, rows, heads, hd))
+    before = out.clone()
+    x.B.dflash_kvq_attention(x.e, x.batch(lens, 0), x.cache, 1, q, out)
+    x.e.device_status()
+    _check(x, q, out, before, lens, counts, True, 1, "long")
+
+
+def test_attention_over_the_draft_and_many_sequences():
+    """The draft's shape where it is another than the target's; more sequences than a wavefront has lanes, some without rows."""
+    import paper_2602_06036_amd as dfl
+    from paper_2602_06036_amd import binding as B
+    torch = _torch()
+    S, rng = 150, np.random.RandomState(0)
+    lens = rng.randint(0, 90, S)
+    lens[::40] = rng.randint(700, 1500, len(lens[::40]))
+    counts = rng.randint(0, 3, S)
+    held = -(-(lens + 2) // PAGE)
+    width, n_pages = int(held.max()) + 1, int(held.sum())
+    e = dfl.Engine(dims(2, 4, 2, 128), dims(3, 4, 1, 64), "bf16", 2, S, width, 1, (0,), 63).create()
+    table, ids, at = np.full((S, width), -1, np.int32), rng.permutation(n_pages).astype(np.int32), 0
+    for s in range(S):
+        table[s, :held[s]] = ids[at:at + held[s]]
+        at += held[s]
+    assert e.kvq_bytes(1, n_pages, 8, 4) == 3 * n_pages * km.unit_bytes(64, 8, 4)
+    data = torch.zeros(e.kvq_bytes(1, n_pages, 8, 4), dtype=torch.uint8, device=e.device)
+    cache = e.kvq(data, 1, n_pages, 8, 4)
+    i32 = lambda t: torch.from_numpy(np.asarray(t, np.int32)).to(e.device)
+    g = torch.Generator(device=e.device)
+    g.manual_seed(3)
+    rows = int(lens.max()) + 2
+    k, v = (torch.randn((S, rows, 1, 64), generator=g, device=e.device).bfloat16() for _ in range(2))
+    zero, table_dev, lens_dev, all_dev, counts_dev = i32(0 * lens), i32(table), i32(lens), i32(lens + counts), i32(counts)
+    B.dflash_kvq_write(e, e.batch(zero, table_dev, zero, 0), cache, 2, k, v, counts=all_dev)
+    q = torch.randn((S, 2, 4, 64), generator=g, device=e.device).bfloat16()
+    for hint in (int(lens.max()), 90):
+        out = torch.full_like(q, 7.0)
+        before = out.clone()
+        B.dflash_kvq_attention(e, e.batch(lens_dev, table_dev, zero, hint), cache, 2, q, out, counts=counts_dev, causal=False)
+        e.device_status()
+        ref = km.Cache(data.view(3, n_pages, 1, -1).cpu().numpy(), 64, 8, 4)
+        exact, slack, wabs = km.attention64(f64(q), *ref.rows(2), table, lens, counts, False, n_pages)
+        for s in range(S):
+            c = counts[s]
+            assert np.array_equal(f64(out)[s, c:], f64(before)[s, c:])
+            assert (np.abs(f64(out)[s, :c] - exact[s, :c]) <= km.allowed(exact, slack, wabs, "bf16")[s, :c]).all(), s
+    for bad in (k[..., :32], k):          # the draft's rows are 64 wide, the queries' heads four
+        with pytest.raises(AssertionError):
+            B.dflash_kvq_attention(e, e.batch(lens_dev, table_dev, zero, 90), cache, 2, bad.contiguous(), torch.zeros_like(bad.contiguous()))
+
+
 @pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 48)])
 def test_missing_pages_and_sequences_that_outgrow_the_table(dtype, hd):
     lens, counts, rows = [100, 70, 20, 0], [3, 3, 3, 3], 3
@@ -582,7 +641,7 @@ def test_refusals():
 
     def each(c, layer=0, rows=3):
         yield e.l.dflash_kvq_write(e.ctx, C.byref(b), C.byref(c), layer, rows, None, P(k), P(k), None)
-        yield e.l.dflash_kvq_read(e.ctx, C.byref(b), C.byref(c), layer, rows, P(x.lens_dev), None, P(k), P(k), None)
+        yield e.l.dflash_kvq_read(e.ctx, C.byref(b), C.byref(c), layer, rows, P(x.lens_dev), None, P(k), P(q), None)
         yield e.l.dflash_kvq_attention(e.ctx, C.byref(b), C.byref(c), layer, rows, None, 1, P(q), P(out), None)
 
     def pages(c):
@@ -601,7 +660,9 @@ def test_refusals():
             refused(code, word, rc)
     c = cache()
     refused(E, "aligned", e.l.dflash_kvq_attention(e.ctx, C.byref(b), C.byref(c), 0, 3, None, 1, P(q) + 2, P(out), None))
-    refused(E, "two", e.l.dflash_kvq_attention(e.ctx, C.byref(b), C.byref(c), 0, 3, None, 1, P(q), P(q), None))
+    refused(E, "overlap", e.l.dflash_kvq_attention(e.ctx, C.byref(b), C.byref(c), 0, 3, None, 1, P(q), P(q), None))
+    refused(E, "overlap", e.l.dflash_kvq_attention(e.ctx, C.byref(b), C.byref(c), 0, 3, None, 1, P(q), P(q) + q.numel() * 2 - 16, None))
+    refused(E, "overlap", e.l.dflash_kvq_read(e.ctx, C.byref(b), C.byref(c), 0, 3, P(x.lens_dev), None, P(k), P(k), None))
     refused(E, "aligned", e.l.dflash_kvq_attention(e.ctx, C.byref(b), C.byref(c), 0, 3, None, 1, None, P(out), None))
     refused(E, "aligned", e.l.dflash_kvq_write(e.ctx, C.byref(b), C.byref(c), 0, 3, None, P(k), None, None))
     refused(E, "starts", e.l.dflash_kvq_read(e.ctx, C.byref(b), C.byref(c), 0, 3, None, None, P(k), P(k), None))
