@@ -522,6 +522,43 @@ struct State {
   }
 };
 
+// A page of a head, UNIT contiguous bytes, from memory to LDS at byte `to`: 1 KB a copy (16 bytes a lane, offsets count on both sides), the last one by as many lanes as are left.
+// One piece of assembly a page: whatever the compiler keeps in m0 is put back once, and the lanes are cut and restored without a branch.  All lanes have to be on.
+template <int UNIT, bool NT>
+__device__ __forceinline__ void copy_page(const unsigned char* from, unsigned to, unsigned voff) {
+  constexpr int FULL = UNIT / 1024;
+  constexpr unsigned long long REST = (1ull << (UNIT % 1024 / 16)) - 1;
+  static_assert(FULL <= 4 && REST != 0, "offsets below 4096; scales are always left");
+  to = __builtin_amdgcn_readfirstlane(to);
+  unsigned keep_m0;
+  unsigned long long keep_exec;
+#define KVQ_BEGIN "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_mov_b64 %1, exec\n\ts_nop 0\n\t"
+#define KVQ_COPY(off, nt) "global_load_lds_dwordx4 %3, %4 offset:" #off nt "\n\t"
+#define KVQ_REST "s_mov_b64 exec, %5\n\ts_nop 0\n\t"
+#define KVQ_END "s_mov_b64 exec, %1\n\ts_nop 0\n\ts_mov_b32 m0, %0"
+#define KVQ_ASM(text) asm volatile(KVQ_BEGIN text KVQ_END : "=&s"(keep_m0), "=&s"(keep_exec) : "s"(to), "v"(voff), "s"(from), "s"(REST) : "memory")
+#define KVQ_PAGE(nt)                                                                                                              \
+  if constexpr (FULL == 0) KVQ_ASM(KVQ_REST KVQ_COPY(0, nt));                                                                     \
+  else if constexpr (FULL == 1) KVQ_ASM(KVQ_COPY(0, nt) KVQ_REST KVQ_COPY(1024, nt));                                             \
+  else if constexpr (FULL == 2) KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(1024, nt) KVQ_REST KVQ_COPY(2048, nt));                          \
+  else if constexpr (FULL == 3) KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(1024, nt) KVQ_COPY(2048, nt) KVQ_REST KVQ_COPY(3072, nt));       \
+  else KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(1024, nt) KVQ_COPY(2048, nt) KVQ_COPY(3072, nt))
+  if constexpr (NT) { KVQ_PAGE(" nt"); }
+  else { KVQ_PAGE(""); }
+  if constexpr (FULL == 4) {   // the rest lies behind the largest offset
+    from += 4096;
+    to += 4096;
+    if constexpr (NT) KVQ_ASM(KVQ_REST KVQ_COPY(0, " nt"));
+    else KVQ_ASM(KVQ_REST KVQ_COPY(0, ""));
+  }
+#undef KVQ_PAGE
+#undef KVQ_ASM
+#undef KVQ_END
+#undef KVQ_REST
+#undef KVQ_COPY
+#undef KVQ_BEGIN
+}
+
 // grid: kv heads (fastest) x row tiles x ranges, or sequences where each is one range (a.parts = 0)
 template <typename T, int NB, int KB, int VB, int RB>
 struct Launch {
@@ -614,37 +651,23 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
   const size_t page_bytes = (size_t)H * UNIT;
   const float scale2 = a.scale * 1.44269504088896340736f;
 
-  auto valid = [&](int id) { return id >= 0 && id < a.c.n_pages; };
-  // ids of 32 pairs at a time, lane l has page l of them; the next ones are asked for when a set has been used up, and waited for in a branch of their own: where every turn
-  // used a register that a load may still be on its way to, the compiler would have every turn wait for all copies
+  // ids of 32 pairs at a time, lane l has page l of them (-1: not there); the next ones are asked for when a set has been used up, and waited for in a branch of their own: where
+  // every turn used a register that a load may still be on its way to, the compiler would have every turn wait for all copies
   auto load_ids = [&](int p) { return table[min(2 * p + lane, last_page)]; };
+  auto there_or_not = [&](int id) { return id >= 0 && id < a.c.n_pages ? id : -1; };
   int ids = load_ids(p0), ids_next = load_ids(p0 + 32), fresh = 0;
-  auto id_of = [&](int p, int i) { return __builtin_amdgcn_readlane((p - p0) & 32 ? ids_next : ids, ((p - p0) & 31) * 2 + i); };
   const unsigned ring = (unsigned)(size_t)&s_raw[0] + (unsigned)wave * (PAIR * 2);
   const unsigned char* my_ring = s_raw + wave * (PAIR * 2);
   const unsigned voff = lane * 16;
-  auto copy = [&](const unsigned char* from, unsigned at) {   // 1 KB, or as far as the page goes
-    const unsigned dst = __builtin_amdgcn_readfirstlane(ring + at);
-    unsigned keep_m0;   // whatever the compiler keeps in m0 is put back
+  auto unit_of = [&](int id) { return layer + (uint64_t)(unsigned)max(id, 0) * (unsigned)page_bytes; };   // pages that are not there alias a readable one and weigh nothing
+  struct Ids { int a, b; };
+  auto fetch = [&](int k, int slot) {
+    const int from = k & 32 ? ids_next : ids;
+    const Ids id = {__builtin_amdgcn_readlane(from, (k & 31) * 2), __builtin_amdgcn_readlane(from, (k & 31) * 2 + 1)};
     // bf16, up to 32 rows: they are one tile and nobody else reads these bytes, which need no place in L2 (single tokens 126 -> 116 us)
-    if constexpr (!L::F32 && RB < 4)
-      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 nt\n\ts_nop 0\n\ts_mov_b32 m0, %0"
-                   : "=&s"(keep_m0) : "s"(dst), "v"(voff), "s"(from) : "memory");
-    else
-      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_nop 0\n\ts_mov_b32 m0, %0"
-                   : "=&s"(keep_m0) : "s"(dst), "v"(voff), "s"(from) : "memory");
-  };
-  auto fetch = [&](int p, int slot) {   // pages that are not there alias a readable one and weigh nothing
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int id = id_of(p, i);
-      const unsigned char* unit = layer + (size_t)(valid(id) ? id : 0) * page_bytes;
-#pragma unroll
-      for (int c = 0; c < UNIT; c += 1024) {
-        if (UNIT - c >= 1024) copy(unit + c, slot * PAIR + i * UNIT + c);
-        else if (lane < (UNIT - c) / 16) copy(unit + c, slot * PAIR + i * UNIT + c);
-      }
-    }
+    copy_page<UNIT, !L::F32 && RB < 4>(unit_of(id.a), ring + slot * PAIR, voff);
+    copy_page<UNIT, !L::F32 && RB < 4>(unit_of(id.b), ring + slot * PAIR + UNIT, voff);
+    return id;
   };
   bool left_out = false;
   auto work = [&](const unsigned char* pair, const Seen& at, bool edge) {   // edge: some row does not see some key
@@ -693,26 +716,30 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
   };
   if (p0 < p1) {
     const int n = p1 - p0;
+    ids = there_or_not(ids);
+    ids_next = there_or_not(ids_next);
     asm volatile("" : "+v"(ids), "+v"(ids_next));
     int slot = 0;   // of the ring, of the pair at hand
-    fetch(p0, 0);
+    Ids next = fetch(0, 0);
 #pragma unroll 1
     for (int k = 0; k < n; ++k) {
       if ((k & 31) == 0 && k) fresh = load_ids(p0 + k + 32);
       if ((k & 31) == 16 && k > 16) {
+        fresh = there_or_not(fresh);
         asm volatile("" : "+v"(fresh));
         if (k & 32) ids = fresh;
         else ids_next = fresh;
       }
+      const Ids at = next;
       if (k + 1 < n) {   // into the slot that the pair before this one has left
-        fetch(p0 + k + 1, slot ^ 1);
+        next = fetch(k + 1, slot ^ 1);
         __builtin_amdgcn_s_waitcnt(0x0F70 | NI);   // vmcnt: this pair's copies have landed
       } else {
         __builtin_amdgcn_s_waitcnt(0x0F70);
       }
       asm volatile("" ::: "memory");
       const int base = c0 + (p0 + k) * 32;
-      const bool ok_a = valid(id_of(p0 + k, 0)), ok_b = valid(id_of(p0 + k, 1));
+      const bool ok_a = at.a >= 0, ok_b = at.b >= 0;
       const unsigned char* pair = my_ring + slot * PAIR;
       work(pair, Seen{base, g, ok_a, ok_b}, base + 32 > all_see || !ok_a || !ok_b);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the pair has been read before its slot is filled again
@@ -721,9 +748,8 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     if (left_out)
 #pragma unroll 1
       for (int k = 0; k < n; ++k) {
-        const int base = c0 + (p0 + k) * 32, ia = table[min(2 * (p0 + k), last_page)], ib = table[min(2 * (p0 + k) + 1, last_page)];
-        if (base + 32 > all_see || !valid(ia) || !valid(ib))
-          st.template add_left_out<P>(layer + (size_t)(valid(ia) ? ia : 0) * page_bytes, layer + (size_t)(valid(ib) ? ib : 0) * page_bytes, Seen{base, g, valid(ia), valid(ib)}, end, lane);
+        const int base = c0 + (p0 + k) * 32, ia = there_or_not(table[min(2 * (p0 + k), last_page)]), ib = there_or_not(table[min(2 * (p0 + k) + 1, last_page)]);
+        if (base + 32 > all_see || ia < 0 || ib < 0) st.template add_left_out<P>(unit_of(ia), unit_of(ib), Seen{base, g, ia >= 0, ib >= 0}, end, lane);
       }
   }
   __syncthreads();   // the wavefronts' outputs overlay the ring
