@@ -379,20 +379,19 @@ __device__ __forceinline__ int wave_scan(int x) {   // sum over the lanes up to 
 }
 struct Ranges {
   int chunk;   // keys, a multiple of 128
-  int lane;
+  int lane, own;   // page pairs of the sequence of this lane, of the first 64
   __device__ __forceinline__ static int pairs(const KvqAttn& a, int s) { return s < a.n_seqs ? (SeqRows(a, s).n_tok + 31) / 32 : 0; }
-  __device__ __forceinline__ Ranges(const KvqAttn& a) : lane(threadIdx.x & 63) {
-    long long all = 0;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) all += __builtin_amdgcn_readlane(wave_scan(pairs(a, s0 + lane)), 63);
-    const long long each = (all + a.parts - 1) / a.parts;
-    chunk = (int)min(max((each + 3) / 4, (long long)kMinPairs / 4), (long long)(1 << 23)) * 128;
+  __device__ __forceinline__ Ranges(const KvqAttn& a) : lane(threadIdx.x & 63), own(pairs(a, lane)) {
+    float all = 0.f;   // in four pairs; rounding must not make ranges shorter than their share, of which there would be too many
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) all += (float)__builtin_amdgcn_readlane(wave_scan(((s0 ? pairs(a, s0 + lane) : own) + 3) / 4), 63);
+    chunk = min(max((int)min(all / (float)a.parts * 1.0001f, 2e7f) + 1, kMinPairs / 4), (1 << 24) - 1) * 128;
   }
-  __device__ __forceinline__ int count(int tokens) const { return (int)((tokens + (long long)chunk - 1) / chunk); }
+  __device__ __forceinline__ int count(int tokens) const { return (int)(((unsigned)tokens + (unsigned)chunk - 1) / (unsigned)chunk); }
   // the sequence that the f-th range belongs to, and the first of its ranges; false: there are not as many
   __device__ __forceinline__ bool find(const KvqAttn& a, int f, int& s, int& first) const {
     int before = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-      const int mine = (pairs(a, s0 + lane) + chunk / 32 - 1) / (chunk / 32), upto = wave_scan(mine);
+      const int mine = ((s0 ? pairs(a, s0 + lane) : own) + chunk / 32 - 1) / (chunk / 32), upto = wave_scan(mine);
       const unsigned long long behind = __ballot(before + upto > f);
       if (behind) {
         const int at = __ffsll(behind) - 1;
@@ -408,7 +407,7 @@ struct Ranges {
     int before = 0;
     for (int s0 = 0; s0 < s; s0 += 64) {
       const int l = s0 + lane;
-      before += __builtin_amdgcn_readlane(wave_scan(l < s ? (pairs(a, l) + chunk / 32 - 1) / (chunk / 32) : 0), 63);
+      before += __builtin_amdgcn_readlane(wave_scan(l < s ? ((s0 ? pairs(a, l) : own) + chunk / 32 - 1) / (chunk / 32) : 0), 63);
     }
     return before;
   }
