@@ -213,7 +213,7 @@ template <typename T, int HD, bool WRITE>
 __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int slots) {
   constexpr int NB = kvq_blocks(HD), SROW = kvq_scale_row(NB), E = 16 / sizeof(T);   // elements of 16 bytes
   constexpr int ROW = HD / E, PIECES = DF_PAGE * ROW, LD = ROW + 1;                   // 16-byte pieces; LD: rows 16 bytes further in LDS, so that a column lies in all banks
-  __shared__ u32x4 s_rows[kRowWaves][2][DF_PAGE * LD];
+  __shared__ u32x4 s_rows[kRowWaves][WRITE ? 1 : 2][DF_PAGE * LD];   // written: K, then V in its place, which leaves room for six wavefronts a SIMD instead of four
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int i = blockIdx.x * kRowWaves + wave, H = a.c.n_kv_heads;
   if (i >= slots * H) return;
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
     return p < PIECES && key >= key0 && key < key1;
   };
   auto place = [&](T* rows, int key, int c) { return reinterpret_cast<u32x4*>(rows + (((size_t)s * a.rows + (size_t)(j0 + key)) * H + head) * HD) + c; };
-  u32x4 *k_rows = s_rows[wave][0], *v_rows = s_rows[wave][1];
+  u32x4 *k_rows = s_rows[wave][0], *v_rows = s_rows[wave][WRITE ? 0 : 1];
   const int key = lane & 15, b = lane >> 4, bc = min(b, NB - 1);
   const bool there = key >= key0 && key < key1 && b < NB;
   constexpr int N = (PIECES + 63) / 64;
@@ -264,14 +264,13 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
         in[kv][n] = (u32x4){0u, 0u, 0u, 0u};
         if (piece(lane + 64 * n, key2, c)) in[kv][n] = *place(static_cast<T*>(kv ? a.v : a.k), key2, c);
       }
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv)
+    float x[32];
+    auto take = [&](u32x4* rows, const u32x4 (&from)[N]) {
+      sync();
 #pragma unroll
       for (int n = 0; n < N; ++n)
-        if (lane + 64 * n < PIECES) s_rows[wave][kv][(lane + 64 * n) / ROW * LD + (lane + 64 * n) % ROW] = in[kv][n];
-    sync();
-    float x[32];
-    auto take = [&](u32x4* rows) {
+        if (lane + 64 * n < PIECES) rows[(lane + 64 * n) / ROW * LD + (lane + 64 * n) % ROW] = from[n];
+      sync();
 #pragma unroll
       for (int e = 0; e < 32; e += 8) {
         float y[8];
@@ -282,12 +281,12 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
         for (int i2 = 0; i2 < 8; ++i2) x[e + i2] = y[i2];
       }
     };
-    take(k_rows);
+    take(k_rows, in[0]);
     if (there) {
       const int e = kb == 4 ? k_encode<4>(x, kc, NB, key, bc) : k_encode<8>(x, kc, NB, key, bc);
       ks[key * SROW + b] = (unsigned char)e;
     }
-    take(v_rows);
+    take(v_rows, in[1]);
     const bool quad = ((unsigned)(__ballot(there) >> (lane & ~3)) & 15u) == 15u;
     const int e = vb == 4 ? v_encode<4>(x, vc, NB, key, bc, there, quad) : v_encode<8>(x, vc, NB, key, bc, there, quad);
     if (there) vs[key * SROW + b] = (unsigned char)e;
