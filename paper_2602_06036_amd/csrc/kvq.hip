@@ -213,7 +213,7 @@ template <typename T, int HD, bool WRITE>
 __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int slots) {
   constexpr int NB = kvq_blocks(HD), SROW = kvq_scale_row(NB), E = 16 / sizeof(T);   // elements of 16 bytes
   constexpr int ROW = HD / E, PIECES = DF_PAGE * ROW, LD = ROW + 1;                   // 16-byte pieces; LD: rows 16 bytes further in LDS, so that a column lies in all banks
-  __shared__ u32x4 s_rows[kRowWaves][WRITE ? 1 : 2][DF_PAGE * LD];   // written: K, then V in its place, which leaves room for six wavefronts a SIMD instead of four
+  __shared__ u32x4 s_rows[kRowWaves][DF_PAGE * LD];   // K, then V in its place, which leaves room for six wavefronts a SIMD instead of four
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int i = blockIdx.x * kRowWaves + wave, H = a.c.n_kv_heads;
   if (i >= slots * H) return;
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
     return p < PIECES && key >= key0 && key < key1;
   };
   auto place = [&](T* rows, int key, int c) { return reinterpret_cast<u32x4*>(rows + (((size_t)s * a.rows + (size_t)(j0 + key)) * H + head) * HD) + c; };
-  u32x4 *k_rows = s_rows[wave][0], *v_rows = s_rows[wave][WRITE ? 0 : 1];
+  u32x4* rows = s_rows[wave];
   const int key = lane & 15, b = lane >> 4, bc = min(b, NB - 1);
   const bool there = key >= key0 && key < key1 && b < NB;
   constexpr int N = (PIECES + 63) / 64;
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   };
-  auto block_at = [&](u32x4* rows, int e) { return rows + key * LD + (bc * 32 + e) / E; };
+  auto block_at = [&](int e) { return rows + key * LD + (bc * 32 + e) / E; };
   if constexpr (WRITE) {
     u32x4 in[2][N];
 #pragma unroll
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
         if (piece(lane + 64 * n, key2, c)) in[kv][n] = *place(static_cast<T*>(kv ? a.v : a.k), key2, c);
       }
     float x[32];
-    auto take = [&](u32x4* rows, const u32x4 (&from)[N]) {
+    auto take = [&](const u32x4 (&from)[N]) {
       sync();
 #pragma unroll
       for (int n = 0; n < N; ++n)
@@ -276,46 +276,45 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
         float y[8];
 #pragma unroll
         for (int i2 = 0; i2 < 8; ++i2) y[i2] = 0.f;
-        if (HD % 32 == 0 || bc * 32 + e < HD) Raw<T>::load8(y, reinterpret_cast<const T*>(block_at(rows, e)));
+        if (HD % 32 == 0 || bc * 32 + e < HD) Raw<T>::load8(y, reinterpret_cast<const T*>(block_at(e)));
 #pragma unroll
         for (int i2 = 0; i2 < 8; ++i2) x[e + i2] = y[i2];
       }
     };
-    take(k_rows, in[0]);
+    take(in[0]);
     if (there) {
       const int e = kb == 4 ? k_encode<4>(x, kc, NB, key, bc) : k_encode<8>(x, kc, NB, key, bc);
       ks[key * SROW + b] = (unsigned char)e;
     }
-    take(v_rows, in[1]);
+    take(in[1]);
     const bool quad = ((unsigned)(__ballot(there) >> (lane & ~3)) & 15u) == 15u;
     const int e = vb == 4 ? v_encode<4>(x, vc, NB, key, bc, there, quad) : v_encode<8>(x, vc, NB, key, bc, there, quad);
     if (there) vs[key * SROW + b] = (unsigned char)e;
   } else {
-    float x[32];
-    auto give = [&](u32x4* rows) {
+    float k[32], v[32];
+    const float k_scale = kvq_scale_clean(ks[key * SROW + bc]), v_scale = kvq_scale_clean(vs[key * SROW + bc]);
+    if (kb == 4) k_decode<4>(k, kc, NB, key, bc, k_scale);
+    else k_decode<8>(k, kc, NB, key, bc, k_scale);
+    if (vb == 4) v_decode<4>(v, vc, NB, key, bc, v_scale);
+    else v_decode<8>(v, vc, NB, key, bc, v_scale);
+    auto give = [&](const float (&x)[32], T* to) {
+      sync();
 #pragma unroll
       for (int e = 0; e < 32; e += 8) {
         float y[8];
 #pragma unroll
         for (int i2 = 0; i2 < 8; ++i2) y[i2] = x[e + i2];
-        if (b < NB && (HD % 32 == 0 || bc * 32 + e < HD)) Raw<T>::store8(reinterpret_cast<T*>(block_at(rows, e)), y);
+        if (b < NB && (HD % 32 == 0 || bc * 32 + e < HD)) Raw<T>::store8(reinterpret_cast<T*>(block_at(e)), y);
       }
-    };
-    const float k_scale = kvq_scale_clean(ks[key * SROW + bc]), v_scale = kvq_scale_clean(vs[key * SROW + bc]);
-    if (kb == 4) k_decode<4>(x, kc, NB, key, bc, k_scale);
-    else k_decode<8>(x, kc, NB, key, bc, k_scale);
-    give(k_rows);
-    if (vb == 4) v_decode<4>(x, vc, NB, key, bc, v_scale);
-    else v_decode<8>(x, vc, NB, key, bc, v_scale);
-    give(v_rows);
-    sync();
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv)
+      sync();
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         int key2, c;
-        if (piece(lane + 64 * n, key2, c)) *place(static_cast<T*>(kv ? a.v : a.k), key2, c) = s_rows[wave][kv][key2 * LD + c];
+        if (piece(lane + 64 * n, key2, c)) *place(to, key2, c) = rows[key2 * LD + c];
       }
+    };
+    give(k, static_cast<T*>(a.k));
+    give(v, static_cast<T*>(a.v));
   }
 }
 
