@@ -331,8 +331,9 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {   // over 16 lanes
 }
 // the four keys' elements (dims n and n + 16) of a block -> codes
 template <int BITS>
-__device__ __forceinline__ void v_pack(float (&lo)[4], float (&hi)[4], unsigned char* at, int (&e)[4]) {
-  uint32_t w[BITS / 4] = {};
+__device__ __forceinline__ void v_pack(float (&lo)[4], float (&hi)[4], uint32_t (&w)[BITS / 4], int (&e)[4]) {
+#pragma unroll
+  for (int i = 0; i < BITS / 4; ++i) w[i] = 0;
   float scale[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -345,26 +346,22 @@ __device__ __forceinline__ void v_pack(float (&lo)[4], float (&hi)[4], unsigned 
     put4<1>(w[0], lo[1], hi[1], scale[1]);
     put4<2>(w[0], lo[2], hi[2], scale[2]);
     put4<3>(w[0], lo[3], hi[3], scale[3]);
-    *reinterpret_cast<uint32_t*>(at) = w[0];
   } else {
     put8<0>(w[0], lo[0], hi[0], scale[0]);
     put8<1>(w[0], lo[1], hi[1], scale[1]);
     put8<0>(w[1], lo[2], hi[2], scale[2]);
     put8<1>(w[1], lo[3], hi[3], scale[3]);
-    *reinterpret_cast<u32x2*>(at) = (u32x2){w[0], w[1]};
   }
 }
 template <int BITS>
-__device__ __forceinline__ void v_unpack(float (&lo)[4], float (&hi)[4], const unsigned char* at, const float (&scale)[4]) {
+__device__ __forceinline__ void v_unpack(float (&lo)[4], float (&hi)[4], const uint32_t (&w)[BITS / 4], const float (&scale)[4]) {
   f32x2 v[4];
   if constexpr (BITS == 4) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(at);
-    v[0] = kvq_f32_of4<0>(w, scale[0]);
-    v[1] = kvq_f32_of4<1>(w, scale[1]);
-    v[2] = kvq_f32_of4<2>(w, scale[2]);
-    v[3] = kvq_f32_of4<3>(w, scale[3]);
+    v[0] = kvq_f32_of4<0>(w[0], scale[0]);
+    v[1] = kvq_f32_of4<1>(w[0], scale[1]);
+    v[2] = kvq_f32_of4<2>(w[0], scale[2]);
+    v[3] = kvq_f32_of4<3>(w[0], scale[3]);
   } else {
-    const u32x2 w = *reinterpret_cast<const u32x2*>(at);
     v[0] = kvq_f32_of8<0>(w[0], scale[0]);
     v[1] = kvq_f32_of8<1>(w[0], scale[1]);
     v[2] = kvq_f32_of8<0>(w[1], scale[2]);
@@ -427,56 +424,82 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_pages_kernel(KvqPages a) {
       }
     }
   }
-  const int q = lane >> 4, n = lane & 15;
-  const int there = min(max(n_rows - 4 * q, 0), 4);   // of the lane's four keys
-  uint32_t sc[SROW];                                   // scales of its four keys, as they lie
-#pragma unroll
-  for (int i2 = 0; i2 < SROW; ++i2) sc[i2] = PACK ? 0u : reinterpret_cast<const uint32_t*>(vs + 4 * q * SROW)[i2];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const bool two = 32 * b + 16 < hd;
-    float lo[4], hi[4];
-    T* at = pv + (2 * b) * 256 + lane * 4;
-    unsigned char* codes = vc + (vb == 4 ? v_place<4>(NB, q, n, b) : v_place<8>(NB, q, n, b));
-    if constexpr (PACK) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) lo[k] = hi[k] = 0.f;
-      if (there) {
-        Raw<T>::load4(lo, at);
-        if (two) Raw<T>::load4(hi, at + 256);
+  // V: all blocks' codes of a lane go to and fro together, 16 bytes of them where there are four blocks (block by block a store wrote 4 bytes in 16)
+  auto v_part = [&](auto bits_c) {
+    constexpr int BITS = decltype(bits_c)::value, W = BITS / 4;
+    const int q = lane >> 4, n = lane & 15;
+    const int there = min(max(n_rows - 4 * q, 0), 4);   // of the lane's four keys
+    uint32_t sc[SROW], w[NB][W];                         // scales of its four keys, as they lie
+    auto codes = [&](auto copy) {                        // (place, first block, blocks that lie together)
+      if constexpr (BITS == 4) copy(vc + (q * 16 + n) * NB * 4, 0, std::integral_constant<int, NB>());
+      else {
+        if constexpr (NB >= 2) copy(vc + (q * 16 + n) * 16, 0, std::integral_constant<int, 2>());
+        if constexpr (NB == 4) copy(vc + 1024 + (q * 16 + n) * 16, 2, std::integral_constant<int, 2>());
+        if constexpr (NB & 1) copy(vc + (NB / 2) * 1024 + (q * 16 + n) * 8, NB - 1, std::integral_constant<int, 1>());
       }
+    };
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k >= there) lo[k] = hi[k] = 0.f;
-      int e[4];
-      if (vb == 4) v_pack<4>(lo, hi, codes, e);
-      else v_pack<8>(lo, hi, codes, e);
+    for (int i2 = 0; i2 < SROW; ++i2) sc[i2] = PACK ? 0u : reinterpret_cast<const uint32_t*>(vs + 4 * q * SROW)[i2];
+    if constexpr (!PACK)
+      codes([&](const unsigned char* at, int b, auto n_c) {
+        constexpr int N = decltype(n_c)::value * W;
+        uint32_t x[N];
+        __builtin_memcpy(x, __builtin_assume_aligned(at, N == 4 ? 16 : N == 2 ? 8 : 4), 4 * N);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sc[(k * SROW + b) / 4] |= (uint32_t)e[k] << ((k * SROW + b) % 4 * 8);
-    } else {
-      float scale[4];
+        for (int i2 = 0; i2 < N; ++i2) w[b + i2 / W][i2 % W] = x[i2];
+      });
 #pragma unroll
-      for (int k = 0; k < 4; ++k) scale[k] = kvq_scale_clean(sc[(k * SROW + b) / 4] >> ((k * SROW + b) % 4 * 8));
-      if (vb == 4) v_unpack<4>(lo, hi, codes, scale);
-      else v_unpack<8>(lo, hi, codes, scale);
-      if (there == 4) {
-        Raw<T>::store4(at, lo);
-        if (two) Raw<T>::store4(at + 256, hi);
-      } else {
+    for (int b = 0; b < NB; ++b) {
+      const bool two = 32 * b + 16 < hd;
+      float lo[4], hi[4];
+      T* at = pv + (2 * b) * 256 + lane * 4;
+      if constexpr (PACK) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) lo[k] = hi[k] = 0.f;
+        if (there) {
+          Raw<T>::load4(lo, at);
+          if (two) Raw<T>::load4(hi, at + 256);
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (k < there) {
-            Raw<T>::store1(at + k, lo[k]);
-            if (two) Raw<T>::store1(at + 256 + k, hi[k]);
-          }
+          if (k >= there) lo[k] = hi[k] = 0.f;
+        int e[4];
+        v_pack<BITS>(lo, hi, w[b], e);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[(k * SROW + b) / 4] |= (uint32_t)e[k] << ((k * SROW + b) % 4 * 8);
+      } else {
+        float scale[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) scale[k] = kvq_scale_clean(sc[(k * SROW + b) / 4] >> ((k * SROW + b) % 4 * 8));
+        v_unpack<BITS>(lo, hi, w[b], scale);
+        if (there == 4) {
+          Raw<T>::store4(at, lo);
+          if (two) Raw<T>::store4(at + 256, hi);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < there) {
+              Raw<T>::store1(at + k, lo[k]);
+              if (two) Raw<T>::store1(at + 256 + k, hi[k]);
+            }
+        }
       }
     }
-  }
-  if constexpr (PACK) {
-    if (n == 0)
+    if constexpr (PACK) {
+      codes([&](unsigned char* at, int b, auto n_c) {
+        constexpr int N = decltype(n_c)::value * W;
+        uint32_t x[N];
 #pragma unroll
-      for (int i2 = 0; i2 < SROW; ++i2) reinterpret_cast<uint32_t*>(vs + 4 * q * SROW)[i2] = sc[i2];
-  }
+        for (int i2 = 0; i2 < N; ++i2) x[i2] = w[b + i2 / W][i2 % W];
+        __builtin_memcpy(__builtin_assume_aligned(at, N == 4 ? 16 : N == 2 ? 8 : 4), x, 4 * N);
+      });
+      if (n == 0)
+#pragma unroll
+        for (int i2 = 0; i2 < SROW; ++i2) reinterpret_cast<uint32_t*>(vs + 4 * q * SROW)[i2] = sc[i2];
+    }
+  };
+  if (vb == 4) v_part(std::integral_constant<int, 4>());
+  else v_part(std::integral_constant<int, 8>());
 }
 
 template <bool WRITE>
