@@ -205,7 +205,7 @@ __device__ __forceinline__ void v_decode(float (&x)[32], const unsigned char* co
 
 // ---- rows [S, rows, Hkv, hd] <-> cache ----------------------------------------------------------------------------------------
 // Codes: lane = (block b, key).  Rows: a wavefront moves them 16 bytes a lane, a row's pieces in neighbouring lanes, and they change places in LDS: a lane by itself would touch a
-// quarter of 64 lines with every load or store (one layer of eight caches read back, 402 MB: 145 us, now 91; four prompts written and read, 207 MB: 66, now 50).
+// quarter of 64 lines with every load or store (one layer of eight caches read back, 402 MB: 145 us, now 82; four prompts written and read, 207 MB: 66, now 48).
 // grid: (pages that a sequence's rows may touch x kv heads / 4 wavefronts, 1, S), kv heads fastest.
 constexpr int kRowWaves = 4;
 
@@ -320,7 +320,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
 
 // ---- pages of a pool <-> cache --------------------------------------------------------------------------------------------------
 // K: lane = (block, key), 8 dims a load.  V: lane = (q, dim % 16) has four keys of a dim, as both layouts do; a block's maximum is that of two registers over the
-// sixteen lanes of a row.  grid: (pages x kv heads / 4 wavefronts, layers, S).
+// sixteen lanes of a row.  Bound by memory: four requests of 700 to 2050 tokens, 36 layers, taken up again 226 us (5.0 TB/s, the rate of a large copy); two put aside
+// 147 us (3.8: V's maxima and two conversions an element take half of the issue).  grid: (pages x kv heads / 4 wavefronts, layers, S).
 __device__ __forceinline__ uint32_t row_max(uint32_t x) {   // over 16 lanes
   auto step = [&](uint32_t y) { x = max(x, y); };
   step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true));

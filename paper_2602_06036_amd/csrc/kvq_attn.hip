@@ -8,6 +8,10 @@
 // base 2, with a reference maximum that moves only when a score passes it by kSlack.  bf16 models: probabilities are rounded to bf16, by 2^-9 of themselves each, where
 // V itself is held to 2^-2 or 2^-4 of its block; their sum is taken over the rounded ones, so the weights still add up to one.  All sums in fp32.
 // Ranges of keys are joined by kvq_merge_kernel in a fixed order: a call repeats itself bit for bit.
+//
+// Single tokens are bound by memory (32 of them behind 1k to 32k tokens, 32 heads over 8 of 128, 4 bits: 590 MB in 102 us, 5.8 TB/s; the copies by themselves 101); blocks of few pairs a wavefront by
+// latency (16 x 16 rows behind up to 4k tokens: 27 us, and 6 for the merge); many rows by vector instructions, which share the issue with the MFMAs (pieces of 391 and 512 rows behind up to
+// 6k tokens: 87 us with the merge, 620 TFLOP/s of the keys that the rows see).
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -562,7 +566,7 @@ __device__ __forceinline__ void copy_page(const unsigned char* from, unsigned to
 template <typename T, int NB, int KB, int VB, int RB>
 struct Launch {
   static constexpr int UNIT = kvq_unit(NB, KB, VB), LD = NB * 32 + 4, WAVES = 4;
-  static constexpr bool F32 = std::is_same<T, float>::value, Q_LDS = RB == 4 || (F32 && RB == 2);   // the queries beside 64 rows' sums are too many for the registers
+  static constexpr bool F32 = std::is_same<T, float>::value, Q_LDS = RB == 4;   // the queries beside 64 rows' sums are too many for the registers
   // A wavefront's ring of page pairs as they lie in memory, filled by direct-to-LDS copies: what is on its way costs no registers.  Two pairs: three or four leave room for
   // fewer workgroups and gain nothing (single tokens 133, 133, 144 us; blocks of 16 rows 42, 42, 65).
   static constexpr int PAIR = 2 * UNIT, NI = 2 * ((UNIT + 1023) / 1024);   // bytes, copies a pair
@@ -807,13 +811,16 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
   __shared__ float s_m[8], s_l[8];
   __shared__ __attribute__((aligned(16))) float s_o[GROUPS][132];
   const int s = blockIdx.y, of = threadIdx.x >> 5, at = GROUPS == 8 ? blockIdx.x : blockIdx.x * 8 + of;
-  const int j = at / a.n_q_heads, h = at % a.n_q_heads, group = a.n_q_heads / a.c.n_kv_heads;
+  const int group = a.n_q_heads / a.c.n_kv_heads;
+  int j, h, kvh, in_group, last_slot, rest;
+  slot_of(at, a.n_q_heads, j, h);
+  slot_of(h, group, kvh, in_group);
   const SeqRows rows(a, s);
   const Ranges ranges(a);
   const int first = ranges.first_of(a, s);
   if (j >= rows.count) return;
-  const int tile = (j * group + h % group) / ROWS, last = min((tile + 1) * ROWS, rows.count * group) - 1;
-  const int parts = ranges.count(rows.end(a, last / group));   // of the row's tile
+  slot_of(min(((j * group + in_group) / ROWS + 1) * ROWS, rows.count * group) - 1, group, last_slot, rest);
+  const int parts = ranges.count(rows.end(a, last_slot));   // of the row's tile
   if (parts <= 1) return;
   const int d = 4 * (threadIdx.x & 31), hd = a.c.hd;
   const size_t step = (size_t)a.rows * a.n_q_heads, from = (first * (size_t)a.rows + j) * a.n_q_heads + h;
@@ -861,7 +868,10 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
   if (d < hd) store_row4(static_cast<T*>(a.out) + ((s * (size_t)a.rows + j) * a.n_q_heads + h) * hd + d, o * (l == 0.f ? 0.f : 1.f / l));
 }
 
-int tile_rows(bool bf16, int rows) { return rows <= 16 ? 16 : rows <= 32 || !bf16 ? 32 : 64; }
+// Rows of a workgroup.  bf16: the more the fewer conversions a row (16 sequences behind up to 4k tokens, 32 heads over 8: 8 rows each by tiles of 16, 32 and 64 28.5, 23.3, 27.4 us, 16 rows each 38, 32.7, 31.7;
+// pieces of a prompt 130, 102, 87).  fp32: bound by its 16x16x4 MFMAs whatever the tile, and the sums of 32 rows leave one wavefront a SIMD (two pieces of 300 to 400 rows, 8 heads of 64:
+// 41 us by 16 rows, 46 by 32).
+int tile_rows(bool bf16, int rows) { return rows <= 16 || !bf16 ? 16 : rows <= 32 ? 32 : 64; }
 
 template <typename T, int NB, int KB, int VB>
 void launch(const KvqAttn& a, int tile, hipStream_t st) {
@@ -879,8 +889,10 @@ void launch(const KvqAttn& a, int tile, hipStream_t st) {
     join(std::integral_constant<int, 16 * RB>());
   };
   if (tile == 16) go(std::integral_constant<int, 1>());
-  else if (tile == 32) go(std::integral_constant<int, 2>());
-  else if constexpr (std::is_same<T, bf16_t>::value) go(std::integral_constant<int, 4>());
+  else if constexpr (std::is_same<T, bf16_t>::value) {
+    if (tile == 32) go(std::integral_constant<int, 2>());
+    else go(std::integral_constant<int, 4>());
+  }
 }
 template <typename T, int NB>
 void launch_bits(const KvqAttn& a, int rb, hipStream_t st) {
