@@ -17,10 +17,10 @@
 #include <utility>
 
 #include "kvq.h"
+#include "plan.h"
 
 namespace {
 
-constexpr int kMinPairs = 8;    // page pairs of a range at least
 constexpr float kSlack = 8.f;   // probabilities up to 2^8 above the reference: nothing that fp32 sums or bf16 exponents notice
 
 __device__ __forceinline__ uint32_t pair_of(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
@@ -386,9 +386,9 @@ struct Ranges {
   int lane, own;   // page pairs of the sequence of this lane, of the first 64
   __device__ __forceinline__ static int pairs(const KvqAttn& a, int s) { return s < a.n_seqs ? (SeqRows(a, s).n_tok + 31) / 32 : 0; }
   __device__ __forceinline__ Ranges(const KvqAttn& a) : lane(threadIdx.x & 63), own(pairs(a, lane)) {
-    float all = 0.f;   // in four pairs; rounding must not make ranges shorter than their share, of which there would be too many
+    float all = 0.f;   // in four pairs of pages
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) all += (float)__builtin_amdgcn_readlane(wave_scan(((s0 ? pairs(a, s0 + lane) : own) + 3) / 4), 63);
-    chunk = min(max((int)min(all / (float)a.parts * 1.0001f, 2e7f) + 1, kMinPairs / 4), (1 << 24) - 1) * 128;
+    chunk = kvq_chunk(all, a.parts);
   }
   __device__ __forceinline__ int count(int tokens) const { return (int)(((unsigned)tokens + (unsigned)chunk - 1) / (unsigned)chunk); }
   // the sequence that the f-th range belongs to, and the first of its ranges; false: there are not as many
@@ -868,11 +868,6 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
   if (d < hd) store_row4(static_cast<T*>(a.out) + ((s * (size_t)a.rows + j) * a.n_q_heads + h) * hd + d, o * (l == 0.f ? 0.f : 1.f / l));
 }
 
-// Rows of a workgroup.  bf16: the more the fewer conversions a row (16 sequences behind up to 4k tokens, 32 heads over 8: 8 rows each by tiles of 16, 32 and 64 28.5, 23.3, 27.4 us, 16 rows each 38, 32.7, 31.7;
-// pieces of a prompt 130, 102, 87).  fp32: bound by its 16x16x4 MFMAs whatever the tile, and the sums of 32 rows leave one wavefront a SIMD (two pieces of 300 to 400 rows, 8 heads of 64:
-// 41 us by 16 rows, 46 by 32).
-int tile_rows(bool bf16, int rows) { return rows <= 16 || !bf16 ? 16 : rows <= 32 ? 32 : 64; }
-
 template <typename T, int NB, int KB, int VB>
 void launch(const KvqAttn& a, int tile, hipStream_t st) {
   const dim3 grid((unsigned)((long long)(a.n_seqs + a.parts) * a.tiles * a.c.n_kv_heads));
@@ -912,22 +907,14 @@ void launch_type(const KvqAttn& a, int rb, hipStream_t st) {
 }  // namespace
 
 bool kvq_attn_plan(KvqAttn& a, bool bf16, int max_tokens, size_t part_rows) {
-  const int rows = a.rows * (a.n_q_heads / a.c.n_kv_heads), tile = tile_rows(bf16, rows);
-  a.tiles = (rows + tile - 1) / tile;
-  const long long heads = (long long)a.c.n_kv_heads * a.tiles, room = (long long)(part_rows / ((size_t)a.rows * a.n_q_heads)) - a.n_seqs;
-  // Twice as many workgroups as the card holds (single tokens, 640: 114 us, 1536: 111, 2176: 111), or as many: a few that come behind the others cost a round (blocks of
-  // 16 rows, 384: 35 us, 448: 33, 512: 38), so half a range a sequence, by which there are more of them, is left out where sequences have several.
-  const int wgs = tile == 16 ? 1536 : 512;
-  long long parts = wgs / heads;
-  if (tile > 16 && 2 * parts >= 3 * a.n_seqs) parts -= a.n_seqs / 2;
-  parts = std::min(parts, room);
-  // Sequences are half as long as the longest, say: with enough of them no range would be cut.
-  a.parts = parts > 0 && parts * 2 > a.n_seqs && max_tokens > 32 * kMinPairs ? (int)parts : 0;
-  return (a.n_seqs + a.parts) * heads <= 0x7FFFFFFFll;
+  const KvqPlan p = kvq_plan(a.n_seqs, a.rows, a.n_q_heads, a.c.n_kv_heads, bf16, max_tokens, part_rows);
+  a.tiles = p.tiles;
+  a.parts = p.parts;
+  return (a.n_seqs + (long long)a.parts) * a.c.n_kv_heads * a.tiles <= 0x7FFFFFFFll;
 }
 
 void kvq_attn_launch(const KvqAttn& a, bool bf16, hipStream_t st) {
-  const int tile = tile_rows(bf16, a.rows * (a.n_q_heads / a.c.n_kv_heads));
+  const int tile = kvq_tile_rows(bf16, a.rows * (a.n_q_heads / a.c.n_kv_heads));
   if (bf16) launch_type<bf16_t>(a, tile, st);
   else launch_type<float>(a, tile, st);
 }

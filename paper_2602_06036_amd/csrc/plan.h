@@ -440,3 +440,34 @@ inline int lse_chunks(int rows, int V, size_t room) {
 inline int accept_chunks(int S, int V, size_t room) {
   return (int)std::max<size_t>(1, std::min<size_t>({(size_t)(1024 / S), (size_t)64, (size_t)(V / 1024), room / S}));
 }
+
+// ---- attention over caches in 4 and 8 bits (kvq_attn.hip) ---------------------------------------------------------------------------
+// Rows of a workgroup.  bf16: the more the fewer conversions a row (16 sequences behind up to 4k tokens, 32 heads over 8: 8 rows each by tiles of 16, 32 and 64 28.5, 23.3, 27.4 us, 16 rows each 38, 32.7, 31.7;
+// pieces of a prompt 130, 102, 87).  fp32: bound by its 16x16x4 MFMAs whatever the tile, and the sums of 32 rows leave one wavefront a SIMD (two pieces of 300 to 400 rows, 8 heads of 64:
+// 41 us by 16 rows, 46 by 32).
+inline int kvq_tile_rows(bool bf16, int rows) { return rows <= 16 || !bf16 ? 16 : rows <= 32 ? 32 : 64; }
+
+// Row tiles of a sequence, and about how many ranges the keys of all sequences are cut into (0: none is).
+struct KvqPlan {
+  int tiles, parts;
+};
+constexpr int kKvqMinPairs = 8;    // page pairs of a range at least
+// There are parts + n_seqs ranges at most (kvq_chunk), each with the partial rows of all rows and query heads of a sequence: part_rows of them in all.
+inline KvqPlan kvq_plan(int n_seqs, int rows, int n_q_heads, int n_kv_heads, bool bf16, int max_tokens, size_t part_rows) {
+  const int tile = kvq_tile_rows(bf16, rows * (n_q_heads / n_kv_heads)), tiles = (rows * (n_q_heads / n_kv_heads) + tile - 1) / tile;
+  const long long heads = (long long)n_kv_heads * tiles, room = (long long)(part_rows / ((size_t)rows * n_q_heads)) - n_seqs;
+  // Twice as many workgroups as the card holds (single tokens, 640: 114 us, 1536: 111, 2176: 111), or as many: a few that come behind the others cost a round (blocks of
+  // 16 rows, 384: 35 us, 448: 33, 512: 38), so half a range a sequence, by which there are more of them, is left out where sequences have several.
+  long long parts = (tile == 16 ? 1536 : 512) / heads;
+  if (tile > 16 && 2 * parts >= 3ll * n_seqs) parts -= n_seqs / 2;
+  parts = std::min(parts, room);
+  // Sequences are half as long as the longest, say: with enough of them no range would be cut.
+  return {tiles, parts > 0 && parts * 2 > n_seqs && max_tokens > 32 * kKvqMinPairs ? (int)parts : 0};
+}
+// Keys of a range, a multiple of 128, where all sequences have `all` times four pairs of pages, each rounded up: the device's part of the plan.  Rounding must not make ranges
+// shorter than their share, or there would be more of them than places.
+constexpr int kvq_chunk(float all, int parts) {
+  const float share = all / (float)parts * 1.0001f;
+  const int fours = (int)(share < 1.6e7f ? share : 1.6e7f) + 1;
+  return (fours > kKvqMinPairs / 4 ? fours : kKvqMinPairs / 4) * 128;
+}

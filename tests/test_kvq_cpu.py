@@ -1,5 +1,8 @@
 """The 4- and 8-bit format of the test side against its definition, and the sizes and refusals that need no GPU."""
 import ctypes as C
+import os
+import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -84,3 +87,78 @@ def test_refusals_without_a_context():
     assert l.dflash_kvq_attention(None, C.byref(b), C.byref(q), 0, 1, None, 1, None, None, None) == B.DFLASH_EINVAL
     assert l.dflash_kvq_pack(None, C.byref(b), C.byref(q), None, None) == B.DFLASH_EINVAL
     assert l.dflash_kvq_unpack(None, C.byref(b), C.byref(q), None, None) == B.DFLASH_EINVAL
+
+
+# ---- launch rules, compiled for the host, and the waits of the sweep ----------------------------------------------------------
+CSRC = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "paper_2602_06036_amd", "csrc")
+DRIVER = r"""
+#include <stdio.h>
+#include "plan.h"
+int main() {
+  int seqs, rows, hq, hkv, bf16, tokens;
+  long long part_rows;
+  float all;
+  while (scanf("%d %d %d %d %d %d %lld %f", &seqs, &rows, &hq, &hkv, &bf16, &tokens, &part_rows, &all) == 8) {
+    const KvqPlan p = kvq_plan(seqs, rows, hq, hkv, bf16 != 0, tokens, part_rows);
+    printf("%d %d %d\n", p.tiles, p.parts, p.parts ? kvq_chunk(all, p.parts) : 0);
+  }
+}
+"""
+
+
+def test_ranges_fit_their_places_whatever_the_lengths(tmp_path):
+    (tmp_path / "p.cpp").write_text(DRIVER)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", CSRC, str(tmp_path / "p.cpp"), "-o", str(tmp_path / "p")], check=True)
+    rng = np.random.RandomState(0)
+    queries, lens = [], []
+    for seqs in (1, 2, 3, 7, 16, 48, 64, 65, 150, 1000, 2000):
+        for rows in (1, 2, 16, 17, 400):
+            for hq, hkv in ((32, 8), (4, 4), (10, 2), (16, 1)):
+                for part_rows in (98304, seqs * rows * hq, 64 * rows * hq, 3 * rows * hq - 1):
+                    n = rng.randint(0, int(rng.choice([40, 4000, 300000])), seqs)
+                    n[rng.randint(seqs)] = rng.choice([0, 1, 9000, 2 ** 28])
+                    pairs = -(-n // 32)
+                    all_fours = np.float32(0)
+                    for s0 in range(0, seqs, 64):       # as the device adds them up
+                        all_fours = np.float32(all_fours + np.float32((-(-pairs[s0:s0 + 64] // 4)).sum()))
+                    # a hint that has little to do with the lengths
+                    queries.append((seqs, rows, hq, hkv, rng.randint(2), int(rng.choice([1, 256, 257, 5000, 40000])), part_rows, repr(float(all_fours))))
+                    lens.append(n)
+    out = subprocess.run([str(tmp_path / "p")], input="\n".join(" ".join(str(x) for x in q) for q in queries), capture_output=True, text=True, check=True).stdout
+    cut = 0
+    for (seqs, rows, hq, hkv, bf16, tokens, part_rows, _), n, line in zip(queries, lens, out.splitlines()):
+        tiles, parts, chunk = (int(x) for x in line.split())
+        tile = 16 if not bf16 or rows * hq // hkv <= 16 else 32 if rows * hq // hkv <= 32 else 64
+        assert tiles == -(-rows * hq // hkv // tile)
+        if parts:
+            cut += 1
+            assert chunk % 128 == 0 and chunk >= 256
+            assert (parts + seqs) * rows * hq <= part_rows
+            assert int((-(-n // chunk)).sum()) <= parts + seqs, (seqs, parts, chunk)
+    assert cut > 100 and cut < len(queries)
+
+
+@pytest.mark.skipif(not os.path.exists(os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")), reason="needs hipcc")
+def test_the_sweep_waits_for_its_pair_and_not_for_the_next(tmp_path):
+    """A turn waits until its own pair's copies have landed, the next pair's (two pages of three copies) in flight.  The compiler does not see the copies: whatever load it
+    waits for by itself drains them all, so such a wait may stand only where page ids are loaded or taken over, and behind the last pair."""
+    from paper_2602_06036_amd import build
+    with open(os.path.join(CSRC, "kvq_attn.hip")) as f:
+        kernels = f.read().split("template <typename T, int NB, int KB, int VB>\nvoid launch(")[0]      # without what makes all others of them
+    (tmp_path / "k.hip").write_text(kernels + "".join("template __global__ void kvq_attn_kernel<bf16_t, 4, 4, 4, %d>(KvqAttn);\n" % rb for rb in (1, 2, 4)) + "}\n")
+    flags = [f for f in build.FLAGS if f not in ("-shared", "-fPIC")]
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *flags, "--offload-device-only", "-S", "-I", CSRC, str(tmp_path / "k.hip"), "-o", str(tmp_path / "k.s")],
+                   check=True, capture_output=True)
+    asm = (tmp_path / "k.s").read_text()
+    for rb in (1, 2, 4):
+        body = re.search(r"^_ZN\S*kvq_attn_kernelItLi4ELi4ELi4ELi%dEEEv7KvqAttn:.*?^\.Lfunc_end" % rb, asm, re.S | re.M).group(0)
+        loops = {}
+        for b in re.split(r"^(?=\.LBB\d+_\d+:|; %bb\.\d+:)", body, flags=re.M):
+            m = re.search(r"Header=(BB\d+_\d+) ", b) or re.match(r"\.L(BB\d+_\d+):.*Loop Header", b)
+            if m:
+                loops.setdefault(m.group(1), []).append(b)
+        sweep = [bs for bs in loops.values() if any("global_load_lds" in b for b in bs) and any("mfma" in b for b in bs)]
+        assert len(sweep) == 1, rb
+        waits = [(int(n), "global_load_lds" in b, "mfma" in b or "ds_read" in b) for b in sweep[0] for n in re.findall(r"s_waitcnt[^\n]*vmcnt\((\d+)\)", b)]
+        assert (6, True, False) in waits, (rb, waits)
+        assert all(w == (6, True, False) or w == (0, False, False) for w in waits) and len(waits) <= 4, (rb, waits)
