@@ -571,8 +571,9 @@ struct Launch {
   // fewer workgroups and gain nothing (single tokens 133, 133, 144 us; blocks of 16 rows 42, 42, 65).
   static constexpr int PAIR = 2 * UNIT, NI = 2 * ((UNIT + 1023) / 1024);   // bytes, copies a pair
   static constexpr int RING = WAVES * PAIR * 2, MERGE = WAVES * 16 * LD * 4, RAW = RING > MERGE ? RING : MERGE;
-  static constexpr int LDS = RAW + (Q_LDS ? RB * 64 * (int)sizeof(typename Math<T, NB, KB, VB>::Query) : 0);
-  static constexpr int ON_SIMD = LDS > 80000 ? 1 : RB == 1 && KB + VB < 16 ? 3 : 2;   // wavefronts
+  // Where a sequence's rows are one tile nobody else reads these bytes, and they need no place in L2 (single tokens 126 -> 116 us).
+  static constexpr bool ONCE = !F32 && (RB == 1 || (RB == 2 && kvq_tiles_of_64(NB, KB, VB)));
+  static constexpr int ON_SIMD = RB == 1 && KB + VB < 16 ? 3 : 2;   // wavefronts
 };
 template <typename T, int NB, int KB, int VB, int RB>
 __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T, NB, KB, VB, RB>::ON_SIMD)) void kvq_attn_kernel(KvqAttn a) {
@@ -667,9 +668,8 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
   auto fetch = [&](int k, int slot) {
     const int from = k & 32 ? ids_next : ids;
     const Ids id = {__builtin_amdgcn_readlane(from, (k & 31) * 2), __builtin_amdgcn_readlane(from, (k & 31) * 2 + 1)};
-    // bf16, up to 32 rows: they are one tile and nobody else reads these bytes, which need no place in L2 (single tokens 126 -> 116 us)
-    copy_page<UNIT, !L::F32 && RB < 4>(unit_of(id.a), ring + slot * PAIR, voff);
-    copy_page<UNIT, !L::F32 && RB < 4>(unit_of(id.b), ring + slot * PAIR + UNIT, voff);
+    copy_page<UNIT, L::ONCE>(unit_of(id.a), ring + slot * PAIR, voff);
+    copy_page<UNIT, L::ONCE>(unit_of(id.b), ring + slot * PAIR + UNIT, voff);
     return id;
   };
   bool left_out = false;
@@ -886,7 +886,7 @@ void launch(const KvqAttn& a, int tile, hipStream_t st) {
   if (tile == 16) go(std::integral_constant<int, 1>());
   else if constexpr (std::is_same<T, bf16_t>::value) {
     if (tile == 32) go(std::integral_constant<int, 2>());
-    else go(std::integral_constant<int, 4>());
+    else if constexpr (kvq_tiles_of_64(NB, KB, VB)) go(std::integral_constant<int, 4>());
   }
 }
 template <typename T, int NB>
@@ -907,14 +907,14 @@ void launch_type(const KvqAttn& a, int rb, hipStream_t st) {
 }  // namespace
 
 bool kvq_attn_plan(KvqAttn& a, bool bf16, int max_tokens, size_t part_rows) {
-  const KvqPlan p = kvq_plan(a.n_seqs, a.rows, a.n_q_heads, a.c.n_kv_heads, bf16, max_tokens, part_rows);
+  const KvqPlan p = kvq_plan(a.n_seqs, a.rows, a.n_q_heads, a.c.n_kv_heads, bf16, kvq_tiles_of_64(kvq_blocks(a.c.hd), a.c.k_bits, a.c.v_bits), max_tokens, part_rows);
   a.tiles = p.tiles;
   a.parts = p.parts;
   return (a.n_seqs + (long long)a.parts) * a.c.n_kv_heads * a.tiles <= 0x7FFFFFFFll;
 }
 
 void kvq_attn_launch(const KvqAttn& a, bool bf16, hipStream_t st) {
-  const int tile = kvq_tile_rows(bf16, a.rows * (a.n_q_heads / a.c.n_kv_heads));
+  const int tile = kvq_tile_rows(bf16, a.rows * (a.n_q_heads / a.c.n_kv_heads), kvq_tiles_of_64(kvq_blocks(a.c.hd), a.c.k_bits, a.c.v_bits));
   if (bf16) launch_type<bf16_t>(a, tile, st);
   else launch_type<float>(a, tile, st);
 }

@@ -444,8 +444,10 @@ inline int accept_chunks(int S, int V, size_t room) {
 // ---- attention over caches in 4 and 8 bits (kvq_attn.hip) ---------------------------------------------------------------------------
 // Rows of a workgroup.  bf16: the more the fewer conversions a row (16 sequences behind up to 4k tokens, 32 heads over 8: 8 rows each by tiles of 16, 32 and 64 28.5, 23.3, 27.4 us, 16 rows each 38, 32.7, 31.7;
 // pieces of a prompt 130, 102, 87).  fp32: bound by its 16x16x4 MFMAs whatever the tile, and the sums of 32 rows leave one wavefront a SIMD (two pieces of 300 to 400 rows, 8 heads of 64:
-// 41 us by 16 rows, 46 by 32).
-inline int kvq_tile_rows(bool bf16, int rows) { return rows <= 16 || !bf16 ? 16 : rows <= 32 ? 32 : 64; }
+// 41 us by 16 rows, 46 by 32).  Four blocks of 8-bit K and V: the pages and queries of 64 rows leave one workgroup a CU (16 x 16 rows as above 48 us, by 32 rows 35; pieces of a prompt 152, by 32
+// rows 108).
+constexpr bool kvq_tiles_of_64(int blocks, int k_bits, int v_bits) { return blocks * (k_bits + v_bits) <= 48; }
+inline int kvq_tile_rows(bool bf16, int rows, bool tiles_of_64) { return rows <= 16 || !bf16 ? 16 : rows <= 32 || !tiles_of_64 ? 32 : 64; }
 
 // Row tiles of a sequence, and about how many ranges the keys of all sequences are cut into (0: none is).
 struct KvqPlan {
@@ -453,8 +455,8 @@ struct KvqPlan {
 };
 constexpr int kKvqMinPairs = 8;    // page pairs of a range at least
 // There are parts + n_seqs ranges at most (kvq_chunk), each with the partial rows of all rows and query heads of a sequence: part_rows of them in all.
-inline KvqPlan kvq_plan(int n_seqs, int rows, int n_q_heads, int n_kv_heads, bool bf16, int max_tokens, size_t part_rows) {
-  const int tile = kvq_tile_rows(bf16, rows * (n_q_heads / n_kv_heads)), tiles = (rows * (n_q_heads / n_kv_heads) + tile - 1) / tile;
+inline KvqPlan kvq_plan(int n_seqs, int rows, int n_q_heads, int n_kv_heads, bool bf16, bool tiles_of_64, int max_tokens, size_t part_rows) {
+  const int tile = kvq_tile_rows(bf16, rows * (n_q_heads / n_kv_heads), tiles_of_64), tiles = (rows * (n_q_heads / n_kv_heads) + tile - 1) / tile;
   const long long heads = (long long)n_kv_heads * tiles, room = (long long)(part_rows / ((size_t)rows * n_q_heads)) - n_seqs;
   // Twice as many workgroups as the card holds (single tokens, 640: 114 us, 1536: 111, 2176: 111), or as many: a few that come behind the others cost a round (blocks of
   // 16 rows, 384: 35 us, 448: 33, 512: 38), so half a range a sequence, by which there are more of them, is left out where sequences have several.

@@ -95,11 +95,11 @@ DRIVER = r"""
 #include <stdio.h>
 #include "plan.h"
 int main() {
-  int seqs, rows, hq, hkv, bf16, tokens;
+  int seqs, rows, hq, hkv, bf16, wide, tokens;
   long long part_rows;
   float all;
-  while (scanf("%d %d %d %d %d %d %lld %f", &seqs, &rows, &hq, &hkv, &bf16, &tokens, &part_rows, &all) == 8) {
-    const KvqPlan p = kvq_plan(seqs, rows, hq, hkv, bf16 != 0, tokens, part_rows);
+  while (scanf("%d %d %d %d %d %d %d %lld %f", &seqs, &rows, &hq, &hkv, &bf16, &wide, &tokens, &part_rows, &all) == 9) {
+    const KvqPlan p = kvq_plan(seqs, rows, hq, hkv, bf16 != 0, wide != 0, tokens, part_rows);
     printf("%d %d %d\n", p.tiles, p.parts, p.parts ? kvq_chunk(all, p.parts) : 0);
   }
 }
@@ -122,13 +122,13 @@ def test_ranges_fit_their_places_whatever_the_lengths(tmp_path):
                     for s0 in range(0, seqs, 64):       # as the device adds them up
                         all_fours = np.float32(all_fours + np.float32((-(-pairs[s0:s0 + 64] // 4)).sum()))
                     # a hint that has little to do with the lengths
-                    queries.append((seqs, rows, hq, hkv, rng.randint(2), int(rng.choice([1, 256, 257, 5000, 40000])), part_rows, repr(float(all_fours))))
+                    queries.append((seqs, rows, hq, hkv, rng.randint(2), rng.randint(2), int(rng.choice([1, 256, 257, 5000, 40000])), part_rows, repr(float(all_fours))))
                     lens.append(n)
     out = subprocess.run([str(tmp_path / "p")], input="\n".join(" ".join(str(x) for x in q) for q in queries), capture_output=True, text=True, check=True).stdout
     cut = 0
-    for (seqs, rows, hq, hkv, bf16, tokens, part_rows, _), n, line in zip(queries, lens, out.splitlines()):
+    for (seqs, rows, hq, hkv, bf16, wide, tokens, part_rows, _), n, line in zip(queries, lens, out.splitlines()):
         tiles, parts, chunk = (int(x) for x in line.split())
-        tile = 16 if not bf16 or rows * hq // hkv <= 16 else 32 if rows * hq // hkv <= 32 else 64
+        tile = 16 if not bf16 or rows * hq // hkv <= 16 else 32 if rows * hq // hkv <= 32 or not wide else 64
         assert tiles == -(-rows * hq // hkv // tile)
         if parts:
             cut += 1
