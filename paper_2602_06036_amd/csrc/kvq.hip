@@ -107,23 +107,29 @@ __device__ __forceinline__ int k_encode(float (&x)[32], unsigned char* codes, in
     *reinterpret_cast<u32x4*>(codes + ((h * nb + b) * 16 + key) * 16) = (u32x4){w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]};
   return e;
 }
+// (codes are asked for and decoded apart: a call's bits are known at run time, and K's, V's and the scales are one trip to memory only if none is waited for in between)
 template <int BITS>
-__device__ __forceinline__ void k_decode(float (&x)[32], const unsigned char* codes, int nb, int key, int b, float scale) {
+__device__ __forceinline__ void k_load(uint32_t (&w)[8], const unsigned char* codes, int nb, int key, int b) {
 #pragma unroll
   for (int h = 0; h < BITS / 4; ++h) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(codes + ((h * nb + b) * 16 + key) * 16);
+    const u32x4 x = *reinterpret_cast<const u32x4*>(codes + ((h * nb + b) * 16 + key) * 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      auto two = [&](int at, f32x2 v) { x[at] = v[0]; x[at + 1] = v[1]; };
-      if constexpr (BITS == 4) {
-        two(8 * i, kvq_f32_of4<0>(w[i], scale));
-        two(8 * i + 2, kvq_f32_of4<1>(w[i], scale));
-        two(8 * i + 4, kvq_f32_of4<2>(w[i], scale));
-        two(8 * i + 6, kvq_f32_of4<3>(w[i], scale));
-      } else {
-        two(16 * h + 4 * i, kvq_f32_of8<0>(w[i], scale));
-        two(16 * h + 4 * i + 2, kvq_f32_of8<1>(w[i], scale));
-      }
+    for (int i = 0; i < 4; ++i) w[4 * h + i] = x[i];
+  }
+}
+template <int BITS>
+__device__ __forceinline__ void k_decode(float (&x)[32], const uint32_t (&w)[8], float scale) {
+#pragma unroll
+  for (int i = 0; i < BITS; ++i) {
+    auto two = [&](int at, f32x2 v) { x[at] = v[0]; x[at + 1] = v[1]; };
+    if constexpr (BITS == 4) {
+      two(8 * i, kvq_f32_of4<0>(w[i], scale));
+      two(8 * i + 2, kvq_f32_of4<1>(w[i], scale));
+      two(8 * i + 4, kvq_f32_of4<2>(w[i], scale));
+      two(8 * i + 6, kvq_f32_of4<3>(w[i], scale));
+    } else {
+      two(4 * i, kvq_f32_of8<0>(w[i], scale));
+      two(4 * i + 2, kvq_f32_of8<1>(w[i], scale));
     }
   }
 }
@@ -178,21 +184,32 @@ __device__ __forceinline__ int v_encode(float (&x)[32], unsigned char* codes, in
   return e;
 }
 template <int BITS>
-__device__ __forceinline__ void v_decode(float (&x)[32], const unsigned char* codes, int nb, int key, int b, float scale) {
-  const int q = key >> 2, k = key & 3;
+__device__ __forceinline__ void v_load(uint32_t (&w)[8], const unsigned char* codes, int nb, int key, int b) {
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
-    const unsigned char* at = codes + v_place<BITS>(nb, q, 4 * m + k, b);
+    const unsigned char* at = codes + v_place<BITS>(nb, key >> 2, 4 * m + (key & 3), b);
+    if constexpr (BITS == 4) {
+      w[m] = *reinterpret_cast<const uint32_t*>(at);
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(at);
+      w[2 * m] = x[0];
+      w[2 * m + 1] = x[1];
+    }
+  }
+}
+template <int BITS>
+__device__ __forceinline__ void v_decode(float (&x)[32], const uint32_t (&w)[8], int k, float scale) {   // k: the lane's place among the four of a quad
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
     auto two = [&](int n, f32x2 v) { x[n] = v[0]; x[n + 16] = v[1]; };
     if constexpr (BITS == 4) {
-      const uint32_t w = quad_bytes(*reinterpret_cast<const uint32_t*>(at), k);
-      two(4 * m, kvq_f32_of4<0>(w, scale));
-      two(4 * m + 1, kvq_f32_of4<1>(w, scale));
-      two(4 * m + 2, kvq_f32_of4<2>(w, scale));
-      two(4 * m + 3, kvq_f32_of4<3>(w, scale));
+      const uint32_t y = quad_bytes(w[m], k);
+      two(4 * m, kvq_f32_of4<0>(y, scale));
+      two(4 * m + 1, kvq_f32_of4<1>(y, scale));
+      two(4 * m + 2, kvq_f32_of4<2>(y, scale));
+      two(4 * m + 3, kvq_f32_of4<3>(y, scale));
     } else {
-      const u32x2 raw = *reinterpret_cast<const u32x2*>(at);
-      uint32_t lo = raw[0], hi = raw[1];
+      uint32_t lo = w[2 * m], hi = w[2 * m + 1];
       quad_halves_swap(lo, hi, k);
       quad_halves_in(lo, hi, k);
       two(4 * m, kvq_f32_of8<0>(lo, scale));
@@ -230,12 +247,6 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
     return;
   }
   const int page = index < a.mpps ? a.table[(size_t)s * a.mpps + index] : -1;
-  if (page < 0 || page >= a.c.n_pages) odd = true;
-  if (odd && head == 0 && lane == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
-  if (page < 0 || page >= a.c.n_pages) return;
-  const int kb = a.c.k_bits, vb = a.c.v_bits;
-  unsigned char* unit = a.c.data + (((size_t)a.layer * a.c.n_pages + page) * H + head) * kvq_unit(NB, kb, vb);
-  unsigned char *kc = unit, *vc = kc + kvq_codes(NB, kb), *ks = vc + kvq_codes(NB, vb), *vs = ks + DF_PAGE * SROW;
   // keys of the page that are the call's
   const int key0 = (int)max(lo - index * DF_PAGE, 0ll), key1 = (int)min(hi - index * DF_PAGE, (long long)DF_PAGE);
   const long long j0 = index * DF_PAGE - lo;   // row of key 0
@@ -254,8 +265,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
     __builtin_amdgcn_wave_barrier();
   };
   auto block_at = [&](int e) { return rows + key * LD + (bc * 32 + e) / E; };
-  if constexpr (WRITE) {
-    u32x4 in[2][N];
+  u32x4 in[2][N];
+  if constexpr (WRITE) {   // on their way while the page's id is
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
@@ -264,6 +275,14 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
         in[kv][n] = (u32x4){0u, 0u, 0u, 0u};
         if (piece(lane + 64 * n, key2, c)) in[kv][n] = *place(static_cast<T*>(kv ? a.v : a.k), key2, c);
       }
+  }
+  if (page < 0 || page >= a.c.n_pages) odd = true;
+  if (odd && head == 0 && lane == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
+  if (page < 0 || page >= a.c.n_pages) return;
+  const int kb = a.c.k_bits, vb = a.c.v_bits;
+  unsigned char* unit = a.c.data + (((size_t)a.layer * a.c.n_pages + page) * H + head) * kvq_unit(NB, kb, vb);
+  unsigned char *kc = unit, *vc = kc + kvq_codes(NB, kb), *ks = vc + kvq_codes(NB, vb), *vs = ks + DF_PAGE * SROW;
+  if constexpr (WRITE) {
     float x[32];
     auto take = [&](const u32x4 (&from)[N]) {
       sync();
@@ -292,11 +311,16 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
     if (there) vs[key * SROW + b] = (unsigned char)e;
   } else {
     float k[32], v[32];
-    const float k_scale = kvq_scale_clean(ks[key * SROW + bc]), v_scale = kvq_scale_clean(vs[key * SROW + bc]);
-    if (kb == 4) k_decode<4>(k, kc, NB, key, bc, k_scale);
-    else k_decode<8>(k, kc, NB, key, bc, k_scale);
-    if (vb == 4) v_decode<4>(v, vc, NB, key, bc, v_scale);
-    else v_decode<8>(v, vc, NB, key, bc, v_scale);
+    const unsigned ke = ks[key * SROW + bc], ve = vs[key * SROW + bc];
+    uint32_t kw[8], vw[8];
+    if (kb == 4) k_load<4>(kw, kc, NB, key, bc);
+    else k_load<8>(kw, kc, NB, key, bc);
+    if (vb == 4) v_load<4>(vw, vc, NB, key, bc);
+    else v_load<8>(vw, vc, NB, key, bc);
+    if (kb == 4) k_decode<4>(k, kw, kvq_scale_clean(ke));
+    else k_decode<8>(k, kw, kvq_scale_clean(ke));
+    if (vb == 4) v_decode<4>(v, vw, key & 3, kvq_scale_clean(ve));
+    else v_decode<8>(v, vw, key & 3, kvq_scale_clean(ve));
     auto give = [&](const float (&x)[32], T* to) {
       sync();
 #pragma unroll
@@ -413,8 +437,11 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_pages_kernel(KvqPages a) {
         ks[key * SROW + b] = (unsigned char)(kb == 4 ? k_encode<4>(x, kc, NB, key, b) : k_encode<8>(x, kc, NB, key, b));
       } else {
         const float scale = kvq_scale_clean(ks[key * SROW + b]);
-        if (kb == 4) k_decode<4>(x, kc, NB, key, b, scale);
-        else k_decode<8>(x, kc, NB, key, b, scale);
+        uint32_t w[8];
+        if (kb == 4) k_load<4>(w, kc, NB, key, b);
+        else k_load<8>(w, kc, NB, key, b);
+        if (kb == 4) k_decode<4>(x, w, scale);
+        else k_decode<8>(x, w, scale);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           float y[8];
