@@ -222,7 +222,7 @@ __device__ __forceinline__ void v_decode(float (&x)[32], const uint32_t (&w)[8],
 
 // ---- rows [S, rows, Hkv, hd] <-> cache ----------------------------------------------------------------------------------------
 // Codes: lane = (block b, key).  Rows: a wavefront moves them 16 bytes a lane, a row's pieces in neighbouring lanes, and they change places in LDS: a lane by itself would touch a
-// quarter of 64 lines with every load or store (one layer of eight caches read back, 402 MB: 145 us, now 82; four prompts written and read, 207 MB: 66, now 48).
+// quarter of 64 lines with every load or store (one layer of eight caches read back, 402 MB: 145 us, now 80; four prompts written and read, 207 MB: 66, now 48).
 // grid: (pages that a sequence's rows may touch x kv heads / 4 wavefronts, 1, S), kv heads fastest.
 constexpr int kRowWaves = 4;
 

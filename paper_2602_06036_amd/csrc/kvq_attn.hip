@@ -540,12 +540,12 @@ __device__ __forceinline__ void copy_page(const unsigned char* from, unsigned to
 #define KVQ_REST "s_mov_b64 exec, %5\n\ts_nop 0\n\t"
 #define KVQ_END "s_mov_b64 exec, %1\n\ts_nop 0\n\ts_mov_b32 m0, %0"
 #define KVQ_ASM(text) asm volatile(KVQ_BEGIN text KVQ_END : "=&s"(keep_m0), "=&s"(keep_exec) : "s"(to), "v"(voff), "s"(from), "s"(REST) : "memory")
-#define KVQ_PAGE(nt)                                                                                                              \
-  if constexpr (FULL == 0) KVQ_ASM(KVQ_REST KVQ_COPY(0, nt));                                                                     \
-  else if constexpr (FULL == 1) KVQ_ASM(KVQ_COPY(0, nt) KVQ_REST KVQ_COPY(1024, nt));                                             \
-  else if constexpr (FULL == 2) KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(1024, nt) KVQ_REST KVQ_COPY(2048, nt));                          \
-  else if constexpr (FULL == 3) KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(1024, nt) KVQ_COPY(2048, nt) KVQ_REST KVQ_COPY(3072, nt));       \
-  else KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(1024, nt) KVQ_COPY(2048, nt) KVQ_COPY(3072, nt))
+#define KVQ_PAGE(nt)                                                                                                            \
+  if constexpr (FULL == 0) KVQ_ASM(KVQ_REST KVQ_COPY(0, nt));                                                                   \
+  else if constexpr (FULL == 1) KVQ_ASM(KVQ_COPY(0, nt) KVQ_REST KVQ_COPY(0x400, nt));                                          \
+  else if constexpr (FULL == 2) KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(0x400, nt) KVQ_REST KVQ_COPY(0x800, nt));                      \
+  else if constexpr (FULL == 3) KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(0x400, nt) KVQ_COPY(0x800, nt) KVQ_REST KVQ_COPY(0xc00, nt));  \
+  else KVQ_ASM(KVQ_COPY(0, nt) KVQ_COPY(0x400, nt) KVQ_COPY(0x800, nt) KVQ_COPY(0xc00, nt))
   if constexpr (NT) { KVQ_PAGE(" nt"); }
   else { KVQ_PAGE(""); }
   if constexpr (FULL == 4) {   // the rest lies behind the largest offset
