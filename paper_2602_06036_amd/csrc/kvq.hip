@@ -265,8 +265,15 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
     __builtin_amdgcn_wave_barrier();
   };
   auto block_at = [&](int e) { return rows + key * LD + (bc * 32 + e) / E; };
-  u32x4 in[2][N];
-  if constexpr (WRITE) {   // on their way while the page's id is
+  if (page < 0 || page >= a.c.n_pages) odd = true;
+  if (odd && head == 0 && lane == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
+  if (page < 0 || page >= a.c.n_pages) return;
+  const int kb = a.c.k_bits, vb = a.c.v_bits;
+  unsigned char* unit = a.c.data + (((size_t)a.layer * a.c.n_pages + page) * H + head) * kvq_unit(NB, kb, vb);
+  unsigned char *kc = unit, *vc = kc + kvq_codes(NB, kb), *ks = vc + kvq_codes(NB, vb), *vs = ks + DF_PAGE * SROW;
+  if constexpr (WRITE) {
+    // all rows at once, behind the page's id: in front of it the rows of short batches are even and those of four prompts 49.0 us instead of 47.6
+    u32x4 in[2][N];
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
@@ -275,14 +282,6 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_rows_kernel(KvqRows a, int
         in[kv][n] = (u32x4){0u, 0u, 0u, 0u};
         if (piece(lane + 64 * n, key2, c)) in[kv][n] = *place(static_cast<T*>(kv ? a.v : a.k), key2, c);
       }
-  }
-  if (page < 0 || page >= a.c.n_pages) odd = true;
-  if (odd && head == 0 && lane == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
-  if (page < 0 || page >= a.c.n_pages) return;
-  const int kb = a.c.k_bits, vb = a.c.v_bits;
-  unsigned char* unit = a.c.data + (((size_t)a.layer * a.c.n_pages + page) * H + head) * kvq_unit(NB, kb, vb);
-  unsigned char *kc = unit, *vc = kc + kvq_codes(NB, kb), *ks = vc + kvq_codes(NB, vb), *vs = ks + DF_PAGE * SROW;
-  if constexpr (WRITE) {
     float x[32];
     auto take = [&](const u32x4 (&from)[N]) {
       sync();
