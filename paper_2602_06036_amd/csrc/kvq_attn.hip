@@ -7,7 +7,7 @@
 // 2 and 4 significant bits.  S^T = K Q^T leaves a lane four consecutive keys of a query column, which is how V^T P^T takes them.  Softmax in one pass,
 // base 2, with a reference maximum that moves only when a score passes it by kSlack.  bf16 models: probabilities are rounded to bf16, by 2^-9 of themselves each, where
 // V itself is held to 2^-2 or 2^-4 of its block; their sum is taken over the rounded ones, so the weights still add up to one.  All sums in fp32.
-// Ranges of keys are joined by kvq_merge_kernel in a fixed order: a call repeats itself bit for bit.
+// Ranges of keys, each the mean of its values with its weights' sum and reference, are joined by kvq_merge_kernel in a fixed order: a call repeats itself bit for bit.
 //
 // Single tokens are bound by memory (32 of them behind 1k to 32k tokens, 32 heads over 8 of 128, 4 bits: 590 MB in 102 us, 5.8 TB/s; the copies by themselves 101); blocks of few pairs a wavefront by
 // latency (16 x 16 rows behind up to 4k tokens: 27 us, and 6 for the merge); many rows by vector instructions, which share the issue with the MFMAs (pieces of 391 and 512 rows behind up to
@@ -22,6 +22,9 @@
 namespace {
 
 constexpr float kSlack = 8.f;   // probabilities up to 2^8 above the reference: nothing that fp32 sums or bf16 exponents notice
+// Sums of finite values can pass fp32 where their weighted mean does not (a hundred keys of 2^122 and weight 1).  A wavefront whose sums are not finite takes its keys again with
+// weights 2^-40 as large, which add up to less than 1 over any number of keys.  Not at once, so that values down to 2^-126 keep their bits where none is above 2^88.
+constexpr float kLift = 40.f;
 
 __device__ __forceinline__ uint32_t pair_of(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
 __device__ __forceinline__ uint32_t finite_half(uint32_t x, uint32_t exponent) { return (x & exponent) == exponent ? 0u : x; }
@@ -442,8 +445,19 @@ struct State {
       for (int t = 0; t < 2 * NB; ++t) acc[rb][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
   }
-  // scores of both pages -> weights; masks where edge is set
-  __device__ __forceinline__ void weigh(typename M::Probs (&pr)[RB], const f32x4 (&sa)[RB], const f32x4 (&sb)[RB], const Seen& at, bool edge, float scale2) {
+  // sums that are infinite or NaN
+  __device__ __forceinline__ bool not_finite() const {
+    float t = 0.f;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int b = 0; b < 2 * NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t = __builtin_fmaf(acc[rb][b][i], 0.f, t);
+    return t != 0.f;
+  }
+  // scores of both pages -> weights, 2^-lift as large; masks where edge is set
+  __device__ __forceinline__ void weigh(typename M::Probs (&pr)[RB], const f32x4 (&sa)[RB], const f32x4 (&sb)[RB], const Seen& at, bool edge, float scale2, float lift) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float v[8], p[8];
@@ -470,7 +484,7 @@ struct State {
 #pragma unroll
         for (int t = 0; t < 2 * NB; ++t) acc[rb][t] *= f;
       }
-      const float mb = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
+      const float mb = (m_run[rb] == -INFINITY ? 0.f : m_run[rb]) + lift;
 #pragma unroll
       for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], scale2, -mb));
       M::probs(pr[rb], p);
@@ -584,7 +598,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
   constexpr bool Q_LDS = L::Q_LDS;
   constexpr int QP = sizeof(typename M::Query) / 16;   // 16-byte pieces of a lane's queries, a lane's neighbour's beside each (a lane's behind each other: four lanes a bank)
   __shared__ u32x4 s_q[Q_LDS ? RB : 1][QP][Q_LDS ? 64 : 1];
-  __shared__ float s_m[WAVES][RB * 16], s_l[WAVES][RB * 16];
+  __shared__ float s_m[WAVES][RB * 16], s_l[WAVES][RB * 16], s_lift[WAVES];
   __shared__ __attribute__((aligned(1024))) unsigned char s_raw[L::RAW];   // the ring, then the wavefronts' outputs
   float (*s_o)[16][LD] = reinterpret_cast<float (*)[16][LD]>(s_raw);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
@@ -673,6 +687,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     return id;
   };
   bool left_out = false;
+  float lift = 0.f;   // kLift: the second time
   auto work = [&](const unsigned char* pair, const Seen& at, bool edge) {   // edge: some row does not see some key
     typename M::Probs pr[RB];
     f32x4 sa[RB], sb[RB];
@@ -694,7 +709,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     P pa, pb;
     pa.load_v(pair, lane);
     pb.load_v(pair + UNIT, lane);
-    st.weigh(pr, sa, sb, at, edge, scale2);
+    st.weigh(pr, sa, sb, at, edge, scale2, lift);
     typename M::Values v[L::F32 ? 1 : NB];   // bf16: all blocks, and one branch for the edge; fp32: block by block
     auto block = [&](auto b_c) -> typename M::Values& { return v[L::F32 ? 0 : decltype(b_c)::value]; };
     unrolled<NB>([&](auto b_c) {
@@ -722,37 +737,48 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     ids = there_or_not(ids);
     ids_next = there_or_not(ids_next);
     asm volatile("" : "+v"(ids), "+v"(ids_next));
-    int slot = 0;   // of the ring, of the pair at hand
-    Ids next = fetch(0, 0);
 #pragma unroll 1
-    for (int k = 0; k < n; ++k) {
-      if ((k & 31) == 0 && k) fresh = load_ids(p0 + k + 32);
-      if ((k & 31) == 16 && k > 16) {
-        fresh = there_or_not(fresh);
-        asm volatile("" : "+v"(fresh));
-        if (k & 32) ids = fresh;
-        else ids_next = fresh;
+    for (;;) {
+      int slot = 0;   // of the ring, of the pair at hand
+      Ids next = fetch(0, 0);
+#pragma unroll 1
+      for (int k = 0; k < n; ++k) {
+        if ((k & 31) == 0 && k) fresh = load_ids(p0 + k + 32);
+        if ((k & 31) == 16 && k > 16) {
+          fresh = there_or_not(fresh);
+          asm volatile("" : "+v"(fresh));
+          if (k & 32) ids = fresh;
+          else ids_next = fresh;
+        }
+        const Ids at = next;
+        if (k + 1 < n) {   // into the slot that the pair before this one has left
+          next = fetch(k + 1, slot ^ 1);
+          __builtin_amdgcn_s_waitcnt(0x0F70 | NI);   // vmcnt: this pair's copies have landed
+        } else {
+          __builtin_amdgcn_s_waitcnt(0x0F70);
+        }
+        asm volatile("" ::: "memory");
+        const int base = c0 + (p0 + k) * 32;
+        const bool ok_a = at.a >= 0, ok_b = at.b >= 0;
+        const unsigned char* pair = my_ring + slot * PAIR;
+        work(pair, Seen{base, g, ok_a, ok_b}, base + 32 > all_see || !ok_a || !ok_b || lift != 0.f);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the pair has been read before its slot is filled again
+        slot ^= 1;
       }
-      const Ids at = next;
-      if (k + 1 < n) {   // into the slot that the pair before this one has left
-        next = fetch(k + 1, slot ^ 1);
-        __builtin_amdgcn_s_waitcnt(0x0F70 | NI);   // vmcnt: this pair's copies have landed
-      } else {
-        __builtin_amdgcn_s_waitcnt(0x0F70);
-      }
-      asm volatile("" ::: "memory");
-      const int base = c0 + (p0 + k) * 32;
-      const bool ok_a = at.a >= 0, ok_b = at.b >= 0;
-      const unsigned char* pair = my_ring + slot * PAIR;
-      work(pair, Seen{base, g, ok_a, ok_b}, base + 32 > all_see || !ok_a || !ok_b);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the pair has been read before its slot is filled again
-      slot ^= 1;
+      if (lift != 0.f || __ballot(st.not_finite()) == 0) break;
+      // again: smaller weights, and whatever value is not finite itself is left out of the products
+      lift = kLift;
+      left_out = false;
+      st.clear();
+      ids = there_or_not(load_ids(p0));
+      ids_next = there_or_not(load_ids(p0 + 32));
+      asm volatile("" : "+v"(ids), "+v"(ids_next));
     }
     if (left_out)
 #pragma unroll 1
       for (int k = 0; k < n; ++k) {
         const int base = c0 + (p0 + k) * 32, ia = there_or_not(table[min(2 * (p0 + k), last_page)]), ib = there_or_not(table[min(2 * (p0 + k) + 1, last_page)]);
-        if (base + 32 > all_see || ia < 0 || ib < 0) st.template add_left_out<P>(unit_of(ia), unit_of(ib), Seen{base, g, ia >= 0, ib >= 0}, end, lane);
+        if (base + 32 > all_see || ia < 0 || ib < 0 || lift != 0.f) st.template add_left_out<P>(unit_of(ia), unit_of(ib), Seen{base, g, ia >= 0, ib >= 0}, end, lane);
       }
   }
   __syncthreads();   // the wavefronts' outputs overlay the ring
@@ -763,9 +789,10 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     const float l = M::total(st.sum[rb]);
     if (g == 0) {
       s_m[wave][rb * 16 + col] = st.m_run[rb];
-      s_l[wave][rb * 16 + col] = l;
+      s_l[wave][rb * 16 + col] = lift != 0.f ? l * 0x1p40f : l;
     }
   }
+  if (lane == 0) s_lift[wave] = lift != 0.f ? 0x1p40f : 1.f;
   const bool whole = end <= chunk;   // the only range: nothing to merge
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -790,12 +817,13 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
       slot_of(row0 + rb * 16 + r, group, j, h);
       h += kvh * group;
       const size_t at = (s * (size_t)a.rows + j) * a.n_q_heads + h, in_part = (part * (size_t)a.rows + j) * a.n_q_heads;
-      const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) f[w] *= inv * s_lift[w];   // the sums' shares, before they are added: a mean is finite where a sum need not be
       for (int d = 4 * (threadIdx.x % LANES); d < hd; d += 4 * LANES) {
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][r][d]) * f[w];
-        o *= inv;
         if (whole) store_row4(static_cast<T*>(a.out) + at * hd + d, o);
         else *reinterpret_cast<f32x4*>(a.part_o + (in_part + h) * hd + d) = o;
       }
@@ -840,9 +868,10 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
     for (int i = 0; i < AHEAD; ++i) {
       if (p0 + i * GROUPS >= parts) break;
       const float top = fmaxf(m, x[i].x), f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), fx = x[i].x == top ? 1.f : __builtin_amdgcn_exp2f(x[i].x - top);
+      const float all = f * l + fx * x[i].y, inv = all == 0.f ? 0.f : __builtin_amdgcn_rcpf(all);
+      o = o * (f * l * inv) + y[i] * (fx * x[i].y * inv);
       m = top;
-      l = f * l + fx * x[i].y;
-      o = o * f + y[i] * fx;
+      l = all;
     }
   }
   if constexpr (GROUPS == 8) {
@@ -853,19 +882,21 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
     }
     __syncthreads();
     if (of) return;
-    float m_all = -INFINITY;
+    float m_all = -INFINITY, f[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) m_all = fmaxf(m_all, s_m[i]);
     l = 0.f;
     o = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float f = s_m[i] == m_all ? 1.f : __builtin_amdgcn_exp2f(s_m[i] - m_all);
-      l += f * s_l[i];
-      o += *reinterpret_cast<const f32x4*>(&s_o[i][d]) * f;
+      f[i] = s_l[i] * (s_m[i] == m_all ? 1.f : __builtin_amdgcn_exp2f(s_m[i] - m_all));
+      l += f[i];
     }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o += *reinterpret_cast<const f32x4*>(&s_o[i][d]) * (f[i] * inv);
   }
-  if (d < hd) store_row4(static_cast<T*>(a.out) + ((s * (size_t)a.rows + j) * a.n_q_heads + h) * hd + d, o * (l == 0.f ? 0.f : 1.f / l));
+  if (d < hd) store_row4(static_cast<T*>(a.out) + ((s * (size_t)a.rows + j) * a.n_q_heads + h) * hd + d, o);
 }
 
 template <typename T, int NB, int KB, int VB>

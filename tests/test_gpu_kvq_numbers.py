@@ -1,0 +1,42 @@
+"""What attention over caches in 4 and 8 bits makes of numbers at the ends of their range, and of weights that many keys share, against attention in 64 bits."""
+import numpy as np
+import pytest
+
+from tests import kvq_model as km
+from tests.shared_pages import PAGE
+from tests.test_gpu_kvq import Setup, _check, f64
+
+pytestmark = pytest.mark.gpu
+
+
+def _scales(x, part, e):
+    """All scales of K (part 0) or V; e as for 4-bit codes, so that the largest value is 6 * 2^(e - 127) in 4 bits and 7 * 2^(e - 127) in 8."""
+    x.ref.data[..., x.ref.at[2 + part].ravel()] = e - (6 if x.bits[part] == 8 else 0)
+
+
+# heads, kv heads, head dim, bits, rows, lengths: tiles of 16, 32 and 64 rows, whole and cut ranges, both forms of the merge
+NUMBERS = [("bf16", 4, 1, 128, (4, 4), 1, (300, 3000, 0)), ("bf16", 8, 2, 64, (8, 8), 5, (40, 1)), ("bf16", 32, 8, 128, (8, 4), 70, (1500, 700)), ("bf16", 4, 1, 96, (4, 8), 6, (2500, 31)),
+           ("f32", 4, 2, 64, (8, 8), 1, (300, 3000, 0)), ("f32", 8, 2, 128, (4, 4), 7, (40, 2200)), ("f32", 32, 2, 32, (4, 8), 70, (1500, 900)), ("bf16", 2, 1, 80, (8, 8), 1, (9000,))]
+
+
+@pytest.mark.parametrize("v_scale", [252, 20])
+@pytest.mark.parametrize("case", range(len(NUMBERS)))
+def test_weighted_means_of_the_largest_and_smallest_values(case, v_scale):
+    """Keys with about the same weight: the sum of their values is beyond the type, their mean is not (up to 1.75 * 2^127; one block of a head has the largest code everywhere).
+    Values of 2^-107 keep their bits all the same."""
+    dtype, heads, kv, hd, bits, rows, lens = NUMBERS[case]
+    counts = (rows,) * len(lens)
+    x = Setup(dtype, heads, kv, hd, bits, len(lens), [n + rows for n in lens], seed=case)
+    _scales(x, 0, 112)                          # scores of some hundredths: hundreds of keys of each row weigh about the same
+    _scales(x, 1, v_scale)
+    x.ref.data[:, :, 0, x.ref.at[1][0][:, 0].ravel()] = 0x77 if bits[1] == 4 else 0x7E
+    x.poison(lens, counts)
+    x.upload()
+    q, out = x.rows((len(lens), rows, heads, hd), 0.7), x.rows((len(lens), rows, heads, hd))
+    before = out.clone()
+    for hint, causal in ((max(lens), True), (0, False)):
+        out.copy_(before)
+        x.B.dflash_kvq_attention(x.e, x.batch(lens, hint), x.cache, 1, q, out, causal=causal)
+        x.e.device_status()
+        assert bool(x.torch.isfinite(out).all()), (case, v_scale, hint)
+        _check(x, q, out, before, lens, counts, causal, 1, (case, v_scale, hint))
