@@ -25,6 +25,9 @@ constexpr float kSlack = 8.f;   // probabilities up to 2^8 above the reference: 
 // Sums of finite values can pass fp32 where their weighted mean does not (a hundred keys of 2^122 and weight 1).  A wavefront whose sums are not finite takes its keys again with
 // weights 2^-40 as large, which add up to less than 1 over any number of keys.  Not at once, so that values down to 2^-126 keep their bits where none is above 2^88.
 constexpr float kLift = 40.f;
+// A score times scale2 less a reference that was rounded after the same product is off by half a step of either: from scores of 2^31 on that is a power of 2^128 or of nothing.
+// Such weights' sum is infinite, NaN or next to nothing where the reference's own is 1: those wavefronts, too, take their keys again, scores less the reference before the product.
+constexpr float kLeast = 0x1p-20f;
 
 __device__ __forceinline__ uint32_t pair_of(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
 __device__ __forceinline__ uint32_t finite_half(uint32_t x, uint32_t exponent) { return (x & exponent) == exponent ? 0u : x; }
@@ -434,7 +437,7 @@ template <typename M, int NB, int RB>
 struct State {
   f32x4 acc[RB][2 * NB];
   typename M::Sum sum[RB];
-  float m_run[RB];
+  float m_run[RB];   // in units of the scores
   int row_end[RB];
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -445,19 +448,23 @@ struct State {
       for (int t = 0; t < 2 * NB; ++t) acc[rb][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
   }
-  // sums that are infinite or NaN
-  __device__ __forceinline__ bool not_finite() const {
+  // sums that are infinite or NaN, or of weights that are next to nothing
+  __device__ __forceinline__ bool unsound() const {
     float t = 0.f;
+    bool odd = false;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+    for (int rb = 0; rb < RB; ++rb) {
+      const float l = M::total(sum[rb]);
+      odd |= m_run[rb] != -INFINITY && !(l >= kLeast && l < INFINITY);
 #pragma unroll
       for (int b = 0; b < 2 * NB; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) t = __builtin_fmaf(acc[rb][b][i], 0.f, t);
-    return t != 0.f;
+    }
+    return odd || t != 0.f;
   }
-  // scores of both pages -> weights, 2^-lift as large; masks where edge is set
-  __device__ __forceinline__ void weigh(typename M::Probs (&pr)[RB], const f32x4 (&sa)[RB], const f32x4 (&sb)[RB], const Seen& at, bool edge, float scale2, float lift) {
+  // scores of both pages -> weights; masks where edge is set.  lift: the second time (0 the first)
+  __device__ __forceinline__ void weigh(typename M::Probs (&pr)[RB], const f32x4 (&sa)[RB], const f32x4 (&sb)[RB], const Seen& at, bool edge, float scale2, float slack, float lift) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float v[8], p[8];
@@ -475,16 +482,22 @@ struct State {
           v[4 + k] = k < left_b ? v[4 + k] : -INFINITY;
         }
       }
-      float mx = scale2 * max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[5], v[6], v[7]));
-      if (__ballot(mx > m_run[rb] + kSlack)) {   // (from minus infinity: the first keys)
+      float mx = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[5], v[6], v[7]));
+      if (__ballot(mx > m_run[rb] + slack)) {   // (from minus infinity: the first keys)
         mx = fmaxf(quarter_max(mx), m_run[rb]);
-        const float f = m_run[rb] == mx ? 1.f : __builtin_amdgcn_exp2f(m_run[rb] - mx);
+        const float f = m_run[rb] == mx ? 1.f : __builtin_amdgcn_exp2f(scale2 * (m_run[rb] - mx));
         m_run[rb] = mx;
         M::scale_sum(sum[rb], f);
 #pragma unroll
         for (int t = 0; t < 2 * NB; ++t) acc[rb][t] *= f;
       }
-      const float mb = (m_run[rb] == -INFINITY ? 0.f : m_run[rb]) + lift;
+      float mb = m_run[rb] == -INFINITY ? 0.f : scale2 * m_run[rb];
+      if (lift != 0.f) {
+        asm volatile("");
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] -= m_run[rb] == -INFINITY ? 0.f : m_run[rb];
+        mb = lift;
+      }
 #pragma unroll
       for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], scale2, -mb));
       M::probs(pr[rb], p);
@@ -667,7 +680,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
   const int last_page = (c1 - c0 + DF_PAGE - 1) / DF_PAGE - 1;    // of the range
   const unsigned char* layer = a.c.data + (size_t)a.layer * a.c.n_pages * H * UNIT + (size_t)kvh * UNIT;
   const size_t page_bytes = (size_t)H * UNIT;
-  const float scale2 = a.scale * 1.44269504088896340736f;
+  const float scale2 = a.scale * 1.44269504088896340736f, slack = kSlack / scale2;
 
   // ids of 32 pairs at a time, lane l has page l of them (-1: not there); the next ones are asked for when a set has been used up, and waited for in a branch of their own: where
   // every turn used a register that a load may still be on its way to, the compiler would have every turn wait for all copies
@@ -709,7 +722,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     P pa, pb;
     pa.load_v(pair, lane);
     pb.load_v(pair + UNIT, lane);
-    st.weigh(pr, sa, sb, at, edge, scale2, lift);
+    st.weigh(pr, sa, sb, at, edge, scale2, slack, lift);
     typename M::Values v[L::F32 ? 1 : NB];   // bf16: all blocks, and one branch for the edge; fp32: block by block
     auto block = [&](auto b_c) -> typename M::Values& { return v[L::F32 ? 0 : decltype(b_c)::value]; };
     unrolled<NB>([&](auto b_c) {
@@ -765,7 +778,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the pair has been read before its slot is filled again
         slot ^= 1;
       }
-      if (lift != 0.f || __ballot(st.not_finite()) == 0) break;
+      if (lift != 0.f || __ballot(st.unsound()) == 0) break;
       // again: smaller weights, and whatever value is not finite itself is left out of the products
       lift = kLift;
       left_out = false;
@@ -810,7 +823,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
         const float m = s_m[w][rb * 16 + r];
-        f[w] = m == m_all ? 1.f : __builtin_amdgcn_exp2f(m - m_all);   // (no key in any: all are minus infinity and all sums 0)
+        f[w] = m == m_all ? 1.f : __builtin_amdgcn_exp2f(scale2 * (m - m_all));   // (no key in any: all are minus infinity and all sums 0)
         l += f[w] * s_l[w][rb * 16 + r];
       }
       int j, h;
@@ -852,6 +865,7 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
   if (parts <= 1) return;
   const int d = 4 * (threadIdx.x & 31), hd = a.c.hd;
   const size_t step = (size_t)a.rows * a.n_q_heads, from = (first * (size_t)a.rows + j) * a.n_q_heads + h;
+  const float scale2 = a.scale * 1.44269504088896340736f;
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   constexpr int AHEAD = 4;
@@ -867,7 +881,8 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       if (p0 + i * GROUPS >= parts) break;
-      const float top = fmaxf(m, x[i].x), f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), fx = x[i].x == top ? 1.f : __builtin_amdgcn_exp2f(x[i].x - top);
+      const float top = fmaxf(m, x[i].x), f = m == top ? 1.f : __builtin_amdgcn_exp2f(scale2 * (m - top));
+      const float fx = x[i].x == top ? 1.f : __builtin_amdgcn_exp2f(scale2 * (x[i].x - top));
       const float all = f * l + fx * x[i].y, inv = all == 0.f ? 0.f : __builtin_amdgcn_rcpf(all);
       o = o * (f * l * inv) + y[i] * (fx * x[i].y * inv);
       m = top;
@@ -889,7 +904,7 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
     o = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      f[i] = s_l[i] * (s_m[i] == m_all ? 1.f : __builtin_amdgcn_exp2f(s_m[i] - m_all));
+      f[i] = s_l[i] * (s_m[i] == m_all ? 1.f : __builtin_amdgcn_exp2f(scale2 * (s_m[i] - m_all)));
       l += f[i];
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;

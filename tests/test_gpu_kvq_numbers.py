@@ -40,3 +40,32 @@ def test_weighted_means_of_the_largest_and_smallest_values(case, v_scale):
         x.e.device_status()
         assert bool(x.torch.isfinite(out).all()), (case, v_scale, hint)
         _check(x, q, out, before, lens, counts, causal, 1, (case, v_scale, hint))
+
+
+# power of two of the scores' size; below 2^30 is ordinary ground
+@pytest.mark.parametrize("power", [20, 31, 34, 60, 100])
+@pytest.mark.parametrize("dtype,heads,kv,hd,bits,rows,lens", [("bf16", 4, 1, 64, (4, 4), 1, (200, 2600)), ("f32", 4, 2, 16, (8, 4), 3, (70, 1900)), ("bf16", 32, 8, 64, (4, 8), 40, (900, 33)),
+                                                              ("f32", 2, 1, 64, (4, 4), 20, (2300,))])
+def test_very_large_scores(dtype, heads, kv, hd, bits, rows, lens, power):
+    """q has one dim, so scores are one product and exact, positive for a row of heads and negative for the next: a row is the mean of the keys that share its largest."""
+    counts = (rows,) * len(lens)
+    x = Setup(dtype, heads, kv, hd, bits, len(lens), [n + rows for n in lens], seed=power)
+    _scales(x, 0, 127 + power // 2)
+    _scales(x, 1, 127)
+    x.poison(lens, counts)
+    x.upload()
+    q = x.torch.zeros((len(lens), rows, heads, hd), dtype=x.tdt, device=x.e.device)
+    q[..., 0] = 2.0 ** (power - power // 2)
+    q[:, ::2, :, 0] *= -1
+    q[:, :, 1, 0] *= -1
+    K, V = x.ref.rows(0)
+    for hint in (max(lens), 0):
+        out = x.rows(q.shape)
+        x.B.dflash_kvq_attention(x.e, x.batch(lens, hint), x.cache, 0, q, out)
+        x.e.device_status()
+        got, ref = f64(out), km.attention64(f64(q), K, V, x.table, lens, counts, True, x.n_pages)[0]
+        n = max(lens) + rows
+        # exact scores, so weights that are off by the roundings of exponentials (2^-22 with the exponent's) and, in bf16, of weights, and sums of n; and the output's rounding
+        v = np.abs(V[np.isfinite(V)]).max()
+        tol = v * (2 * (n + 64) * 2.0 ** -24 + 2.0 ** -22 + (2.0 ** -7 if dtype == "bf16" else 0)) + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref)
+        assert np.isfinite(got).all() and (np.abs(got - ref) <= tol).all(), (power, hint, float(np.abs(got - ref).max()))
