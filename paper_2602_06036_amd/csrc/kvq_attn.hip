@@ -5,8 +5,8 @@
 // Row r of a kv head = (slot of the block) * group + query head.  A workgroup takes up to 16 RB of them and a range of keys, its four wavefronts a quarter of the range
 // each, pages in pairs.  Codes become bf16 (fp32 models: fp32) in registers by the conversion instructions that take the block's scale, both exact: e2m1 and e4m3 numbers have
 // 2 and 4 significant bits.  S^T = K Q^T leaves a lane four consecutive keys of a query column, which is how V^T P^T takes them.  Softmax in one pass,
-// base 2, with a reference maximum that moves only when a score passes it by kSlack.  bf16 models: probabilities are rounded to bf16, by 2^-9 of themselves each, where
-// V itself is held to 2^-2 or 2^-4 of its block; their sum is taken over the rounded ones, so the weights still add up to one.  All sums in fp32.
+// base 2, with a reference maximum that moves only when a score passes it by kSlack.  bf16 models: probabilities are hi + lo bf16 pairs, off by 2^-16 of themselves, as everywhere in them; by
+// one number, off by 2^-8, the error against 64 bits was 0.0018 to 0.0020 of a row where the output's own rounding makes 0.0016.  All sums in fp32.
 // Ranges of keys, each the mean of its values with its weights' sum and reference, are joined by kvq_merge_kernel in a fixed order: a call repeats itself bit for bit.
 //
 // Single tokens are bound by memory (32 of them behind 1k to 32k tokens, 32 heads over 8 of 128, 4 bits: 590 MB in 102 us, 5.8 TB/s; the copies by themselves 101); blocks of few pairs a wavefront by
@@ -144,8 +144,8 @@ template <int NB, int KB, int VB>
 struct Math<bf16_t, NB, KB, VB> {
   using P = Page<NB, KB, VB, false>;
   struct Query { u32x4 q[NB]; };
-  struct Sum { f32x4 l; };          // all four and all four lanes of a column the same
-  struct Probs { u32x4 p; };        // four keys of the first page, four of the second
+  struct Sum { float l; };          // the lane's own keys
+  struct Probs { u32x4 p, rest; };  // four keys of the first page, four of the second: hi + lo
   static __device__ __forceinline__ int dim(int g, int j) { return P::OWN ? 8 * (NB * g + j) : 8 * (4 * j + g); }
   static __device__ __forceinline__ void query(Query& f, const bf16_t* row, int hd, int lane) {
 #pragma unroll
@@ -175,14 +175,16 @@ struct Math<bf16_t, NB, KB, VB> {
   }
   static __device__ __forceinline__ void probs(Probs& f, const float (&p)[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f.p[i] = pair_of(p[2 * i], p[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) {
+      f.p[i] = pair_of(p[2 * i], p[2 * i + 1]);
+      f.rest[i] = pair_of(p[2 * i] - __uint_as_float(f.p[i] << 16), p[2 * i + 1] - __uint_as_float(f.p[i] & 0xFFFF0000u));
+    }
   }
-  static __device__ __forceinline__ void sum(Sum& l, const Probs& p, const float (&)[8]) {
-    const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-    l.l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, p.p), l.l, 0, 0, 0);
+  static __device__ __forceinline__ void sum(Sum& l, const Probs&, const float (&p)[8]) {
+    l.l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
   }
   static __device__ __forceinline__ void scale_sum(Sum& l, float f) { l.l *= f; }
-  static __device__ __forceinline__ float total(const Sum& l) { return l.l[0]; }
+  static __device__ __forceinline__ float total(const Sum& l) { return quarter_sum(l.l); }
   struct Values { u32x4 v[2]; };    // dims below 16 of a block, and those from 16 on
   template <int B>
   static __device__ __forceinline__ void values(Values& f, const P& a, const P& b) {
@@ -232,6 +234,8 @@ struct Math<bf16_t, NB, KB, VB> {
   static __device__ __forceinline__ void add(f32x4& lo, f32x4& hi, const Values& v, const Probs& p) {
     lo = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v.v[0]), __builtin_bit_cast(bf16x8, p.p), lo, 0, 0, 0);
     hi = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v.v[1]), __builtin_bit_cast(bf16x8, p.p), hi, 0, 0, 0);
+    lo = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v.v[0]), __builtin_bit_cast(bf16x8, p.rest), lo, 0, 0, 0);
+    hi = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v.v[1]), __builtin_bit_cast(bf16x8, p.rest), hi, 0, 0, 0);
   }
 };
 
@@ -465,9 +469,10 @@ struct State {
   }
   // scores of both pages -> weights; masks where edge is set.  lift: the second time (0 the first)
   __device__ __forceinline__ void weigh(typename M::Probs (&pr)[RB], const f32x4 (&sa)[RB], const f32x4 (&sb)[RB], const Seen& at, bool edge, float scale2, float slack, float lift) {
+    float all[RB][8], ref[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      float v[8], p[8];
+      float (&v)[8] = all[rb];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         v[k] = sa[rb][k];
@@ -491,15 +496,22 @@ struct State {
 #pragma unroll
         for (int t = 0; t < 2 * NB; ++t) acc[rb][t] *= f;
       }
-      float mb = m_run[rb] == -INFINITY ? 0.f : scale2 * m_run[rb];
-      if (lift != 0.f) {
-        asm volatile("");
+      ref[rb] = m_run[rb] == -INFINITY ? 0.f : scale2 * m_run[rb];
+    }
+    if (lift != 0.f) {
+      asm volatile("");
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] -= m_run[rb] == -INFINITY ? 0.f : m_run[rb];
-        mb = lift;
+      for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) all[rb][k] -= m_run[rb] == -INFINITY ? 0.f : m_run[rb];
+        ref[rb] = lift;
       }
+    }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], scale2, -mb));
+    for (int rb = 0; rb < RB; ++rb) {
+      float p[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(all[rb][k], scale2, -ref[rb]));
       M::probs(pr[rb], p);
       M::sum(sum[rb], pr[rb], p);
     }

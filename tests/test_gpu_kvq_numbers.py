@@ -69,3 +69,64 @@ def test_very_large_scores(dtype, heads, kv, hd, bits, rows, lens, power):
         v = np.abs(V[np.isfinite(V)]).max()
         tol = v * (2 * (n + 64) * 2.0 ** -24 + 2.0 ** -22 + (2.0 ** -7 if dtype == "bf16" else 0)) + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref)
         assert np.isfinite(got).all() and (np.abs(got - ref) <= tol).all(), (power, hint, float(np.abs(got - ref).max()))
+
+
+def _pair_bound(ref, slack, wabs, dtype):
+    """bf16 weights as hi + lo: hi is off by 2^-8 of itself at most and lo holds that to 2^-8 of it, so weights by 2^-16 and their shares by twice that; the output's rounding, 2^-8 of
+    the value."""
+    if dtype == "f32":
+        return km.allowed(ref, slack, wabs, dtype)
+    return slack + 2.0 ** -15 * (1 + 2.0 ** -8) * wabs + 2.0 ** -8 * (1 + 2.0 ** -7) * np.abs(ref)
+
+
+@pytest.mark.parametrize("heads,kv,hd,bits,rows,lens", [(4, 1, 128, (8, 8), 1, (3, 4, 2, 6, 1)), (8, 2, 64, (4, 8), 6, (2, 0, 9)), (8, 2, 96, (4, 4), 16, (1, 5)), (10, 2, 80, (8, 4), 3, (7, 2, 700)),
+                                                        (32, 8, 128, (4, 4), 17, (800, 5))])
+def test_bf16_weights_are_held_to_sixteen_bits(heads, kv, hd, bits, rows, lens):
+    """Few keys, whose values cancel in some dims: there the output's own rounding is small, and weights of eight bits would be seen."""
+    counts = (rows,) * len(lens)
+    x = Setup("bf16", heads, kv, hd, bits, len(lens), [n + rows for n in lens], seed=hd + rows, scales=(124, 129))
+    x.poison(lens, counts)
+    x.upload()
+    q, out = x.rows((len(lens), rows, heads, hd), 0.1), x.rows((len(lens), rows, heads, hd))
+    x.B.dflash_kvq_attention(x.e, x.batch(lens), x.cache, 1, q, out)
+    x.e.device_status()
+    ref, slack, wabs = km.attention64(f64(q), *x.ref.rows(1), x.table, lens, counts, True, x.n_pages)
+    over = np.abs(f64(out) - ref) / np.maximum(_pair_bound(ref, slack, wabs, "bf16"), 1e-30)
+    assert over.max() <= 1, float(over.max())
+
+
+@pytest.mark.parametrize("dtype,hd,bits,rows", [("bf16", 128, (4, 4), 1), ("bf16", 64, (8, 8), 40), ("f32", 48, (4, 8), 5), ("bf16", 32, (8, 4), 9)])
+def test_values_beyond_the_type_are_infinities(dtype, hd, bits, rows):
+    """Codes that stand for more than the type's largest number: an infinity of their sign in the rows that see the key, whatever its weight, among keys that all rows see and behind."""
+    heads, kv, lens = 4, 2, (200, 2000)
+    counts = (rows, rows)
+    x = Setup(dtype, heads, kv, hd, bits, 2, [n + rows for n in lens], seed=rows, scales=(120, 124))
+    x.poison(lens, counts)
+    (at, shift), e_at = x.ref.at[1], x.ref.at[3]
+    b = bits[1]
+    hits = [(0, 5, 0, 3, 0), (0, 200 + rows - 1, 1, 1, 1), (1, 1203, 0, hd - 1, 1), (1, 40, 1, 0, 0), (1, 2000, 1, 2, 0)]   # sequence, position, head, dim, sign
+    for s, p, h, d, neg in hits:
+        unit, key = x.ref.data[:, x.table[s, p // PAGE], h], p % PAGE
+        blk = d // 32
+        unit[:, at[key, blk]] = 0
+        sh = int(shift[key, blk, d % 32])
+        unit[:, at[key, blk, d % 32]] |= ((6 if b == 4 else 0x78) | ((8 if b == 4 else 0x80) if neg else 0)) << sh      # 4 or 256 ...
+        unit[:, e_at[key, blk]] = 253 if b == 4 else 247                                                              # ... times 2^126 or 2^120
+    x.upload()
+    q, out = x.rows((2, rows, heads, hd), 0.5), x.rows((2, rows, heads, hd))
+    before = out.clone()
+    want = {}
+    for s, p, h, d, neg in hits:
+        for j in range(rows):
+            if p <= lens[s] + j:
+                for g in range(heads // kv):
+                    want[(s, j, h * (heads // kv) + g, d)] = -np.inf if neg else np.inf
+    x.B.dflash_kvq_attention(x.e, x.batch(lens), x.cache, 0, q, out)
+    x.e.device_status()
+    got = f64(out)
+    bad = ~np.isfinite(got)
+    assert {tuple(int(i) for i in at_): got[tuple(at_)] for at_ in np.argwhere(bad)} == want
+    # the other elements as if the values were not there
+    ref, slack, wabs = km.attention64(f64(q), *(np.where(np.abs(t) > 2.0 ** 127, 0.0, t) for t in x.ref.rows(0)), x.table, lens, counts, True, x.n_pages)
+    tol = _pair_bound(ref, slack, wabs, dtype)
+    assert (np.abs(got - ref)[~bad] <= tol[~bad]).all()
