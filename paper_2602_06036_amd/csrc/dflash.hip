@@ -1509,8 +1509,7 @@ int kvq_pages_checked(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* 
   if (b->n_seqs == 0) return DFLASH_OK;
   if ((rc = check_kvq(ctx, b, q, what))) return rc;
   if (!table) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: null table", what);
-  const int pages = (b->max_seq_len + DFLASH_PAGE_SIZE - 1) / DFLASH_PAGE_SIZE;
-  if (pages == 0) return DFLASH_OK;
+  const int pages = (b->max_seq_len + DFLASH_PAGE_SIZE - 1) / DFLASH_PAGE_SIZE;   // (0: the launch still looks at the lengths)
   const dflash_dims& m = kvq_model(ctx, q);
   if (m.n_layers > 65535) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: more than 65535 layers", what);
   const KvqPages a{kvq_cache(m, q), m.n_layers, b->n_seqs, pages, ctx->rt.max_pages_per_seq, ctx->rt.n_pages, b->seq_lens, b->block_table, table,

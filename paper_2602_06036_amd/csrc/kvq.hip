@@ -1,6 +1,7 @@
 // Rows and pages of caches held in 4 or 8 bits (kvq.h): quantised as they are written, read back, packed from a context's pool and unpacked into it.
 // One wavefront takes one page of one kv head.  All of it is bound by memory; a block's 32 elements are in one lane (rows) or in the 16 lanes of a row of lanes (V of a pool's
 // page), so a block's maximum costs no trip through LDS.
+#include <algorithm>
 #include <type_traits>
 
 #include "kvq.h"
@@ -551,7 +552,7 @@ void rows_launch(const KvqRows& a, bool bf16, hipStream_t st) {
 }
 template <bool PACK>
 void pages_launch(const KvqPages& a, bool bf16, hipStream_t st) {
-  const dim3 grid((unsigned)(((long long)a.max_pages * a.c.n_kv_heads + kRowWaves - 1) / kRowWaves), a.n_layers, a.n_seqs), block(64 * kRowWaves);
+  const dim3 grid((unsigned)(((long long)std::max(a.max_pages, 1) * a.c.n_kv_heads + kRowWaves - 1) / kRowWaves), a.n_layers, a.n_seqs), block(64 * kRowWaves);
   auto go = [&](auto nb) {
     constexpr int NB = decltype(nb)::value;
     if (bf16) hipLaunchKernelGGL((kvq_pages_kernel<bf16_t, NB, PACK>), grid, block, 0, st, a);
