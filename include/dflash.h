@@ -320,7 +320,7 @@ int dflash_kvq_read(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq
 
 /* Attention over the cache: rows j < counts[s] (nullable: all `rows`) of sequence s at positions seq_lens[s] + j, whose own K/V rows are there already; causal != 0: row j sees
  * positions up to seq_lens[s] + j, else all seq_lens[s] + counts[s].  rows >= 1, not bound to the context's block size: 1 is plain decoding, hundreds are a piece of a prompt.  The batch's
- * max_seq_len balances launches only.  Entries of the block table outside the cache are keys that are not there; a row that sees no key is zeros.  An infinity or NaN in a row of K or V
+ * max_seq_len balances launches only.  A length that is negative or that the block-table row does not cover counts as the nearest one that there is, and raises the sticky status.  Entries of the block table outside the cache are keys that are not there; a row that sees no key is zeros.  An infinity or NaN in a row of K or V
  * reaches the rows that see the key, and only them; a row whose scores are all minus infinity (q with an infinity) is zeros too.  q (device) [S, rows, n_q_heads, head_dim] after norm and rotation, out (device) the same shape; both in the model's dtype, contiguous,
  * 16-byte aligned, apart from each other; rows behind counts[s] are left as they are.  Uses the workspace as the step's calls do. */
 int dflash_kvq_attention(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, int32_t layer, int32_t rows, const int32_t *counts, int32_t causal,

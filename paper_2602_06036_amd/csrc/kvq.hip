@@ -405,7 +405,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void kvq_pages_kernel(KvqPages a) {
   const int i = blockIdx.x * kRowWaves + wave, H = a.c.n_kv_heads;
   const int s = blockIdx.z, layer = blockIdx.y, head = i % H, index = i / H;
   const int len = min(max(a.lens[s], 0), a.mpps * DF_PAGE);
-  if (i == 0 && layer == 0 && lane == 0 && (a.lens[s] > a.max_pages * DF_PAGE || a.lens[s] > a.mpps * DF_PAGE)) atomicOr(a.status, DF_STATUS_CAPACITY);
+  if (i == 0 && layer == 0 && lane == 0 && (a.lens[s] < 0 || a.lens[s] > a.max_pages * DF_PAGE || a.lens[s] > a.mpps * DF_PAGE)) atomicOr(a.status, DF_STATUS_CAPACITY);
   if (index >= a.max_pages || index * DF_PAGE >= len) return;
   const int from = a.pool_table[(size_t)s * a.mpps + index], to = a.table[(size_t)s * a.mpps + index];
   if (from < 0 || from >= a.pool_pages || to < 0 || to >= a.c.n_pages) {

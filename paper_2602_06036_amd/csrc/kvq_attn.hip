@@ -356,13 +356,13 @@ template <> __device__ __forceinline__ void store_row4<bf16_t>(bf16_t* p, f32x4 
 // What a sequence's rows see: the same in the attention and the merge launch.
 struct SeqRows {
   int len, count, n_tok;
-  bool outgrown;
+  bool odd;   // a length or count that the call does not have
   __device__ __forceinline__ SeqRows(const KvqAttn& a, int s) {
     const int cap = a.mpps * DF_PAGE, c = a.counts ? a.counts[s] : a.rows, n = a.lens[s];
     len = min(max(n, 0), cap);
     count = min(max(c, 0), a.rows);
     n_tok = count > 0 ? min(len + count, cap) : 0;
-    outgrown = c > a.rows || (count > 0 && n > cap - count);
+    odd = c > a.rows || (count > 0 && (n < 0 || n > cap - count));
   }
   // keys in front of the first one that slot j does not see
   __device__ __forceinline__ int end(const KvqAttn& a, int j) const { return a.causal ? min(len + j + 1, n_tok) : n_tok; }
@@ -638,7 +638,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
   const int split = part - first;
   const SeqRows rows(a, s);
   const int row0 = tile * 16 * RB, n_rows = min(rows.count * group - row0, 16 * RB);
-  if (rows.outgrown && split + kvh + tile == 0 && threadIdx.x == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
+  if (rows.odd && split + kvh + tile == 0 && threadIdx.x == 0) atomicOr(a.status, DF_STATUS_CAPACITY);
   if (n_rows <= 0) return;
   const int end = rows.end(a, (row0 + n_rows - 1) / group);      // keys that some row of the tile sees
   const int all_see = rows.end(a, row0 / group);                 // ... that all rows see

@@ -50,3 +50,34 @@ def test_a_hint_of_no_tokens_does_not_lose_a_request_in_silence(lens):
     for call in (x.B.dflash_kvq_pack, x.B.dflash_kvq_unpack):       # nothing there, nothing said
         call(x.e, x.batch([0, 0], 0), x.cache, x.theirs)
     x.e.device_status()
+
+
+@pytest.mark.parametrize("lens", [[-1, 20], [33, -(2 ** 31)]])
+def test_negative_lengths_of_requests_raise_the_status(lens):
+    x = Pool()
+    for call in (x.B.dflash_kvq_pack, x.B.dflash_kvq_unpack):
+        for hint in (0, 40):
+            call(x.e, x.batch(lens, hint), x.cache, x.theirs)
+            x.status_is_capacity()
+    at = 0 if lens[0] < 0 else 1                              # such a sequence's pages stay as they are
+    gone = x.theirs[at].long()
+    assert bool((x.data.view(x.n, -1)[gone] == 7).all())
+
+
+@pytest.mark.parametrize("lens,hint", [([-1, 20, 0], 20), ([500, 3, -7], 500), ([-(2 ** 31), 0, 700], 0)])
+def test_negative_lengths_of_attention_count_as_none_and_raise_the_status(lens, hint):
+    real = [max(n, 0) for n in lens]
+    x = Setup("bf16", 4, 2, 64, (4, 8), 3, [n + 3 for n in real])
+    x.poison(real, (3, 3, 3))
+    x.upload()
+    q, out = x.rows((3, 3, 4, 64)), x.rows((3, 3, 4, 64))
+    before = out.clone()
+    for counts in ((3, 3, 3), (1, 2, 3)):
+        out.copy_(before)
+        x.B.dflash_kvq_attention(x.e, x.batch(lens, hint), x.cache, 0, q, out, counts=x.ints(counts))
+        with pytest.raises(x.B.DFlashError) as err:
+            x.e.device_status()
+        assert err.value.code == x.B.DFLASH_ECAPACITY
+        _check(x, q, out, before, real, counts, True, 0, (lens, counts))
+    x.B.dflash_kvq_attention(x.e, x.batch(lens, hint), x.cache, 0, q, out, counts=x.ints([0 if n < 0 else 1 for n in lens]))   # no rows of it, nothing to say
+    x.e.device_status()
