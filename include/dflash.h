@@ -297,7 +297,7 @@ int dflash_group_attention(dflash_ctx *ctx, const dflash_batch *batch, const dfl
  *   V, 4 bits: [q][d % 16][b][k], dim below 16 low   V, 8 bits, per pair of blocks: [q][d % 16][b % 2][k][d / 16]
  *   scales: [key][NB, of three blocks 4]
  * The calls below are enqueued on `stream`, read nothing back and allocate nothing; they belong to a batch whose seq_lens and block_table (row length max_pages_per_seq, as
- * everywhere) speak of this cache's pages, 0..n_pages-1.  Rows whose page is none of those, and ranges that a call does not have, are skipped and raise the sticky
+ * everywhere) speak of this cache's pages, 0..n_pages-1 (anchor and block_size are not looked at, and max_seq_len is at most what a block-table row covers: no block has to fit behind it).  Rows whose page is none of those, and ranges that a call does not have, are skipped and raise the sticky
  * device status.  Sequences of a call must not write to the same page; dflash_pages_* calls move and count the pages of the context's pools only. */
 typedef struct {
   void *data;      /* (device) dflash_kvq_bytes() bytes, 256-byte aligned */

@@ -1381,13 +1381,18 @@ int run_kv_copy(dflash_ctx* ctx, const dflash_batch* b, int pool, int layer, int
   return e.hip_err ? DFLASH_EHIP : DFLASH_OK;
 }
 
-int check_batch(dflash_ctx* ctx, const dflash_batch* b) {
+int check_seqs(dflash_ctx* ctx, const dflash_batch* b, bool anchors) {
   if (!ctx) return fail(nullptr, DFLASH_EINVAL, "ctx: null");
   if (!b) return CTX_FAIL(ctx, DFLASH_EINVAL, "batch: null pointer");
   if (b->n_seqs == 0) return DFLASH_OK;   // an empty batch is valid: the step calls enqueue nothing
-  if (!b->seq_lens || !b->block_table || !b->anchor) return CTX_FAIL(ctx, DFLASH_EINVAL, "batch: null pointer");
+  if (!b->seq_lens || !b->block_table || (anchors && !b->anchor)) return CTX_FAIL(ctx, DFLASH_EINVAL, "batch: null pointer");
   if (b->n_seqs < 0 || b->n_seqs > ctx->rt.max_seqs) return CTX_FAIL(ctx, DFLASH_EINVAL, "batch: n_seqs %d outside [0,%d]", b->n_seqs, ctx->rt.max_seqs);
   if (b->max_seq_len < 0) return CTX_FAIL(ctx, DFLASH_EINVAL, "batch: negative max_seq_len");
+  return DFLASH_OK;
+}
+int check_batch(dflash_ctx* ctx, const dflash_batch* b) {
+  const int rc = check_seqs(ctx, b, true);
+  if (rc || b->n_seqs == 0) return rc;
   if (b->block_size != 0 && (b->block_size < 2 || b->block_size > ctx->rt.block_size))
     return CTX_FAIL(ctx, DFLASH_EINVAL, "batch: block_size %d outside [2,%d] (0 = the context's)", b->block_size, ctx->rt.block_size);
   const int blk = b->block_size > 0 ? b->block_size : ctx->rt.block_size;
@@ -1461,6 +1466,14 @@ const dflash_dims& kvq_model(const dflash_ctx* ctx, const dflash_kvq* q) { retur
 KvqCache kvq_cache(const dflash_dims& m, const dflash_kvq* q) {
   return KvqCache{static_cast<unsigned char*>(q->data), q->n_pages, m.n_kv_heads, m.head_dim, q->k_bits, q->v_bits};
 }
+// (no block of the step's stands behind these calls' sequences: they may fill their block-table row)
+int check_kvq_batch(dflash_ctx* ctx, const dflash_batch* b) {
+  const int rc = check_seqs(ctx, b, false);
+  if (rc || b->n_seqs == 0) return rc;
+  const int64_t cap = (int64_t)ctx->rt.max_pages_per_seq * DFLASH_PAGE_SIZE;
+  if (b->max_seq_len > cap) return CTX_FAIL(ctx, DFLASH_ECAPACITY, "batch: max_seq_len %d exceeds the %lld tokens a block-table row covers", b->max_seq_len, (long long)cap);
+  return DFLASH_OK;
+}
 int check_kvq(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q, const char* what) {
   if (!q || !q->data) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: null cache", what);
   if (q->pool != DFLASH_POOL_TARGET && q->pool != DFLASH_POOL_DRAFT) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: bad pool", what);
@@ -1490,7 +1503,7 @@ int kvq_rows_checked(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q
                      bool write, void* stream) {
   const char* what = write ? "kvq_write" : "kvq_read";
   int rc;
-  if ((rc = check_batch(ctx, b))) return rc;
+  if ((rc = check_kvq_batch(ctx, b))) return rc;
   if (b->n_seqs == 0) return DFLASH_OK;
   if ((rc = check_kvq(ctx, b, q, what)) || (rc = check_kvq_rows(ctx, b, q, layer, rows, what))) return rc;
   if (!first) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: null starts", what);
@@ -1505,7 +1518,7 @@ int kvq_rows_checked(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q
 int kvq_pages_checked(dflash_ctx* ctx, const dflash_batch* b, const dflash_kvq* q, const int32_t* table, bool pack, void* stream) {
   const char* what = pack ? "kvq_pack" : "kvq_unpack";
   int rc;
-  if ((rc = check_batch(ctx, b))) return rc;
+  if ((rc = check_kvq_batch(ctx, b))) return rc;
   if (b->n_seqs == 0) return DFLASH_OK;
   if ((rc = check_kvq(ctx, b, q, what))) return rc;
   if (!table) return CTX_FAIL(ctx, DFLASH_EINVAL, "%s: null table", what);
@@ -1992,7 +2005,7 @@ int dflash_kvq_read(dflash_ctx* ctx, const dflash_batch* batch, const dflash_kvq
 int dflash_kvq_attention(dflash_ctx* ctx, const dflash_batch* batch, const dflash_kvq* cache, int32_t layer, int32_t rows, const int32_t* counts, int32_t causal,
                          const void* q, void* out, void* stream) {
   int rc;
-  if ((rc = check_batch(ctx, batch))) return rc;
+  if ((rc = check_kvq_batch(ctx, batch))) return rc;
   if (batch->n_seqs == 0) return DFLASH_OK;
   if ((rc = check_kvq(ctx, batch, cache, "kvq_attention")) || (rc = check_kvq_rows(ctx, batch, cache, layer, rows, "kvq_attention"))) return rc;
   if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 15)) return CTX_FAIL(ctx, DFLASH_EINVAL, "kvq_attention: q and out must be 16-byte aligned device buffers");

@@ -81,3 +81,76 @@ def test_negative_lengths_of_attention_count_as_none_and_raise_the_status(lens, 
         _check(x, q, out, before, real, counts, True, 0, (lens, counts))
     x.B.dflash_kvq_attention(x.e, x.batch(lens, hint), x.cache, 0, q, out, counts=x.ints([0 if n < 0 else 1 for n in lens]))   # no rows of it, nothing to say
     x.e.device_status()
+
+
+@pytest.mark.parametrize("rows,short", [(1, 1), (1, 0), (16, 16), (5, 4)])
+def test_sequences_may_fill_their_block_table_row(rows, short):
+    """The context's block of 16 rows means nothing to rows and attention: the last of them may be at the row's last position, under a hint that says so."""
+    x = Setup("bf16", 4, 2, 64, (8, 4), 2, [40, 100], block=16, extra=4)
+    spare = [p for p in range(x.n_pages) if p not in x.table]
+    x.table[1, -2:] = spare[:2]
+    cap = x.width * PAGE
+    lens = [20, cap - short]
+    counts = [rows, min(rows, short)]
+    x.upload()
+    b = x.batch(lens)
+    k, v, q = x.rows((2, rows, 2, 64)), x.rows((2, rows, 2, 64)), x.rows((2, rows, 4, 64))
+    c = x.ints(counts)
+    x.B.dflash_kvq_write(x.e, b, x.cache, 1, k, v, counts=c)
+    for s in range(2):
+        for j in range(counts[s]):
+            p = lens[s] + j
+            x.ref.put(1, x.table[s, p // PAGE], p % PAGE, f64(k[s, j]), f64(v[s, j]))
+    assert np.array_equal(x.data.cpu().numpy(), x.ref.data)
+    ko, vo = x.torch.zeros_like(k), x.torch.zeros_like(v)
+    x.B.dflash_kvq_read(x.e, b, x.cache, 1, ko, vo, x.lens_dev, counts=c)
+    want = x.ref.rows(1)
+    for s in range(2):
+        for j in range(counts[s]):
+            p = lens[s] + j
+            for o, w in zip((ko, vo), want):
+                assert np.array_equal(f64(o[s, j]), f64(x.torch.from_numpy(w[x.table[s, p // PAGE], p % PAGE]).to(x.tdt)))
+    for causal in (True, False):
+        out = x.rows(q.shape)
+        before = out.clone()
+        x.B.dflash_kvq_attention(x.e, b, x.cache, 1, q, out, counts=c, causal=causal)
+        x.e.device_status()
+        _check(x, q, out, before, lens, counts, causal, 1, (rows, short, causal))
+
+
+@pytest.mark.parametrize("lens", [[64, 3], [48, 64], [49, 60]])
+def test_requests_that_fill_their_block_table_row_are_put_aside_and_taken_up(lens):
+    x = Pool(block=16, bits=(8, 8))
+    before = x.e.target_pool.clone()
+    b = x.batch(lens, max(lens))
+    x.B.dflash_kvq_pack(x.e, b, x.cache, x.theirs)
+    x.e.target_pool.zero_()
+    x.B.dflash_kvq_unpack(x.e, b, x.cache, x.theirs)
+    x.e.device_status()
+    # [page, kv head, K | V, 16 rows of 64]: K [dim / 8][key][8], V [dim / 16][key / 4][dim % 16][key % 4]
+    def rows(pool):
+        p = pool.view(x.torch.bfloat16).view(x.n, 2, 2, 16 * 64).double().cpu()
+        return p[:, :, 0].view(x.n, 2, 8, 16, 8).permute(0, 3, 1, 2, 4).reshape(x.n, 16, 2, 64), p[:, :, 1].view(x.n, 2, 4, 4, 16, 4).permute(0, 3, 5, 1, 2, 4).reshape(x.n, 16, 2, 64)
+    table = x.mine.cpu().numpy()
+    for old, new in zip(rows(before), rows(x.e.target_pool)):
+        for s, n in enumerate(lens):
+            for p in range(16 * x.width):
+                a, w = new[table[s, p // PAGE], p % PAGE].numpy(), old[table[s, p // PAGE], p % PAGE].numpy()
+                assert np.array_equal(a, km.values(*km.quantise(w, 8), 8, 64) if p < n else 0 * w), (s, p)
+
+
+def test_hints_beyond_the_block_table_row_are_refused():
+    import ctypes as C
+    x = Pool(block=16)
+    q = x.torch.zeros((2, 1, 4, 64), dtype=x.torch.bfloat16, device=x.e.device)
+    out, k = q.clone(), q[:, :, :2].contiguous()
+    b = x.batch([1, 1], 65)
+    for call in (lambda: x.B.dflash_kvq_pack(x.e, b, x.cache, x.theirs), lambda: x.B.dflash_kvq_unpack(x.e, b, x.cache, x.theirs),
+                 lambda: x.B.dflash_kvq_write(x.e, b, x.cache, 0, k, k), lambda: x.B.dflash_kvq_attention(x.e, b, x.cache, 0, q, out)):
+        with pytest.raises(x.B.DFlashError) as err:
+            call()
+        assert err.value.code == x.B.DFLASH_ECAPACITY and "max_seq_len" in str(err.value)
+    # neither anchors nor a block of the step's are looked at
+    b = x.B.Batch(2, 20, x.lens.data_ptr(), x.theirs.data_ptr(), None, 99)
+    x.B.dflash_kvq_attention(x.e, b, x.cache, 0, q, out)
+    x.e.device_status()
