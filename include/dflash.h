@@ -336,7 +336,7 @@ int dflash_kvq_unpack(dflash_ctx *ctx, const dflash_batch *batch, const dflash_k
  * While enabled, every GEMM and attention launch is bracketed by a pair of HIP events on the caller's
  * stream (this slows the step down: time whole steps with profiling off).  dflash_profile_read
  * synchronises the stream, sums elapsed milliseconds, launch counts and algorithmic bytes (GEMM: the
- * weight matrix once; attention: the K and V rows within the host's max_seq_len hint once) per class
+ * weight matrix once; attention: the K and V rows within the host's max_seq_len hint once, codes and scales where the cache is held in 4 or 8 bits) per class
  * into arrays of DFLASH_PROF_CLASSES entries (host) and forgets the recorded launches. */
 #define DFLASH_PROF_CLASSES 8
 enum {

@@ -2023,7 +2023,14 @@ int dflash_kvq_attention(dflash_ctx* ctx, const dflash_batch* batch, const dflas
   const bool bf16 = m.dtype == DFLASH_BF16;
   const int64_t most = std::min<int64_t>((int64_t)batch->max_seq_len + rows, (int64_t)ctx->rt.max_pages_per_seq * DFLASH_PAGE_SIZE);
   if (!kvq_attn_plan(a, bf16, (int)most, ctx->ws.part_rows)) return CTX_FAIL(ctx, DFLASH_EINVAL, "kvq_attention: %d sequences of %d rows are too many for one launch", batch->n_seqs, rows);
-  kvq_attn_launch(a, bf16, (hipStream_t)stream);
+  {
+    const double bytes = (double)a.n_seqs * most * m.n_kv_heads * kvq_unit(kvq_blocks(m.head_dim), cache->k_bits, cache->v_bits) / DFLASH_PAGE_SIZE;
+    ProfScope prof(ctx, (hipStream_t)stream, DFLASH_PROF_ATTN, bytes);
+    kvq_attn_launch(a, bf16, (hipStream_t)stream);
+  }
+  if ((rc = launched(ctx, "kvq_attention")) || !a.parts) return rc;
+  ProfScope prof(ctx, (hipStream_t)stream, DFLASH_PROF_ATTN_MERGE, 0.0);
+  kvq_merge_launch(a, bf16, (hipStream_t)stream);
   return launched(ctx, "kvq_attention");
 }
 

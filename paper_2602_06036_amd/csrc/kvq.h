@@ -62,6 +62,7 @@ void kvq_unpack_launch(const KvqPages& a, bool bf16, hipStream_t st);
 // fills in parts and tiles: part_rows partial rows fit part_o and part_ml; max_tokens: the longest sequence with its rows.  False: no launch is that large
 bool kvq_attn_plan(KvqAttn& a, bool bf16, int max_tokens, size_t part_rows);
 void kvq_attn_launch(const KvqAttn& a, bool bf16, hipStream_t st);
+void kvq_merge_launch(const KvqAttn& a, bool bf16, hipStream_t st);   // where a.parts is not 0
 
 #ifdef __HIPCC__
 // ---- device side ----------------------------------------------------------------------------------------------------------

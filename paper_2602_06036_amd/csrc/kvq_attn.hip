@@ -929,23 +929,32 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
 template <typename T, int NB, int KB, int VB>
 void launch(const KvqAttn& a, int tile, hipStream_t st) {
   const dim3 grid((unsigned)((long long)(a.n_seqs + a.parts) * a.tiles * a.c.n_kv_heads));
-  auto join = [&](auto rows_c) {
-    constexpr int ROWS = decltype(rows_c)::value;
-    const int rows = a.rows * a.n_q_heads;
-    if (!a.parts) return;
-    if ((long long)rows * a.n_seqs < 4096) hipLaunchKernelGGL((kvq_merge_kernel<T, ROWS, 8>), dim3(rows, a.n_seqs), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((kvq_merge_kernel<T, ROWS, 1>), dim3((rows + 7) / 8, a.n_seqs), dim3(256), 0, st, a);
-  };
   auto go = [&](auto rb_c) {
     constexpr int RB = decltype(rb_c)::value;
     hipLaunchKernelGGL((kvq_attn_kernel<T, NB, KB, VB, RB>), grid, dim3(64 * Launch<T, NB, KB, VB, RB>::WAVES), 0, st, a);
-    join(std::integral_constant<int, 16 * RB>());
   };
   if (tile == 16) go(std::integral_constant<int, 1>());
   else if constexpr (std::is_same<T, bf16_t>::value) {
     if (tile == 32) go(std::integral_constant<int, 2>());
     else if constexpr (kvq_tiles_of_64(NB, KB, VB)) go(std::integral_constant<int, 4>());
   }
+}
+template <typename T>
+void launch_merge(const KvqAttn& a, int tile, hipStream_t st) {
+  auto go = [&](auto rows_c) {
+    constexpr int ROWS = decltype(rows_c)::value;
+    const int rows = a.rows * a.n_q_heads;
+    if ((long long)rows * a.n_seqs < 4096) hipLaunchKernelGGL((kvq_merge_kernel<T, ROWS, 8>), dim3(rows, a.n_seqs), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((kvq_merge_kernel<T, ROWS, 1>), dim3((rows + 7) / 8, a.n_seqs), dim3(256), 0, st, a);
+  };
+  if (tile == 16) go(std::integral_constant<int, 16>());
+  else if constexpr (std::is_same<T, bf16_t>::value) {
+    if (tile == 32) go(std::integral_constant<int, 32>());
+    else go(std::integral_constant<int, 64>());
+  }
+}
+int tile_rows(const KvqAttn& a, bool bf16) {
+  return kvq_tile_rows(bf16, a.rows * (a.n_q_heads / a.c.n_kv_heads), kvq_tiles_of_64(kvq_blocks(a.c.hd), a.c.k_bits, a.c.v_bits));
 }
 template <typename T, int NB>
 void launch_bits(const KvqAttn& a, int rb, hipStream_t st) {
@@ -972,7 +981,10 @@ bool kvq_attn_plan(KvqAttn& a, bool bf16, int max_tokens, size_t part_rows) {
 }
 
 void kvq_attn_launch(const KvqAttn& a, bool bf16, hipStream_t st) {
-  const int tile = kvq_tile_rows(bf16, a.rows * (a.n_q_heads / a.c.n_kv_heads), kvq_tiles_of_64(kvq_blocks(a.c.hd), a.c.k_bits, a.c.v_bits));
-  if (bf16) launch_type<bf16_t>(a, tile, st);
-  else launch_type<float>(a, tile, st);
+  if (bf16) launch_type<bf16_t>(a, tile_rows(a, true), st);
+  else launch_type<float>(a, tile_rows(a, false), st);
+}
+void kvq_merge_launch(const KvqAttn& a, bool bf16, hipStream_t st) {
+  if (bf16) launch_merge<bf16_t>(a, tile_rows(a, true), st);
+  else launch_merge<float>(a, tile_rows(a, false), st);
 }

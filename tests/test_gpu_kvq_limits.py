@@ -154,3 +154,26 @@ def test_hints_beyond_the_block_table_row_are_refused():
     b = x.B.Batch(2, 20, x.lens.data_ptr(), x.theirs.data_ptr(), None, 99)
     x.B.dflash_kvq_attention(x.e, b, x.cache, 0, q, out)
     x.e.device_status()
+
+
+@pytest.mark.parametrize("rows,lens,cut", [(1, [2000, 900, 40], True), (16, [30, 9, 0], False)])
+def test_attention_launches_are_bracketed(rows, lens, cut):
+    """dflash_profile_enable speaks of every attention launch: those of these calls, and the launches that join their ranges."""
+    x = Setup("bf16", 8, 2, 64, (4, 8), 3, [n + rows for n in lens]).upload()
+    q = x.rows((3, rows, 8, 64))
+    out = x.torch.zeros_like(q)
+    b = x.batch(lens)
+    x.e.profile_enable(True)
+    try:
+        for _ in range(3):
+            x.B.dflash_kvq_attention(x.e, b, x.cache, 1, q, out)
+        prof = x.e.profile_read()
+    finally:
+        x.e.profile_enable(False)
+    ms, n, read = prof[3]
+    assert n == 3 and ms > 0
+    assert read == 3 * 3 * (max(lens) + rows) * 2 * km.unit_bytes(64, 4, 8) / PAGE
+    if cut:
+        assert prof[4][1] == 3 and prof[4][0] > 0
+    else:
+        assert 4 not in prof
