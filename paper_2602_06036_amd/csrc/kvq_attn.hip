@@ -432,8 +432,8 @@ struct Ranges {
 struct Seen {
   int base, g;
   bool ok_a, ok_b;
-  __device__ __forceinline__ unsigned before(int stop) const {   // those of the lane's eight keys in front of `stop`, a bit each
-    const int left = stop - base - 4 * g, a4 = ok_a ? min(max(left, 0), 4) : 0, b4 = ok_b ? min(max(left - DF_PAGE, 0), 4) : 0;
+  __device__ __forceinline__ unsigned before(int stop) const {   // those of the lane's eight keys in front of `stop` + 4 g, a bit each
+    const int left = stop - base, a4 = ok_a ? min(max(left, 0), 4) : 0, b4 = ok_b ? min(max(left - DF_PAGE, 0), 4) : 0;
     return ((1u << a4) - 1) | ((1u << b4) - 1) << 4;
   }
 };
@@ -442,7 +442,7 @@ struct State {
   f32x4 acc[RB][2 * NB];
   typename M::Sum sum[RB];
   float m_run[RB];   // in units of the scores
-  int row_end[RB];
+  int row_end[RB];   // keys in front of the first one that the row does not see, less 4 g
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -467,8 +467,8 @@ struct State {
     }
     return odd || t != 0.f;
   }
-  // scores of both pages -> weights; masks where edge is set.  lift: the second time (0 the first)
-  __device__ __forceinline__ void weigh(typename M::Probs (&pr)[RB], const f32x4 (&sa)[RB], const f32x4 (&sb)[RB], const Seen& at, bool edge, float scale2, float slack, float lift) {
+  // scores of both pages -> weights; masks where edge is set.  again: the second time
+  __device__ __forceinline__ void weigh(typename M::Probs (&pr)[RB], const f32x4 (&sa)[RB], const f32x4 (&sb)[RB], const Seen& at, bool edge, float scale2, float slack, bool again) {
     float all[RB][8], ref[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -480,7 +480,7 @@ struct State {
       }
       if (edge) {
         asm volatile("");   // a branch, not selects in every turn
-        const int left = row_end[rb] - at.base - 4 * at.g, left_a = at.ok_a ? left : 0, left_b = at.ok_b ? left - DF_PAGE : 0;
+        const int left = row_end[rb] - at.base, left_a = at.ok_a ? left : 0, left_b = at.ok_b ? left - DF_PAGE : 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           v[k] = k < left_a ? v[k] : -INFINITY;
@@ -498,13 +498,13 @@ struct State {
       }
       ref[rb] = m_run[rb] == -INFINITY ? 0.f : scale2 * m_run[rb];
     }
-    if (lift != 0.f) {
+    if (again) {
       asm volatile("");
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) all[rb][k] -= m_run[rb] == -INFINITY ? 0.f : m_run[rb];
-        ref[rb] = lift;
+        ref[rb] = kLift;
       }
     }
 #pragma unroll
@@ -519,7 +519,7 @@ struct State {
   // Values where some row does not see some key: those from `end` on are not there; those that are not finite, whose product with a weight of 0 would be NaN, are left out,
   // and whether there are any.
   __device__ __forceinline__ static bool finite_values(typename M::Values& v, const Seen& at, int end) {
-    const bool odd = M::clear(v, at.before(end));
+    const bool odd = M::clear(v, at.before(end - 4 * at.g));
     if (__ballot(odd) == 0) return false;
     M::drop(v);
     return true;
@@ -535,7 +535,7 @@ struct State {
       constexpr int b = decltype(b_c)::value;
       typename M::Values v, w;
       M::template values<b>(v, pa, pb);
-      M::clear(v, at.before(end));
+      M::clear(v, at.before(end - 4 * at.g));
 #pragma unroll
       for (int sign = 0; sign < 2; ++sign) {
         M::mark(w, v, sign);
@@ -655,7 +655,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     int j, h;
     slot_of(row0 + min(r, n_rows - 1), group, j, h);
     const T* p = q_base + ((size_t)(s * (size_t)a.rows + j) * a.n_q_heads + kvh * group + h) * hd;
-    st.row_end[rb] = rows.end(a, j);
+    st.row_end[rb] = rows.end(a, j) - 4 * g;
     if constexpr (Q_LDS) {
       if (wave == rb) {
         typename M::Query f;
@@ -712,7 +712,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     return id;
   };
   bool left_out = false;
-  float lift = 0.f;   // kLift: the second time
+  int again = 0;   // the second time
   auto work = [&](const unsigned char* pair, const Seen& at, bool edge) {   // edge: some row does not see some key
     typename M::Probs pr[RB];
     f32x4 sa[RB], sb[RB];
@@ -734,7 +734,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
     P pa, pb;
     pa.load_v(pair, lane);
     pb.load_v(pair + UNIT, lane);
-    st.weigh(pr, sa, sb, at, edge, scale2, slack, lift);
+    st.weigh(pr, sa, sb, at, edge, scale2, slack, again != 0);
     typename M::Values v[L::F32 ? 1 : NB];   // bf16: all blocks, and one branch for the edge; fp32: block by block
     auto block = [&](auto b_c) -> typename M::Values& { return v[L::F32 ? 0 : decltype(b_c)::value]; };
     unrolled<NB>([&](auto b_c) {
@@ -786,48 +786,52 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
         const int base = c0 + (p0 + k) * 32;
         const bool ok_a = at.a >= 0, ok_b = at.b >= 0;
         const unsigned char* pair = my_ring + slot * PAIR;
-        work(pair, Seen{base, g, ok_a, ok_b}, base + 32 > all_see || !ok_a || !ok_b || lift != 0.f);
+        work(pair, Seen{base, g, ok_a, ok_b}, base + 32 > all_see || !ok_a || !ok_b || again);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the pair has been read before its slot is filled again
         slot ^= 1;
       }
-      if (lift != 0.f || __ballot(st.unsound()) == 0) break;
+      if (again || __ballot(st.unsound()) == 0) break;
       // again: smaller weights, and whatever value is not finite itself is left out of the products
-      lift = kLift;
+      again = 1;
       left_out = false;
       st.clear();
-      ids = there_or_not(load_ids(p0));
-      ids_next = there_or_not(load_ids(p0 + 32));
+      int p = p0;
+      asm volatile("" : "+s"(p));   // (their places, worked out here)
+      ids = there_or_not(load_ids(p));
+      ids_next = there_or_not(load_ids(p + 32));
       asm volatile("" : "+v"(ids), "+v"(ids_next));
     }
     if (left_out)
 #pragma unroll 1
       for (int k = 0; k < n; ++k) {
         const int base = c0 + (p0 + k) * 32, ia = there_or_not(table[min(2 * (p0 + k), last_page)]), ib = there_or_not(table[min(2 * (p0 + k) + 1, last_page)]);
-        if (base + 32 > all_see || ia < 0 || ib < 0 || lift != 0.f) st.template add_left_out<P>(unit_of(ia), unit_of(ib), Seen{base, g, ia >= 0, ib >= 0}, end, lane);
+        if (base + 32 > all_see || ia < 0 || ib < 0 || again) st.template add_left_out<P>(unit_of(ia), unit_of(ib), Seen{base, g, ia >= 0, ib >= 0}, end, lane);
       }
   }
   __syncthreads();   // the wavefronts' outputs overlay the ring
 
   // ---- the wavefronts' results become one ----
+  unsigned thread = threadIdx.x;
+  asm("" : "+v"(thread));   // places are worked out again: kept over the sweep they cost 64 rows' tiles registers that they do not have
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const float l = M::total(st.sum[rb]);
-    if (g == 0) {
-      s_m[wave][rb * 16 + col] = st.m_run[rb];
-      s_l[wave][rb * 16 + col] = lift != 0.f ? l * 0x1p40f : l;
+    if ((thread & 48) == 0) {
+      s_m[wave][rb * 16 + (thread & 15)] = st.m_run[rb];
+      s_l[wave][rb * 16 + (thread & 15)] = again ? l * 0x1p40f : l;
     }
   }
-  if (lane == 0) s_lift[wave] = lift != 0.f ? 0x1p40f : 1.f;
+  if ((thread & 63) == 0) s_lift[wave] = again ? 0x1p40f : 1.f;
   const bool whole = end <= chunk;   // the only range: nothing to merge
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     if (rb * 16 >= n_rows) break;
     if (rb) __syncthreads();
 #pragma unroll
-    for (int t = 0; t < 2 * NB; ++t) *reinterpret_cast<f32x4*>(&s_o[wave][col][t * 16 + 4 * g]) = st.acc[rb][t];
+    for (int t = 0; t < 2 * NB; ++t) *reinterpret_cast<f32x4*>(&s_o[wave][thread & 15][t * 16 + (thread >> 4 & 3) * 4]) = st.acc[rb][t];
     __syncthreads();
     constexpr int LANES = WAVES * 4;   // of a row
-    const int r = threadIdx.x / LANES;
+    const int r = thread / LANES;
     if (rb * 16 + r < n_rows) {
       float m_all = -INFINITY, l = 0.f, f[WAVES];
 #pragma unroll
@@ -845,14 +849,14 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
       const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) f[w] *= inv * s_lift[w];   // the sums' shares, before they are added: a mean is finite where a sum need not be
-      for (int d = 4 * (threadIdx.x % LANES); d < hd; d += 4 * LANES) {
+      for (int d = 4 * (thread % LANES); d < hd; d += 4 * LANES) {
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) o += *reinterpret_cast<const f32x4*>(&s_o[w][r][d]) * f[w];
         if (whole) store_row4(static_cast<T*>(a.out) + at * hd + d, o);
         else *reinterpret_cast<f32x4*>(a.part_o + (in_part + h) * hd + d) = o;
       }
-      if (!whole && threadIdx.x % LANES == 0) a.part_ml[in_part + h] = make_float2(m_all, l);
+      if (!whole && thread % LANES == 0) a.part_ml[in_part + h] = make_float2(m_all, l);
     }
   }
 }
