@@ -130,3 +130,33 @@ def test_values_beyond_the_type_are_infinities(dtype, hd, bits, rows):
     ref, slack, wabs = km.attention64(f64(q), *(np.where(np.abs(t) > 2.0 ** 127, 0.0, t) for t in x.ref.rows(0)), x.table, lens, counts, True, x.n_pages)
     tol = _pair_bound(ref, slack, wabs, dtype)
     assert (np.abs(got - ref)[~bad] <= tol[~bad]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_every_code_and_scale_is_read_back_rounded_once(dtype, bits):
+    """255 pages, one a scale from 2^-127 to 2^127; every code in every place of a row by turns.  Numbers below the smallest normal one keep the bits that the type has for them."""
+    x = Setup(dtype, 2, 1, 64, (bits, bits), 1, [255 * PAGE], layers=1, extra=0)
+    n = 16 if bits == 4 else 256
+    for part in (0, 1):
+        at, shift = x.ref.at[part]
+        code = (np.arange(255)[:, None, None, None] * 5 + np.arange(PAGE)[:, None, None] * 16 + np.arange(2)[:, None] * 32 + np.arange(32)) % n
+        if bits == 8:
+            code = np.where(code & 127 == 127, code ^ 1, code)
+        data = np.zeros((255, x.ref.data.shape[-1]), np.int64)
+        for page in range(255):
+            np.add.at(data[page], at.ravel(), (code[page] << shift).ravel())
+        used = np.unique(at)
+        where = x.table[0, :255]
+        x.ref.data[0, where[:, None], 0, used[None, :]] = data[:, used].astype(np.uint8)
+        x.ref.data[0, where[:, None], 0, x.ref.at[2 + part].ravel()[None, :]] = np.arange(255)[:, None]
+    x.upload()
+    rows = 255 * PAGE
+    k, v = (x.torch.full((1, rows, 1, 64), 9.0, dtype=x.tdt, device=x.e.device) for _ in range(2))
+    x.B.dflash_kvq_read(x.e, x.batch([0], 0), x.cache, 0, k, v, x.ints([0]))
+    x.e.device_status()
+    for got, want in zip((k, v), x.ref.rows(0)):
+        want = x.torch.from_numpy(np.ascontiguousarray(want[x.table[0, :255]].reshape(1, rows, 1, 64))).to(x.tdt)
+        same = (got.cpu() == want) | (want == 0) & (got.cpu() == 0)
+        bad = (~same).nonzero()
+        assert not len(bad), (len(bad), [(int(b[1]) // PAGE, float(got[tuple(b)]), float(want[tuple(b)])) for b in bad[:5]])
