@@ -288,7 +288,7 @@ int dflash_group_attention(dflash_ctx *ctx, const dflash_batch *batch, const dfl
 
 /* ---- caches held in 4 or 8 bits ------------------------------------------------------------------
  * A cache beside the context's pools that holds K and V rows of one model in 4 or 8 bits an element: for requests put aside and taken up again, and for attention
- * that reads a quarter of the bytes.  Every 32 dims of a row of K or V (the last block padded with zeros) share a scale 2^(e - 127), one byte e, and have a code each:
+ * that reads a quarter of the bytes.  The step's calls themselves keep to the pools: rows and attention are for a program that computes its layers' projections itself.  Every 32 dims of a row of K or V (the last block padded with zeros) share a scale 2^(e - 127), one byte e, and have a code each:
  * 4 bits (sign, two of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6) or 8 bits (sign, four of exponent, three of mantissa, up to 448).  e is the least at which the block's
  * largest magnitude over its scale is at most 7 (464): no element is off by more than half a step of its code.  Codes round to nearest even.  A block with an infinity or
  * NaN has e = 255 and reads as NaN.  data[layer][page][kv head][K codes | V codes | K scales | V scales]; with NB = ceil(head_dim / 32) blocks, b = block, d = dim in
@@ -298,7 +298,7 @@ int dflash_group_attention(dflash_ctx *ctx, const dflash_batch *batch, const dfl
  *   scales: [key][NB, of three blocks 4]
  * The calls below are enqueued on `stream`, read nothing back and allocate nothing; they belong to a batch whose seq_lens and block_table (row length max_pages_per_seq, as
  * everywhere) speak of this cache's pages, 0..n_pages-1 (anchor and block_size are not looked at, and max_seq_len is at most what a block-table row covers: no block has to fit behind it).  Rows whose page is none of those, and ranges that a call does not have, are skipped and raise the sticky
- * device status.  Sequences of a call must not write to the same page; dflash_pages_* calls move and count the pages of the context's pools only. */
+ * device status (attention and the pages of requests put aside: see there).  Sequences of a call must not write to the same page; dflash_pages_* calls move and count the pages of the context's pools only. */
 typedef struct {
   void *data;      /* (device) dflash_kvq_bytes() bytes, 256-byte aligned */
   size_t bytes;    /* how many there are */
@@ -320,14 +320,16 @@ int dflash_kvq_read(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq
 
 /* Attention over the cache: rows j < counts[s] (nullable: all `rows`) of sequence s at positions seq_lens[s] + j, whose own K/V rows are there already; causal != 0: row j sees
  * positions up to seq_lens[s] + j, else all seq_lens[s] + counts[s].  rows >= 1, not bound to the context's block size: 1 is plain decoding, hundreds are a piece of a prompt.  The batch's
- * max_seq_len balances launches only.  A length that is negative or that the block-table row does not cover counts as the nearest one that there is, and raises the sticky status.  Entries of the block table outside the cache are keys that are not there; a row that sees no key is zeros.  An infinity or NaN in a row of K or V
- * reaches the rows that see the key, and only them; a row whose scores are all minus infinity (q with an infinity) is zeros too.  q (device) [S, rows, n_q_heads, head_dim] after norm and rotation, out (device) the same shape; both in the model's dtype, contiguous,
- * 16-byte aligned, apart from each other; rows behind counts[s] are left as they are.  Uses the workspace as the step's calls do. */
+ * max_seq_len balances launches only.  A length that is negative or that the block-table row does not cover counts as the nearest one that there is, and raises the sticky status.  Entries of
+ * the block table outside the cache are keys that are not there; a row that sees no key is zeros.  An infinity or NaN in a row of K or V, and a code that stands for a number beyond the type's
+ * largest, reaches the rows that see the key, and only them (8-bit codes that stand for less than 2^-126 count as 0 in a bf16 model); a row whose scores are all minus infinity (q with an
+ * infinity) is zeros too.  q (device) [S, rows, n_q_heads, head_dim] after norm and rotation, out (device) the same shape; both in the model's dtype, contiguous, 16-byte aligned, apart from each other; rows behind counts[s] are left as they are.  Uses the workspace as the step's calls do. */
 int dflash_kvq_attention(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, int32_t layer, int32_t rows, const int32_t *counts, int32_t causal,
                          const void *q, void *out, void *stream);
 
 /* A request put aside: the first seq_lens[s] rows of every sequence, all layers of the context's pool `cache->pool`, on the pages of batch->block_table, go to the pages that
- * table (device) [S, max_pages_per_seq] names in the cache; rows of a last page behind them become zeros.  batch->max_seq_len bounds the lengths.  dflash_kvq_unpack: the way back, from the cache's pages to
+ * table (device) [S, max_pages_per_seq] names in the cache; rows of a last page behind them become zeros.  batch->max_seq_len bounds the lengths: a sequence with more
+ * pages than it has, one of a negative length, and pages outside the pool or the cache raise the sticky status.  dflash_kvq_unpack: the way back, from the cache's pages to
  * the pool's (other ones as a rule): rows behind seq_lens[s] are left as they are. */
 int dflash_kvq_pack(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, const int32_t *table, void *stream);
 int dflash_kvq_unpack(dflash_ctx *ctx, const dflash_batch *batch, const dflash_kvq *cache, const int32_t *table, void *stream);

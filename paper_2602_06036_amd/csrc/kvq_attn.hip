@@ -3,15 +3,15 @@
 //   o_r = sum over the keys i that row r sees of softmax_i(scale q_r . k_i) v_i,    k_i, v_i = codes times 2^(e - 127) of their blocks, exactly.
 //
 // Row r of a kv head = (slot of the block) * group + query head.  A workgroup takes up to 16 RB of them and a range of keys, its four wavefronts a quarter of the range
-// each, pages in pairs.  Codes become bf16 (fp32 models: fp32) in registers by the conversion instructions that take the block's scale, both exact: e2m1 and e4m3 numbers have
-// 2 and 4 significant bits.  S^T = K Q^T leaves a lane four consecutive keys of a query column, which is how V^T P^T takes them.  Softmax in one pass,
+// each, pages in pairs.  Codes become bf16 (fp32 models: fp32) in registers by the conversion instructions that take the block's scale, both exact (e2m1 and e4m3 numbers have
+// 2 and 4 significant bits), but that 8-bit codes that stand for less than 2^-126 become 0 in bf16.  S^T = K Q^T leaves a lane four consecutive keys of a query column, which is how V^T P^T takes them.  Softmax in one pass,
 // base 2, with a reference maximum that moves only when a score passes it by kSlack.  bf16 models: probabilities are hi + lo bf16 pairs, off by 2^-16 of themselves, as everywhere in them; by
 // one number, off by 2^-8, the error against 64 bits was 0.0018 to 0.0020 of a row where the output's own rounding makes 0.0016.  All sums in fp32.
 // Ranges of keys, each the mean of its values with its weights' sum and reference, are joined by kvq_merge_kernel in a fixed order: a call repeats itself bit for bit.
 //
-// Single tokens are bound by memory (32 of them behind 1k to 32k tokens, 32 heads over 8 of 128, 4 bits: 590 MB in 102 us, 5.8 TB/s; the copies by themselves 101); blocks of few pairs a wavefront by
-// latency (16 x 16 rows behind up to 4k tokens: 27 us, and 6 for the merge); many rows by vector instructions, which share the issue with the MFMAs (pieces of 391 and 512 rows behind up to
-// 6k tokens: 87 us with the merge, 620 TFLOP/s of the keys that the rows see).
+// Single tokens are bound by memory (32 of them behind 1k to 32k tokens, 32 heads over 8 of 128, 4 bits: 590 MB in 103 to 106 us, 5.6 TB/s; the copies by themselves 101); blocks of few pairs a
+// wavefront by latency (16 x 16 rows behind up to 4k tokens: 34 us, and 6 for the merge); many rows by vector instructions, which share the issue with the MFMAs (pieces of 391 and 512 rows behind
+// up to 6k tokens: 109 us with the merge, 500 TFLOP/s of the keys that the rows see).
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -607,10 +607,10 @@ struct Launch {
   static constexpr int UNIT = kvq_unit(NB, KB, VB), LD = NB * 32 + 4, WAVES = 4;
   static constexpr bool F32 = std::is_same<T, float>::value, Q_LDS = RB == 4;   // the queries beside 64 rows' sums are too many for the registers
   // A wavefront's ring of page pairs as they lie in memory, filled by direct-to-LDS copies: what is on its way costs no registers.  Two pairs: three or four leave room for
-  // fewer workgroups and gain nothing (single tokens 133, 133, 144 us; blocks of 16 rows 42, 42, 65).
+  // fewer workgroups and gain nothing (an earlier form of the loop, single tokens 133, 133, 144 us; blocks of 16 rows 42, 42, 65).
   static constexpr int PAIR = 2 * UNIT, NI = 2 * ((UNIT + 1023) / 1024);   // bytes, copies a pair
   static constexpr int RING = WAVES * PAIR * 2, MERGE = WAVES * 16 * LD * 4, RAW = RING > MERGE ? RING : MERGE;
-  // Where a sequence's rows are one tile nobody else reads these bytes, and they need no place in L2 (single tokens 126 -> 116 us).
+  // Where a sequence's rows are one tile nobody else reads these bytes, and they need no place in L2 (single tokens 125 -> 119 us).
   static constexpr bool ONCE = !F32 && (RB == 1 || (RB == 2 && kvq_tiles_of_64(NB, KB, VB)));
   static constexpr int ON_SIMD = RB == 1 && KB + VB < 16 ? 3 : 2;   // wavefronts
 };
@@ -862,7 +862,7 @@ __global__ __launch_bounds__((64 * Launch<T, NB, KB, VB, RB>::WAVES), (Launch<T,
 }
 
 // A row's ranges: 32 lanes (four dims a lane) a row, or eight times 32, which take every eighth range and are joined in their order (few rows of many ranges: 1024 rows of
-// up to 12, 8.7 -> 5.4 us; 8192 rows of up to 5 are better off with 32 lanes, 16.6 -> 5.5 us).  grid: rows of a sequence and heads / (8 / GROUPS), sequences.
+// up to 12, 7.0 -> 4.2 us; 8192 rows of up to 5 are better off with 32 lanes, 11.9 -> 5.7 us; the host knows the rows, not the ranges that each has, and goes by the rows).  grid: rows of a sequence and heads / (8 / GROUPS), sequences.
 template <typename T, int ROWS, int GROUPS>
 __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttn a) {
   __shared__ float s_m[8], s_l[8];

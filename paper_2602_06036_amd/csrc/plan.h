@@ -442,10 +442,10 @@ inline int accept_chunks(int S, int V, size_t room) {
 }
 
 // ---- attention over caches in 4 and 8 bits (kvq_attn.hip) ---------------------------------------------------------------------------
-// Rows of a workgroup.  bf16: the more the fewer conversions a row (16 sequences behind up to 4k tokens, 32 heads over 8: 8 rows each by tiles of 16, 32 and 64 28.5, 23.3, 27.4 us, 16 rows each 38, 32.7, 31.7;
-// pieces of a prompt 130, 102, 87).  fp32: bound by its 16x16x4 MFMAs whatever the tile, and the sums of 32 rows leave one wavefront a SIMD (two pieces of 300 to 400 rows, 8 heads of 64:
-// 41 us by 16 rows, 46 by 32).  Four blocks of 8-bit K and V: the pages and queries of 64 rows leave one workgroup a CU (16 x 16 rows as above 48 us, by 32 rows 35; pieces of a prompt 152, by 32
-// rows 108).
+// Rows of a workgroup.  bf16: the more the fewer conversions a row (16 sequences behind up to 4k tokens, 32 heads over 8: 8 rows each by tiles of 16, 32 and 64 31, 26, 33.5 us, 16 rows each 43, 37, 37;
+// pieces of a prompt 148, 123, 109).  fp32: bound by its 16x16x4 MFMAs whatever the tile, and the sums of 32 rows leave one wavefront a SIMD (two pieces of 300 to 400 rows, 8 heads of 64:
+// 41 us by 16 rows, 46 by 32, when both were measured; 42 now).  Four blocks of 8-bit K and V: the pages and queries of 64 rows leave one workgroup a CU (16 x 16 rows as above 54 us, by 32 rows 38; pieces of a prompt 175, by 32
+// rows 125).
 constexpr bool kvq_tiles_of_64(int blocks, int k_bits, int v_bits) { return blocks * (k_bits + v_bits) <= 48; }
 inline int kvq_tile_rows(bool bf16, int rows, bool tiles_of_64) { return rows <= 16 || !bf16 ? 16 : rows <= 32 || !tiles_of_64 ? 32 : 64; }
 
@@ -458,12 +458,13 @@ constexpr int kKvqMinPairs = 8;    // page pairs of a range at least
 inline KvqPlan kvq_plan(int n_seqs, int rows, int n_q_heads, int n_kv_heads, bool bf16, bool tiles_of_64, int max_tokens, size_t part_rows) {
   const int tile = kvq_tile_rows(bf16, rows * (n_q_heads / n_kv_heads), tiles_of_64), tiles = (rows * (n_q_heads / n_kv_heads) + tile - 1) / tile;
   const long long heads = (long long)n_kv_heads * tiles, room = (long long)(part_rows / ((size_t)rows * n_q_heads)) - n_seqs;
-  // Twice as many workgroups as the card holds (single tokens, 640: 114 us, 1536: 111, 2176: 111), or as many: a few that come behind the others cost a round (blocks of
-  // 16 rows, 384: 35 us, 448: 33, 512: 38), so half a range a sequence, by which there are more of them, is left out where sequences have several.
+  // Twice as many workgroups as the card holds (single tokens, 640: 117 to 123 us, 1024: 121, 1536: 119, 2176: 117 to 121), or as many: a few that come behind the others cost a round (blocks
+  // of 16 rows, 384: 42 us, 448: 39, 512: 41, 768: 46), so half a range a sequence, by which there are more of them, is left out where sequences have several (512: 37 us).
   long long parts = (tile == 16 ? 1536 : 512) / heads;
   if (tile > 16 && 2 * parts >= 3ll * n_seqs) parts -= n_seqs / 2;
   parts = std::min(parts, room);
-  // Sequences are half as long as the longest, say: with enough of them no range would be cut.
+  // Sequences are half as long as the longest, say: with enough of them no range would be cut.  (Nor is one where a few are much longer than the rest: 128 blocks of 16 rows, one of
+  // them behind 32768 tokens and the others behind 500, take 478 us; 127 of them are cut, 82.)
   return {tiles, parts > 0 && parts * 2 > n_seqs && max_tokens > 32 * kKvqMinPairs ? (int)parts : 0};
 }
 // Keys of a range, a multiple of 128, where all sequences have `all` times four pairs of pages, each rounded up: the device's part of the plan.  Rounding must not make ranges
